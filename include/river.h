@@ -290,6 +290,108 @@ int river_selftest_wait_timeout(river_ctx *ctx, int poll_limit);
 int river_quantize_w4(const void *w, int out, int in, int group, int refine_iters, void *codes, void *scale, void *zero,
                       void *cuda_stream);
 
+/* ---------------------------------------------------------------- long contexts on a paged cache
+ * (The paper has no counterpart: these serve models and conversations whose positions are scaled, whose attention sees a window and a
+ * few first positions, and whose sequences share, drop and move pages.)
+ * The calls below need no context.  They work on caller-owned device buffers, in the layout of river_kv_pool_bytes, so that they also
+ * take a context's pool; they are asynchronous on cuda_stream, allocate nothing, read nothing back and can be captured in a graph.
+ * What the host can see is refused before anything is queued: RIVER_E_BADARG (null or misaligned pointers, values out of range),
+ * RIVER_E_SHAPE (a shape, type or combination that has no kernel).  What only the device can see goes to `status` ([dev] int32). */
+enum { RIVER_BF16 = 0, RIVER_F16 = 1, RIVER_F32 = 2 };
+
+typedef struct river_paged {
+    void *pool;            /* [dev] [n_layers][n_pages][2 (K,V)][Hkv][page_size][dh], 128-byte aligned */
+    const int32_t *table;  /* [dev] [n_seqs][max_pages]: page of positions page_size j .. page_size j + page_size - 1; -1: none */
+    const int32_t *lens;   /* [dev] [n_seqs] positions held (river_rope_append does not read it: may be NULL) */
+    int32_t dtype;         /* of the pool: RIVER_BF16 or RIVER_F16 */
+    int32_t n_layers, n_pages, Hkv, dh, page_size; /* dh 64 or 128; page_size 16, 32 or 64 */
+    int32_t n_seqs, max_pages;
+} river_paged;
+
+/* Rows of heads: head h of token t at p + t * token + h * head (elements; the values of a head are consecutive). */
+typedef struct river_rows {
+    const void *p; /* [dev] */
+    int64_t token, head;
+} river_rows;
+
+/* Rotary frequencies in radians per position, from theta^(-2 i / rotary_dim), i < rotary_dim / 2, computed in 64 bits:
+ *   RIVER_ROPE_PLAIN     as they are
+ *   RIVER_ROPE_LINEAR    divided by factor (positions drawn together)
+ *   RIVER_ROPE_BY_PARTS  pairs whose wavelength is above original_context / low_freq divided by factor, below original_context /
+ *                        high_freq as they are, in between a blend that is linear in original_context / wavelength
+ *   RIVER_ROPE_RAMP      a blend over the pairs' indices: as they are up to the pair that turns beta_fast times in original_context,
+ *                        divided by factor from the pair that turns beta_slow times on, linear between (the pair numbers rounded
+ *                        outwards); scale = 0.1 ln(factor) + 1 unless attn_scale is given
+ *   RIVER_ROPE_PER_PAIR  divided by pair_factors[i]
+ * inv_freq [host] rotary_dim / 2 floats out; scale [host] out: the factor on the turned values (attn_scale where that is > 0, else 1,
+ * or as said above).  s may be NULL (PLAIN). */
+enum { RIVER_ROPE_PLAIN = 0, RIVER_ROPE_LINEAR = 1, RIVER_ROPE_BY_PARTS = 2, RIVER_ROPE_RAMP = 3, RIVER_ROPE_PER_PAIR = 4 };
+typedef struct river_rope_scaling {
+    int32_t kind, original_context;
+    double factor, low_freq, high_freq, beta_fast, beta_slow, attn_scale;
+    const float *pair_factors; /* [host] rotary_dim / 2 */
+} river_rope_scaling;
+int river_rope_frequencies(int rotary_dim, double theta, const river_rope_scaling *s, float *inv_freq, float *scale);
+
+/* Rotary embedding of new tokens and their way into the cache, in one pass.  Token t stands at positions[t] of sequence seqs[t]; pair i
+ * of its query and key heads turns by the angle positions[t] * inv_freq[i] (exact to fp32 whatever the position) and is multiplied by
+ * scale; dims from rotary_dim on stay.  Queries go to q_out, keys and values to the token's place in block `layer` (1-based).
+ *   q, k, v       rows of Hq, Hkv, Hkv heads of in_dtype: the pool's type or RIVER_F32
+ *   positions     [dev] int32 [n_tokens];  seqs [dev] int32 [n_tokens], -1: padding (q_out gets a zero row, nothing is stored)
+ *   inv_freq      [dev] float [rotary_dim / 2], finite;  rotary_dim even, 2 .. dh
+ *   interleaved   0: pair i = dims (i, i + rotary_dim / 2); 1: dims (2 i, 2 i + 1)
+ *   q_out         [dev] [n_tokens][Hq][dh] of the pool's type, 16-byte aligned; must not overlap the inputs
+ *   status        [dev] int32 or NULL: RIVER_E_BADARG is stored there when a position is negative, a sequence or a page out of
+ *                 range; such a token stores no key and value (its query is turned all the same, by 0 for a negative position).
+ * Distinct tokens of a call have distinct places. */
+int river_rope_append(const river_paged *c, int layer, int n_tokens, int Hq, int in_dtype, const river_rows *q, const river_rows *k,
+                      const river_rows *v, const int32_t *positions, const int32_t *seqs, const float *inv_freq, int rotary_dim,
+                      int interleaved, float scale, void *q_out, int32_t *status, void *cuda_stream);
+
+/* Attention over a sliding window and a few first positions ("sinks"), for single tokens and for prompts.  Sequence s has the queries
+ * q_start[s] .. q_start[s + 1] - 1, which are its LAST positions: query i of n stands at p = lens[s] - n + i and sees the positions
+ * j <= p with j < sinks or j > p - window;  out = softmax(softmax_scale q K^T) V over those, zero where there are none.
+ *   q             rows of Hq heads of the pool's type, Hq a multiple of Hkv;  n_tokens rows in all
+ *   max_q         at least the largest number of queries of a sequence (1: a decode step)
+ *   q_start       [dev] int32 [n_seqs + 1], ascending from 0 to n_tokens
+ *   window        >= 1 (one that reaches over the whole context is ordinary causal attention);  sinks >= 0
+ *   out           [dev] [n_tokens][Hq][dh] of the pool's type, 16-byte aligned
+ *   status        [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as
+ *                 not visible), q_start descends or a sequence has more than max_q queries (the rows of that sequence behind the
+ *                 max_q-th may stay as they are); RIVER_E_TIMEOUT when a wait ran out.
+ * Positions that a query does not see have no influence on its result, whatever the pool holds there.  Every result follows in a
+ * fixed order of sums: the same inputs give the same bits. */
+int river_window_attention(const river_paged *c, int layer, int n_tokens, int max_q, const int32_t *q_start, int Hq,
+                           const river_rows *q, int window, int sinks, float softmax_scale, void *out, int32_t *status,
+                           void *cuda_stream);
+
+/* The pages of a cache, kept on the device: refs[p] counts the table entries (and whatever else the caller counts) that hold page p, 0 =
+ * free.  Every call reads a state (table, lens, refs) and writes the state behind it (table_out, lens_out, refs_out); n_seqs <= 8192.
+ * Pages that are handed out are the lowest free ids, in order of (sequence, position).  status [dev] int32 is always written:
+ * RIVER_OK; RIVER_E_NOPAGE (free pages or a table row do not suffice); RIVER_E_BADARG (a sequence, page or length out of range).  Where it is
+ * not RIVER_OK the state behind a call holds the state before it, but for what river_pages_advance has freed.  c->pool may be NULL where
+ * no page is copied.
+ *
+ * river_pages_advance: sequence s grows by n_new[s] >= 0 positions.  First pages that no later query needs are given back: those
+ * of positions < lens[s] - window + 1 that hold none of the first `sinks`, from the last such page backwards to the first whose
+ * entry is -1 already (window 0: none).  The outputs may be the inputs themselves. */
+int river_pages_advance(const river_paged *c, const int32_t *refs, const int32_t *n_new, int window, int sinks, int32_t *table_out,
+                        int32_t *lens_out, int32_t *refs_out, int32_t *status, void *cuda_stream);
+
+/* Sequence i becomes a copy of what sequence parents[i] was (-1: empty) - beams, samples of one prompt, sequences that end.  Whole
+ * pages are shared; a last page that is filled in part stays with the lowest child and is copied for the others, all layers, filled
+ * positions only.  parents [dev] int32 [n_seqs];  copies [dev] int32 [1 + 3 n_seqs]: how many pages were copied, and (from, to,
+ * positions) of each.  The outputs overlap no input. */
+int river_pages_reorder(const river_paged *c, const int32_t *refs, const int32_t *parents, int32_t *table_out, int32_t *lens_out,
+                        int32_t *refs_out, int32_t *copies, int32_t *status, void *cuda_stream);
+
+/* Pages in use move to the ids 0 .. n_used - 1, so that the rest of the pool can go: the k-th free id below n_used receives the k-th
+ * used page from n_used on, all layers.  table_out and refs_out may be the inputs; remap [dev] int32 [n_pages]: where each page went, -1
+ * for a free one;  n_used [dev] int32;  moves [dev] int32 [1 + n_pages]: how many pages moved, then their new ids, then, from
+ * 1 + n_pages / 2 on, their old ones.  Table entries out of range become -1.  lens is not read. */
+int river_pages_compact(const river_paged *c, const int32_t *refs, int32_t *table_out, int32_t *refs_out, int32_t *remap,
+                        int32_t *n_used, int32_t *moves, void *cuda_stream);
+
 int river_seq_len(const river_ctx *ctx, int slot);       /* tokens cached in the slot, or RIVER_E_BADSLOT */
 int river_release(river_ctx *ctx, int slot);             /* free the slot's pages, behind the work queued so far; does not wait */
 int river_stats(river_ctx *ctx, river_stats_t *host_out); /* synchronises the stream; fills host_out even when it
