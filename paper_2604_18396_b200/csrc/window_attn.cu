@@ -2,27 +2,11 @@
 #include <algorithm>
 #include <cmath>
 
-#include "window_attn_step.cuh"
+#include "tensor_maps.h"
+#include "window_attn_prompt.cuh"
 
 namespace river {
 namespace {
-
-// grid (max_q * Hq / warps, n_seqs): a warp per query row
-template <class T, int DH>
-__global__ void __launch_bounds__(128) window_attn_rows_kernel(const WindowArgs a) {
-    const int seq = blockIdx.y, row = blockIdx.x * 4 + (threadIdx.x >> 5), i = row / a.Hq, head = row % a.Hq;
-    const int t0 = a.q_start[seq], n = a.q_start[seq + 1] - t0;
-    if (n < 0 || n > a.max_q || t0 < 0 || t0 + n > a.n_tokens) {
-        if (threadIdx.x == 0) flag(a.status, RIVER_E_BADARG);
-        return;
-    }
-    if (i < n) window_attn_row<T, DH>(a, t0 + i, head, seq, a.c.lens[seq] - n + i);
-}
-
-template <class T, int DH>
-void launch_rows(const WindowArgs &a, cudaStream_t st) {
-    window_attn_rows_kernel<T, DH><<<dim3((a.max_q * a.Hq + 3) / 4, a.c.n_seqs), 128, 0, st>>>(a);
-}
 
 template <class T, int DH>
 void launch_step(const WindowArgs &a, cudaStream_t st) {
@@ -40,9 +24,30 @@ void launch_step(const WindowArgs &a, cudaStream_t st) {
 }
 
 template <class T, int DH>
-void launch(const WindowArgs &a, cudaStream_t st) {
-    if (a.max_q <= 4) launch_step<T, DH>(a, st);
-    else launch_rows<T, DH>(a, st);
+int launch_prompt(const WindowArgs &a, cudaStream_t st) {
+    const int per = kWpRows / (a.Hq / a.c.Hkv);
+    PromptArgs pa = {a, 2};
+    auto ctas = [&] { return (int64_t)(a.n_tokens / (per * pa.tiles) + a.c.n_seqs) * a.c.Hkv; };
+    if (ctas() < 148) pa.tiles = 1;
+    // the pages of this block, as rows of a head's dims
+    CUtensorMap map;
+    const size_t rows = (size_t)a.c.n_pages * 2 * a.c.Hkv << a.c.ps_log2;
+    if (rows >= (1ull << 31)) return RIVER_E_SHAPE;
+    if (!make_map_bf16(&map, a.c.pool + rows * DH * 2 * a.layer0, DH, rows, 16)) return RIVER_E_DEVICE;
+    const size_t smem = window_attn_prompt_smem();
+    if (cudaFuncSetAttribute(window_attn_prompt_kernel<T, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return RIVER_E_DEVICE;
+    window_attn_prompt_kernel<T, DH><<<(unsigned)ctas(), kWpThreads, smem, st>>>(map, pa);
+    return RIVER_OK;
+}
+
+template <class T, int DH>
+int launch(const WindowArgs &a, cudaStream_t st) {
+    const int gq = a.Hq / a.c.Hkv;
+    if (a.max_q <= 4 || gq > kWpRows) {
+        launch_step<T, DH>(a, st);
+        return RIVER_OK;
+    }
+    return launch_prompt<T, DH>(a, st);
 }
 
 }  // namespace
@@ -74,7 +79,7 @@ extern "C" int river_window_attention(const river_paged *c, int layer, int n_tok
     a.out = out;
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (c->dtype == RIVER_BF16) c->dh == 64 ? launch<__nv_bfloat16, 64>(a, st) : launch<__nv_bfloat16, 128>(a, st);
-    else c->dh == 64 ? launch<__half, 64>(a, st) : launch<__half, 128>(a, st);
-    return launch_rc();
+    const int rc = c->dtype == RIVER_BF16 ? (c->dh == 64 ? launch<__nv_bfloat16, 64>(a, st) : launch<__nv_bfloat16, 128>(a, st))
+                                          : (c->dh == 64 ? launch<__half, 64>(a, st) : launch<__half, 128>(a, st));
+    return rc ? rc : launch_rc();
 }

@@ -1,0 +1,367 @@
+// Windowed attention of prompts on tcgen05 (sm_100a, internal).
+//
+// A CTA owns two tiles of 128 query rows - 128 / GQ consecutive tokens of one sequence x the GQ query heads of one KV head, token by
+// token - and walks the blocks of 16 positions that some of its rows see (those of the sinks, then those of the windows' union), eight
+// blocks = 128 keys at a time.  Both tiles use the same K and V:
+//   S [128 x 128] = Q K^T     Q and K in shared memory, S in tensor memory
+//   O [128 x DH] += P V       P (rounded to the inputs' type) in tensor memory over the place of S, V as it lies in the cache
+//   warp 0        TMA: K and V pages, one 16 x 64 box per lane, two stages each
+//   warp 1        tensor memory; one lane issues the MMAs: P V of a tile, S of its next keys, then the other tile's, so that the softmax of
+//                 one tile runs under the MMAs of the other
+//   warps 4..11   softmax, four per tile: thread = query row = TMEM lane; online, base 2, fp32; all 128 scores of a row in registers; O is
+//                 rescaled only when a row's maximum has grown by more than 2^8 since it last was.  P goes out in two halves.
+//
+// P in 16 bits: its rounding weighs as much as the rounding of the result (2^-9 of sum p |v| against 2^-9 of the result in bf16, both
+// random), and one product instead of two is half of the tensor pipe's work.
+//
+// Hidden positions: scores are replaced, not added to; V rows that no row of the CTA sees are set to zero in shared memory.  A row of V
+// that some rows see and others do not is harmless as long as it is finite (0 x v); tiles that have such rows are looked through,
+// and where one holds no number the CTA computes its rows again one by one (window_attn_row).
+#pragma once
+#include "attn_prefill_tc.cuh"
+#include "window_attn_step.cuh"
+
+namespace river {
+
+constexpr int kWpRows = 128, kWpKeys = 128, kWpThreads = 384;
+constexpr float kWpLazy = 8.f;  // growth of a row's maximum (log2) that O waits for before it is rescaled
+
+struct PromptArgs {
+    WindowArgs w;
+    int tiles;  // query tiles of a CTA: 2, or 1 where there are few
+};
+
+__device__ __forceinline__ void wp_ld32(uint32_t taddr, uint32_t (&r)[32]) {  // left under way (wp_ld_wait)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void wp_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Nothing that uses r moves above this point (the compiler does not know that r is filled only at the wait).
+__device__ __forceinline__ void wp_pin(uint32_t (&r)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+template <class T, int DH>
+__device__ __noinline__ void window_attn_rows_again(const WindowArgs &a, int tok0, int n_tok, int kvh, int gq, int seq, int pos0) {
+    for (int r = (threadIdx.x >> 5) - 4; r < n_tok * gq; r += 8)
+        window_attn_row<T, DH>(a, tok0 + r / gq, kvh * gq + r % gq, seq, pos0 + r / gq);
+}
+
+// The sequence whose tiles hold slot x: sequence s has the slots from q_start[s] / per + s on, enough for its queries.
+__device__ __forceinline__ int prompt_seq(const int32_t *q_start, int n_seqs, int per, int x) {
+    int lo = 0, hi = n_seqs;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (q_start[mid] / per + mid <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+template <class T, int DH>
+__global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const __grid_constant__ CUtensorMap tmap, const PromptArgs pa) {
+    const WindowArgs &a = pa.w;
+    constexpr int NB = DH / 64;                                          // blocks of 64 dims
+    constexpr uint32_t QB = kWpRows * 128, KB = kWpKeys * 128;           // bytes of one block of Q / of K or V
+    constexpr uint32_t kO = 256;                                         // TMEM: tile q has S / P in columns 128 q .., O in 256 + DH q ..
+    constexpr uint32_t kIdS = (1u << 4) | (sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) |
+                              ((uint32_t)(kWpRows >> 4) << 24) | ((uint32_t)(kWpKeys >> 3) << 17);
+    constexpr uint32_t kIdO = (kIdS & ~(0x3Fu << 17)) | ((uint32_t)(DH >> 3) << 17) | (1u << 16);  // (B of the second product: N-major)
+    extern __shared__ uint8_t wp_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(wp_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *const sq = smem, *const sk = sq + 2 * NB * QB, *const sv = sk + 2 * NB * KB;  // [tile] / [stage] [NB][128 rows][128 bytes]
+    __shared__ uint64_t bars[16];
+    __shared__ uint32_t s_tmem, s_valid[2];
+    __shared__ int s_abort, s_err, s_poison;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int gq = a.Hq / a.c.Hkv, per = kWpRows / gq;  // tokens of a tile
+    // heavy tiles, those behind a long history, first
+    const int kvh = blockIdx.x % a.c.Hkv, slot = gridDim.x / a.c.Hkv - 1 - blockIdx.x / a.c.Hkv;
+    const int seq = prompt_seq(a.q_start, a.c.n_seqs, per * pa.tiles, slot);
+    const int first = a.q_start[seq], n = a.q_start[seq + 1] - first, at = (slot - (first / (per * pa.tiles) + seq)) * per * pa.tiles;
+    if (blockIdx.x == 0)
+        for (int s = tid; s < a.c.n_seqs; s += kWpThreads) {
+            const int x = a.q_start[s], y = a.q_start[s + 1];
+            if (x < 0 || y < x || y > a.n_tokens || y - x > a.max_q) flag(a.status, RIVER_E_BADARG);
+        }
+    if (first < 0 || n < 0 || first + n > a.n_tokens || at < 0 || at >= n) return;
+    const int n_tok = min(n - at, per * pa.tiles), tok0 = first + at, pos0 = a.c.lens[seq] - n + at, last_pos = pos0 + n_tok - 1;
+    const int nq = n_tok > per ? 2 : 1;
+
+    const uint32_t b_k = smem_u32(&bars[0]), b_v = smem_u32(&bars[2]), b_kf = smem_u32(&bars[4]), b_vf = smem_u32(&bars[6]), b_s = smem_u32(&bars[8]),
+                   b_p = smem_u32(&bars[10]), b_o = smem_u32(&bars[14]);
+    volatile int *abortp = &s_abort;
+    if (tid == 0) {
+        s_abort = s_err = s_poison = 0;
+        for (int i = 0; i < 16; ++i) mbar_init(smem_u32(&bars[i]), i >= 10 && i < 14 ? 4 : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        tc_alloc(smem_u32(&s_tmem), 512u);
+        tc_fence_before();
+    }
+    // blocks of 16 positions: n_sb of the sinks, then wb0 .. last_pos / 16; a column is a place on that list, of position column
+    // (sinks) or column + shift
+    const int low0 = window_low(pos0, a.window), wb0 = low0 >> 4, n_sb = min((min(a.sinks, low0) + 15) >> 4, wb0), shift = 16 * (wb0 - n_sb);
+    const int nb = last_pos < 0 ? 0 : n_sb + (last_pos >> 4) - wb0 + 1, n_kt = (nb + 7) / 8;
+
+    // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
+    const uint32_t turn = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+    for (int u = tid; u < nq * kWpRows * (DH / 8); u += kWpThreads) {
+        const int r = u / (DH / 8), c8 = u % (DH / 8), q = r / kWpRows, rr = r % kWpRows, p = q * per + rr / gq, g = rr % gq;
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (rr < per * gq && p < n_tok) {
+            x = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + (tok0 + p) * a.q_tok + (kvh * gq + g) * a.q_head + 8 * c8);
+            x.x ^= turn; x.y ^= turn; x.z ^= turn; x.w ^= turn;
+        }
+        *reinterpret_cast<uint4 *>(sq + q * NB * QB + (c8 >> 3) * QB + rr * 128 + (((c8 & 7) ^ (rr & 7)) * 16)) = x;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 0) {
+            const int32_t *tbl = a.c.table + (size_t)seq * a.c.max_pages;
+            const int blk = lane / NB, half = lane % NB, bpp = a.c.ps_log2 - 4;
+            for (int j = 0; j < n_kt; ++j) {
+                const int st = j & 1, u = 8 * j + blk, b = u < n_sb ? u : wb0 + u - n_sb;
+                const bool on = blk < 8 && u < nb;
+                int page = -1;
+                if (on) {
+                    const int col = b >> bpp;
+                    page = col < a.c.max_pages ? tbl[col] : -1;
+                    if (page < 0 || page >= a.c.n_pages) { page = -1; s_err = DEV_BAD_PAGE; }
+                }
+                const unsigned got = __ballot_sync(0xffffffffu, page >= 0);
+                const uint32_t bytes = (uint32_t)__popc(got) * 16 * 128;
+                const int row = page < 0 ? 0 : ((page * 2 * a.c.Hkv + kvh) << a.c.ps_log2) + ((b << 4) & ((1 << a.c.ps_log2) - 1));
+                int good = 1;
+                if (lane == 0 && j >= 2) good = mbar_wait(b_kf + 8 * st, ((j >> 1) - 1) & 1, abortp, &s_err) ? 1 : 0;
+                if (lane == 0 && good) mbar_expect_tx(b_k + 8 * st, bytes);
+                if (!__shfl_sync(0xffffffffu, good, 0)) break;
+                if (page >= 0) tma_load_2d(smem_u32(sk) + (st * NB + half) * KB + blk * 2048, &tmap, 64 * half, row, b_k + 8 * st);
+                if (lane == 0 && j >= 2) good = mbar_wait(b_vf + 8 * st, ((j >> 1) - 1) & 1, abortp, &s_err) ? 1 : 0;
+                if (lane == 0 && good) {
+                    uint32_t valid = 0;  // blocks that are there, for the softmax
+                    for (int i = 0; i < 8; ++i) valid |= ((got >> (i * NB)) & 1u) << i;
+                    s_valid[st] = valid;
+                    mbar_expect_tx(b_v + 8 * st, bytes);
+                }
+                if (!__shfl_sync(0xffffffffu, good, 0)) break;
+                if (page >= 0) tma_load_2d(smem_u32(sv) + (st * NB + half) * KB + blk * 2048, &tmap, 64 * half, row + (a.c.Hkv << a.c.ps_log2), b_v + 8 * st);
+            }
+        } else if (warp == 1 && lane == 0) {
+            const uint64_t dq = tc_smem_desc(smem_u32(sq)), dk = tc_smem_desc(smem_u32(sk)), dv = pt_desc_n(smem_u32(sv), KB);
+            auto scores = [&](int q, int j) {
+                if (q == 0 && !mbar_wait(b_k + 8 * (j & 1), (j >> 1) & 1, abortp, &s_err)) return false;
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < DH / 16; ++k)
+                    tc_mma(tmem + 128u * q, dq + (q * NB + (k >> 2)) * (QB >> 4) + 2 * (k & 3), dk + ((j & 1) * NB + (k >> 2)) * (KB >> 4) + 2 * (k & 3), kIdS, k ? 1u : 0u);
+                tc_commit(b_s + 8 * q);
+                if (q == nq - 1) tc_commit(b_kf + 8 * (j & 1));
+                return true;
+            };
+            auto values = [&](int q, int j) {
+                if (q == 0 && !mbar_wait(b_v + 8 * (j & 1), (j >> 1) & 1, abortp, &s_err)) return false;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {  // half of the keys
+                    if (!mbar_wait(b_p + 8 * (2 * q + h), j & 1, abortp, &s_err)) return false;
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)  // 16 keys: 8 columns of P, 2048 bytes of V
+                        tc_mma_ts(tmem + kO + (uint32_t)DH * q, tmem + 128u * q + 32 * h + 8 * k, dv + (j & 1) * (NB * KB >> 4) + (4 * h + k) * (2048 >> 4), kIdO, (j | h | k) ? 1u : 0u);
+                }
+                if (q == nq - 1) tc_commit(b_vf + 8 * (j & 1));
+                if (j == n_kt - 1) tc_commit(b_o + 8 * q);
+                return true;
+            };
+            bool ok = n_kt > 0;
+            for (int q = 0; q < nq && ok; ++q) ok = scores(q, 0);
+            for (int j = 0; j < n_kt && ok; ++j)
+                for (int q = 0; q < nq && ok; ++q) ok = values(q, j) && (j + 1 == n_kt || scores(q, j + 1));
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int q = (warp - 4) >> 2, r = 32 * (warp & 3) + lane, p = q * per + r / gq;
+        const bool live = r < per * gq && p < n_tok;
+        if (q < nq) {
+            const int pos = pos0 + min(p, n_tok - 1);
+            const int c_sink = min(a.sinks, max(pos + 1, 0)), c_lo = window_low(pos, a.window) - shift, c_hi = pos + 1 - shift;  // columns seen: [0, c_sink), [c_lo, c_hi)
+            // over all rows of the CTA
+            const int all_lo = window_low(last_pos, a.window) - shift, all_hi = pos0 + 1 - shift, any_lo = low0 - shift, any_hi = last_pos + 1 - shift;
+            const int all_sink = min(a.sinks, max(pos0 + 1, 0)), any_sink = min(a.sinks, last_pos + 1);
+            const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + 128u * q + quarter, t_o = tmem + kO + (uint32_t)DH * q + quarter;
+            const float c = fmaxf(fabsf(a.scale_log2), 1e-30f);  // (a scale of 0: every score 0, hidden ones -inf still)
+            float m = -CUDART_INF_F, l = 0.f;
+            bool ok = true;
+            for (int j = 0; j < n_kt; ++j) {
+                const int c0 = 128 * j, st = j & 1;
+                bool part = !(c0 >= all_lo && c0 + 128 <= all_hi) && !(c0 + 128 <= all_sink);
+                uint32_t valid = 0xffu;
+                // (which blocks are there is written before the barrier of V; K's tells of nothing missing only together with it)
+                ok = __all_sync(0xffffffffu, mbar_wait(b_v + 8 * st, (j >> 1) & 1, abortp, &s_err));
+                if (!ok) break;
+                valid = s_valid[st];
+                part = part || valid != 0xffu;
+                if (part && q == 0) {  // thread = V row: those that nobody sees become zero, the others are looked through
+                    const int cc = c0 + r;
+                    const bool any = (valid >> (r >> 4) & 1u) && (cc < any_sink || (cc >= any_lo && cc < any_hi));
+                    uint8_t *row = sv + st * NB * KB + r * 128;
+                    bool odd = false;
+#pragma unroll
+                    for (int i = 0; i < DH / 8; ++i) {
+                        uint4 *x = reinterpret_cast<uint4 *>(row + (i >> 3) * KB + (((i & 7) ^ (r & 7)) * 16));
+                        if (!any) {
+                            *x = make_uint4(0u, 0u, 0u, 0u);
+                        } else {
+                            constexpr uint32_t E = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;  // the exponent of what is no number
+                            const uint4 y = *x;
+                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) odd = odd || (w[e] & E) == E || (w[e] >> 16 & E) == E;
+                        }
+                    }
+                    if (odd) s_poison = 1;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                ok = __all_sync(0xffffffffu, mbar_wait(b_s + 8 * q, j & 1, abortp, &s_err));
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) wp_ld32(t_s + 32 * i, s[i]);
+                wp_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) wp_pin(s[i]);
+                if (part) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int cc = c0 + 32 * i + e;
+                            if (!((cc < c_sink || (cc >= c_lo && cc < c_hi)) && (valid >> (2 * i + (e >> 4)) & 1u))) s[i][e] = 0xff800000u;  // -inf
+                        }
+                }
+                float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[e & 3] = fmaxf(x[e & 3], __uint_as_float(s[i][e]));
+                const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * c;
+                const bool grow = mx > m + kWpLazy || (m == -CUDART_INF_F && mx > m);
+                if (__any_sync(0xffffffffu, grow)) {
+                    const float corr = grow ? ex2(m - mx) : 1.f;
+                    if (grow) m = mx;
+                    l *= corr;
+                    if (j > 0) {  // (the MMAs that wrote O are complete: S of these keys was issued behind them)
+#pragma unroll 1
+                        for (int d = 0; d < DH; d += 32) {
+                            uint32_t o[32];
+                            wp_ld32(t_o + d, o);
+                            wp_ld_wait();
+                            wp_pin(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr);
+                            tc_st32(t_o + d, o);
+                        }
+                    }
+                }
+                const float base = m == -CUDART_INF_F ? 0.f : m;
+                const uint64_t c2 = f2_pack(c, c), m2 = f2_pack(-base, -base);
+                uint64_t sum = 0ull;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        float p0, p1;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[2 * h + (e >> 4)][2 * (e & 15)]), __uint_as_float(s[2 * h + (e >> 4)][2 * (e & 15) + 1])), c2, m2), p0, p1);
+                        p0 = ex2(p0);
+                        p1 = ex2(p1);
+                        sum = f2_add(sum, f2_pack(p0, p1));
+                        w[e] = pack_pair<T>(p0, p1);
+                    }
+                    tc_st32(t_s + 32 * h, w);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_p + 8 * (2 * q + h));
+                }
+                float l0, l1;
+                f2_unpack(sum, l0, l1);
+                l += l0 + l1;
+            }
+            if (ok && n_kt > 0) ok = __all_sync(0xffffffffu, mbar_wait(b_o + 8 * q, 0, abortp, &s_err));
+            tc_fence_after();
+            if (ok) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                T *out = static_cast<T *>(a.out) + ((size_t)(tok0 + p) * a.Hq + kvh * gq + r % gq) * DH;
+#pragma unroll 1
+                for (int d = 0; d < DH; d += 32) {
+                    uint32_t o[32];
+                    if (n_kt > 0) {
+                        wp_ld32(t_o + d, o);
+                        wp_ld_wait();
+                        wp_pin(o);
+                    }
+                    if (live) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[e] = n_kt > 0 ? pack_pair<T>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
+                        if (l == 0.f) {  // (no key seen: O may be 0 x whatever)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) w[e] = 0u;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4 *>(out + d + 2 * e) = make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]);
+                    }
+                }
+                tc_fence_before();
+            }
+        }
+    }
+    __syncwarp();
+    if (*abortp) {  // a wait ran out: what this CTA has asked for lands within microseconds; do not leave before
+        for (int i = 0; i < 64; ++i) __nanosleep(4000);
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tc_dealloc(tmem, 512u);
+    }
+    if (tid == 0 && s_err) flag(a.status, s_err == DEV_WAIT_TIMEOUT ? RIVER_E_TIMEOUT : RIVER_E_BADARG);
+    if (s_poison && warp >= 4) window_attn_rows_again<T, DH>(a, tok0, n_tok, kvh, gq, seq, pos0);
+}
+
+// (the head dim of 64 asks for as much as 128 does: no CTA that wants tensor memory shares an SM with one that holds all of it)
+inline size_t window_attn_prompt_smem() { return 1024 + 6 * 2 * 128 * 128; }
+
+}  // namespace river
