@@ -66,10 +66,19 @@ __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
     return r;
 }
 
-template <class T, int DH>
-__device__ __noinline__ void window_attn_rows_again(const WindowArgs &a, int tok0, int n_tok, int kvh, int gq, int seq, int pos0) {
-    for (int r = (threadIdx.x >> 5) - 4; r < n_tok * gq; r += 8)
-        window_attn_row<T, DH>(a, tok0 + r / gq, kvh * gq + r % gq, seq, pos0 + r / gq);
+// One lane of the warp.  A warp runs its loop as a whole and only the tcgen05 instructions are one lane's: their operands live in
+// uniform registers, and in a branch that the compiler must take for divergent each of them is carried there anew.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+// bits lo .. hi - 1 of a word, whatever the ends
+__device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
+    const uint32_t below_hi = hi >= 32 ? 0xffffffffu : hi <= 0 ? 0u : (1u << hi) - 1u, below_lo = lo >= 32 ? 0xffffffffu : lo <= 0 ? 0u : (1u << lo) - 1u;
+    return below_hi & ~below_lo;
 }
 
 // The sequence whose tiles hold slot x: sequence s has the slots from q_start[s] / per + s on, enough for its queries.
@@ -94,10 +103,10 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     extern __shared__ uint8_t wp_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(wp_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *const sq = smem, *const sk = sq + 2 * NB * QB, *const sv = sk + 2 * NB * KB;  // [tile] / [stage] [NB][128 rows][128 bytes]
-    __shared__ uint64_t bars[16];
+    __shared__ uint64_t bars[17];
     __shared__ uint32_t s_tmem, s_valid[2];
     __shared__ int s_abort, s_err, s_poison;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int gq = a.Hq / a.c.Hkv, per = kWpRows / gq;  // tokens of a tile
     // heavy tiles, those behind a long history, first
     const int kvh = blockIdx.x % a.c.Hkv, slot = gridDim.x / a.c.Hkv - 1 - blockIdx.x / a.c.Hkv;
@@ -113,11 +122,11 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     const int nq = n_tok > per ? 2 : 1;
 
     const uint32_t b_k = smem_u32(&bars[0]), b_v = smem_u32(&bars[2]), b_kf = smem_u32(&bars[4]), b_vf = smem_u32(&bars[6]), b_s = smem_u32(&bars[8]),
-                   b_p = smem_u32(&bars[10]), b_o = smem_u32(&bars[14]);
+                   b_p = smem_u32(&bars[10]), b_o = smem_u32(&bars[14]), b_q = smem_u32(&bars[16]);
     volatile int *abortp = &s_abort;
     if (tid == 0) {
         s_abort = s_err = s_poison = 0;
-        for (int i = 0; i < 16; ++i) mbar_init(smem_u32(&bars[i]), i >= 10 && i < 14 ? 4 : 1);
+        for (int i = 0; i < 17; ++i) mbar_init(smem_u32(&bars[i]), i == 16 ? 8 : i >= 10 && i < 14 ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -130,21 +139,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     const int low0 = window_low(pos0, a.window), wb0 = low0 >> 4, n_sb = min((min(a.sinks, low0) + 15) >> 4, wb0), shift = 16 * (wb0 - n_sb);
     const int nb = last_pos < 0 ? 0 : n_sb + (last_pos >> 4) - wb0 + 1, n_kt = (nb + 7) / 8;
 
-    // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
-    const uint32_t turn = a.scale_log2 < 0.f ? 0x80008000u : 0u;
-    for (int u = tid; u < nq * kWpRows * (DH / 8); u += kWpThreads) {
-        const int r = u / (DH / 8), c8 = u % (DH / 8), q = r / kWpRows, rr = r % kWpRows, p = q * per + rr / gq, g = rr % gq;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (rr < per * gq && p < n_tok) {
-            x = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + (tok0 + p) * a.q_tok + (kvh * gq + g) * a.q_head + 8 * c8);
-            x.x ^= turn; x.y ^= turn; x.z ^= turn; x.w ^= turn;
-        }
-        *reinterpret_cast<uint4 *>(sq + q * NB * QB + (c8 >> 3) * QB + rr * 128 + (((c8 & 7) ^ (rr & 7)) * 16)) = x;
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = uniform(s_tmem);
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -178,39 +175,70 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 if (!__shfl_sync(0xffffffffu, good, 0)) break;
                 if (page >= 0) tma_load_2d(smem_u32(sv) + (st * NB + half) * KB + blk * 2048, &tmap, 64 * half, row + (a.c.Hkv << a.c.ps_log2), b_v + 8 * st);
             }
-        } else if (warp == 1 && lane == 0) {
+        } else if (warp == 1) {
             const uint64_t dq = tc_smem_desc(smem_u32(sq)), dk = tc_smem_desc(smem_u32(sk)), dv = pt_desc_n(smem_u32(sv), KB);
+            const int n_t = uniform(n_kt), n_q = uniform(nq);
             auto scores = [&](int q, int j) {
-                if (q == 0 && !mbar_wait(b_k + 8 * (j & 1), (j >> 1) & 1, abortp, &s_err)) return false;
+                if (q == 0 && !__all_sync(0xffffffffu, mbar_wait(b_k + 8 * (j & 1), (j >> 1) & 1, abortp, &s_err))) return false;
                 tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < DH / 16; ++k)
-                    tc_mma(tmem + 128u * q, dq + (q * NB + (k >> 2)) * (QB >> 4) + 2 * (k & 3), dk + ((j & 1) * NB + (k >> 2)) * (KB >> 4) + 2 * (k & 3), kIdS, k ? 1u : 0u);
-                tc_commit(b_s + 8 * q);
-                if (q == nq - 1) tc_commit(b_kf + 8 * (j & 1));
+                    for (int k = 0; k < DH / 16; ++k)
+                        tc_mma(tmem + 128u * q, dq + (q * NB + (k >> 2)) * (QB >> 4) + 2 * (k & 3), dk + ((j & 1) * NB + (k >> 2)) * (KB >> 4) + 2 * (k & 3), kIdS, k ? 1u : 0u);
+                    tc_commit(b_s + 8 * q);
+                    if (q == n_q - 1) tc_commit(b_kf + 8 * (j & 1));
+                }
+                __syncwarp();
                 return true;
             };
             auto values = [&](int q, int j) {
-                if (q == 0 && !mbar_wait(b_v + 8 * (j & 1), (j >> 1) & 1, abortp, &s_err)) return false;
+                if (q == 0 && !__all_sync(0xffffffffu, mbar_wait(b_v + 8 * (j & 1), (j >> 1) & 1, abortp, &s_err))) return false;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {  // half of the keys
-                    if (!mbar_wait(b_p + 8 * (2 * q + h), j & 1, abortp, &s_err)) return false;
+                    if (!__all_sync(0xffffffffu, mbar_wait(b_p + 8 * (2 * q + h), j & 1, abortp, &s_err))) return false;
                     tc_fence_after();
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)  // 16 keys: 8 columns of P, 2048 bytes of V
-                        tc_mma_ts(tmem + kO + (uint32_t)DH * q, tmem + 128u * q + 32 * h + 8 * k, dv + (j & 1) * (NB * KB >> 4) + (4 * h + k) * (2048 >> 4), kIdO, (j | h | k) ? 1u : 0u);
+                        for (int k = 0; k < 4; ++k)  // 16 keys: 8 columns of P, 2048 bytes of V
+                            tc_mma_ts(tmem + kO + (uint32_t)DH * q, tmem + 128u * q + 32 * h + 8 * k, dv + (j & 1) * (NB * KB >> 4) + (4 * h + k) * (2048 >> 4), kIdO, (j | h | k) ? 1u : 0u);
+                        if (h == 1) {
+                            if (q == n_q - 1) tc_commit(b_vf + 8 * (j & 1));
+                            if (j == n_t - 1) tc_commit(b_o + 8 * q);
+                        }
+                    }
+                    __syncwarp();
                 }
-                if (q == nq - 1) tc_commit(b_vf + 8 * (j & 1));
-                if (j == n_kt - 1) tc_commit(b_o + 8 * q);
                 return true;
             };
-            bool ok = n_kt > 0;
-            for (int q = 0; q < nq && ok; ++q) ok = scores(q, 0);
-            for (int j = 0; j < n_kt && ok; ++j)
-                for (int q = 0; q < nq && ok; ++q) ok = values(q, j) && (j + 1 == n_kt || scores(q, j + 1));
+            bool ok = n_t > 0 && __all_sync(0xffffffffu, mbar_wait(b_q, 0, abortp, &s_err));
+            for (int q = 0; q < n_q && ok; ++q) ok = scores(q, 0);
+            for (int j = 0; j < n_t && ok; ++j)
+                for (int q = 0; q < n_q && ok; ++q) ok = values(q, j) && (j + 1 == n_t || scores(q, j + 1));
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        {  // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
+            const uint32_t turn = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+            constexpr int C8 = DH / 8, U = C8;  // 16-byte chunks of a row; all of a thread's are under way together
+            const int u0 = tid - 128, n_u = nq * kWpRows * C8;
+            uint4 x[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int u = u0 + 256 * i, rr = u / C8 % kWpRows, p = u / (C8 * kWpRows) * per + rr / gq, g = rr % gq;
+                x[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (u < n_u && rr < per * gq && p < n_tok)
+                    x[i] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + (tok0 + p) * a.q_tok + (kvh * gq + g) * a.q_head + 8 * (u % C8));
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int u = u0 + 256 * i, c8 = u % C8, rr = u / C8 % kWpRows;
+                x[i].x ^= turn; x[i].y ^= turn; x[i].z ^= turn; x[i].w ^= turn;
+                if (u < n_u) *reinterpret_cast<uint4 *>(sq + u / (C8 * kWpRows) * NB * QB + (c8 >> 3) * QB + rr * 128 + (((c8 & 7) ^ (rr & 7)) * 16)) = x[i];
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_q);
+        }
         const int q = (warp - 4) >> 2, r = 32 * (warp & 3) + lane, p = q * per + r / gq;
         const bool live = r < per * gq && p < n_tok;
         if (q < nq) {
@@ -234,23 +262,21 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 part = part || valid != 0xffu;
                 if (part && q == 0) {  // thread = V row: those that nobody sees become zero, the others are looked through
                     const int cc = c0 + r;
-                    const bool any = (valid >> (r >> 4) & 1u) && (cc < any_sink || (cc >= any_lo && cc < any_hi));
                     uint8_t *row = sv + st * NB * KB + r * 128;
-                    bool odd = false;
+                    if ((valid >> (r >> 4) & 1u) && (cc < any_sink || (cc >= any_lo && cc < any_hi))) {
+                        // an exponent of ones (what is no number) and one more carries into the sign's place
+                        constexpr uint32_t E = std::is_same<T, __nv_bfloat16>::value ? 0x7f807f80u : 0x7c007c00u, ONE = E & ~(E << 1);
+                        uint32_t odd = 0u;
 #pragma unroll
-                    for (int i = 0; i < DH / 8; ++i) {
-                        uint4 *x = reinterpret_cast<uint4 *>(row + (i >> 3) * KB + (((i & 7) ^ (r & 7)) * 16));
-                        if (!any) {
-                            *x = make_uint4(0u, 0u, 0u, 0u);
-                        } else {
-                            constexpr uint32_t E = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;  // the exponent of what is no number
-                            const uint4 y = *x;
-                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) odd = odd || (w[e] & E) == E || (w[e] >> 16 & E) == E;
+                        for (int i = 0; i < DH / 8; ++i) {
+                            const uint4 y = *reinterpret_cast<const uint4 *>(row + (i >> 3) * KB + (((i & 7) ^ (r & 7)) * 16));
+                            odd |= ((y.x & E) + ONE) | ((y.y & E) + ONE) | ((y.z & E) + ONE) | ((y.w & E) + ONE);
                         }
+                        if (odd & 0x80008000u) s_poison = 1;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<uint4 *>(row + (i >> 3) * KB + (((i & 7) ^ (r & 7)) * 16)) = make_uint4(0u, 0u, 0u, 0u);
                     }
-                    if (odd) s_poison = 1;
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 ok = __all_sync(0xffffffffu, mbar_wait(b_s + 8 * q, j & 1, abortp, &s_err));
@@ -264,12 +290,13 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 for (int i = 0; i < 4; ++i) wp_pin(s[i]);
                 if (part) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i) {
+                        const int cc = c0 + 32 * i;
+                        const uint32_t there = (valid >> (2 * i) & 1u ? 0xffffu : 0u) | (valid >> (2 * i + 1) & 1u ? 0xffff0000u : 0u);
+                        const uint32_t see = (bits_between(0, c_sink - cc) | bits_between(c_lo - cc, c_hi - cc)) & there;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int cc = c0 + 32 * i + e;
-                            if (!((cc < c_sink || (cc >= c_lo && cc < c_hi)) && (valid >> (2 * i + (e >> 4)) & 1u))) s[i][e] = 0xff800000u;  // -inf
-                        }
+                        for (int e = 0; e < 32; ++e) s[i][e] = see >> e & 1u ? s[i][e] : 0xff800000u;  // -inf
+                    }
                 }
                 float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
@@ -358,7 +385,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
         tc_dealloc(tmem, 512u);
     }
     if (tid == 0 && s_err) flag(a.status, s_err == DEV_WAIT_TIMEOUT ? RIVER_E_TIMEOUT : RIVER_E_BADARG);
-    if (s_poison && warp >= 4) window_attn_rows_again<T, DH>(a, tok0, n_tok, kvh, gq, seq, pos0);
+    if (s_poison && warp >= 4)
+#pragma unroll 1
+        for (int r = warp - 4; r < n_tok * gq; r += 8) window_attn_row<T, DH>(a, tok0 + r / gq, kvh * gq + r % gq, seq, pos0 + r / gq);
 }
 
 // (the head dim of 64 asks for as much as 128 does: no CTA that wants tensor memory shares an SM with one that holds all of it)
