@@ -5,7 +5,7 @@
 // blocks = 128 keys at a time.  Both tiles use the same K and V:
 //   S [128 x 128] = Q K^T     Q and K in shared memory, S in tensor memory
 //   O [128 x DH] += P V       P (rounded to the inputs' type) in tensor memory over the place of S, V as it lies in the cache
-//   warp 0        TMA: K and V pages, one 16 x 64 box per lane, two stages each
+//   warp 0        TMA: K and V pages, one 16 x 64 box per lane, five places
 //   warp 1        tensor memory; one lane issues the MMAs: P V of a tile, S of its next keys, then the other tile's, so that the softmax of
 //                 one tile runs under the MMAs of the other
 //   warps 4..11   softmax, four per tile: thread = query row = TMEM lane; online, base 2, fp32; all 128 scores of a row in registers; O is
@@ -24,6 +24,7 @@
 namespace river {
 
 constexpr int kWpRows = 128, kWpKeys = 128, kWpThreads = 384;
+constexpr int kWpSlots = 5;     // places of K and V tiles, K and V of a tile one after the other
 constexpr float kWpLazy = 8.f;  // growth of a row's maximum (log2) that O waits for before it is rescaled
 
 struct PromptArgs {
@@ -91,6 +92,66 @@ __device__ __forceinline__ int prompt_seq(const int32_t *q_start, int n_seqs, in
     return lo;
 }
 
+__device__ __forceinline__ uint64_t f2_sub(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// max of three that hands on what is no number
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x of two values by arithmetic: x = n + f with n the nearest whole number (the low bits of x + 1.5 x 2^23), 2^f by its minimax polynomial
+// on [-1/2, 1/2] (found by exchange; relative error 7.5e-5 in degree 3, 2.6e-6 in degree 4: below a twentieth of the rounding of P in
+// either type), n added to the exponent.  x below -126 gives 2^-126.
+template <class T>
+__device__ __forceinline__ uint64_t f2_ex2(uint64_t x) {
+    float x0, x1, t0, t1, p0, p1;
+    f2_unpack(x, x0, x1);
+    x = f2_pack(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+    const uint64_t t = f2_add(x, f2_pack(12582912.f, 12582912.f)), f = f2_sub(x, f2_sub(t, f2_pack(12582912.f, 12582912.f)));
+    uint64_t p;
+    auto two = [](float a) { return f2_pack(a, a); };
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        p = f2_fma(f, two(0.0551716685295105f), two(0.2426111251115799f));
+        p = f2_fma(f, p, two(0.6932609677314758f));
+        p = f2_fma(f, p, two(0.9999280571937561f));
+    } else {
+        p = f2_fma(f, two(0.009570102207362652f), two(0.05591785907745361f));
+        p = f2_fma(f, p, two(0.240247443318367f));
+        p = f2_fma(f, p, two(0.6931217908859253f));
+        p = f2_fma(f, p, two(0.9999992847442627f));
+    }
+    f2_unpack(t, t0, t1);
+    f2_unpack(p, p0, p1);
+    return f2_pack(__uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23)), __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23)));
+}
+// Probabilities of 64 keys: w = 2^(s c - m) in pairs, their sum on top of `sum`.  Every fourth pair by arithmetic: the special-function units
+// (4 lanes a cycle and quarter of an SM) would else take as long as the MMAs.
+constexpr int kWpByHand = 99;
+template <class T>
+__device__ __forceinline__ void wp_exps(const uint32_t (&a)[32], const uint32_t (&b)[32], uint64_t c2, uint64_t m2, uint64_t &sum, uint32_t (&w)[32]) {
+    uint64_t part[2] = {sum, 0ull};
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+        const uint32_t *s = e < 16 ? a + 2 * e : b + 2 * e - 32;
+        const uint64_t x = f2_fma(f2_pack(__uint_as_float(s[0]), __uint_as_float(s[1])), c2, m2);
+        float p0, p1;
+        if (e % kWpByHand == kWpByHand - 1) {
+            f2_unpack(f2_ex2<T>(x), p0, p1);
+        } else {
+            f2_unpack(x, p0, p1);
+            p0 = ex2(p0);
+            p1 = ex2(p1);
+        }
+        part[e & 1] = f2_add(part[e & 1], f2_pack(p0, p1));
+        w[e] = pack_pair<T>(p0, p1);
+    }
+    sum = f2_add(part[0], part[1]);
+}
+
 template <class T, int DH>
 __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const __grid_constant__ CUtensorMap tmap, const PromptArgs pa) {
     const WindowArgs &a = pa.w;
@@ -102,9 +163,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     constexpr uint32_t kIdO = (kIdS & ~(0x3Fu << 17)) | ((uint32_t)(DH >> 3) << 17) | (1u << 16);  // (B of the second product: N-major)
     extern __shared__ uint8_t wp_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(wp_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t *const sq = smem, *const sk = sq + 2 * NB * QB, *const sv = sk + 2 * NB * KB;  // [tile] / [stage] [NB][128 rows][128 bytes]
-    __shared__ uint64_t bars[17];
-    __shared__ uint32_t s_tmem, s_valid[2];
+    uint8_t *const sq = smem, *const skv = sq + 2 * NB * QB;  // [tile] / [slot] [NB][128 rows][128 bytes]
+    __shared__ uint64_t bars[2 * kWpSlots + 13];  // slots: landed, free; per tile: S done (1 each), P written (2 each), O done; Q there; blocks known (4)
+    __shared__ uint32_t s_tmem, s_valid[4];
     __shared__ int s_abort, s_err, s_poison;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int gq = a.Hq / a.c.Hkv, per = kWpRows / gq;  // tokens of a tile
@@ -121,12 +182,18 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     const int n_tok = min(n - at, per * pa.tiles), tok0 = first + at, pos0 = a.c.lens[seq] - n + at, last_pos = pos0 + n_tok - 1;
     const int nq = n_tok > per ? 2 : 1;
 
-    const uint32_t b_k = smem_u32(&bars[0]), b_v = smem_u32(&bars[2]), b_kf = smem_u32(&bars[4]), b_vf = smem_u32(&bars[6]), b_s = smem_u32(&bars[8]),
-                   b_p = smem_u32(&bars[10]), b_o = smem_u32(&bars[14]), b_q = smem_u32(&bars[16]);
+    const uint32_t b_full = smem_u32(&bars[0]), b_free = smem_u32(&bars[kWpSlots]), b_s = smem_u32(&bars[2 * kWpSlots]), b_p = b_s + 16, b_o = b_p + 32,
+                   b_q = b_o + 16, b_i = b_q + 8;
+    // K of tile j: fill 2 j of the slots, V: fill 2 j + 1
+    auto slot_of = [](int fill) { return (uint32_t)fill % kWpSlots; };
+    auto turn_of = [](int fill) { return ((uint32_t)fill / kWpSlots) & 1u; };
     volatile int *abortp = &s_abort;
     if (tid == 0) {
         s_abort = s_err = s_poison = 0;
-        for (int i = 0; i < 17; ++i) mbar_init(smem_u32(&bars[i]), i == 16 ? 8 : i >= 10 && i < 14 ? 4 : 1);
+        for (int i = 0; i < 2 * kWpSlots + 13; ++i) {
+            const int k = i - 2 * kWpSlots;
+            mbar_init(smem_u32(&bars[i]), k >= 2 && k < 6 ? 4 : k == 8 ? 8 : 1);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -148,51 +215,61 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
         if (warp == 0) {
             const int32_t *tbl = a.c.table + (size_t)seq * a.c.max_pages;
             const int blk = lane / NB, half = lane % NB, bpp = a.c.ps_log2 - 4;
+            auto block_of = [&](int j) { const int u = 8 * j + blk; return u < n_sb ? u : wb0 + u - n_sb; };
+            auto page_of = [&](int j) {
+                const int col = block_of(j) >> bpp;
+                return blk < 8 && 8 * j + blk < nb && col < a.c.max_pages ? tbl[col] : -1;
+            };
+            int ahead = page_of(0);
             for (int j = 0; j < n_kt; ++j) {
-                const int st = j & 1, u = 8 * j + blk, b = u < n_sb ? u : wb0 + u - n_sb;
-                const bool on = blk < 8 && u < nb;
-                int page = -1;
-                if (on) {
-                    const int col = b >> bpp;
-                    page = col < a.c.max_pages ? tbl[col] : -1;
-                    if (page < 0 || page >= a.c.n_pages) { page = -1; s_err = DEV_BAD_PAGE; }
+                int page = ahead;
+                ahead = page_of(j + 1);  // (under way while this tile waits for its place)
+                if (page < 0 || page >= a.c.n_pages) {
+                    if (blk < 8 && 8 * j + blk < nb) s_err = DEV_BAD_PAGE;
+                    page = -1;
                 }
                 const unsigned got = __ballot_sync(0xffffffffu, page >= 0);
                 const uint32_t bytes = (uint32_t)__popc(got) * 16 * 128;
-                const int row = page < 0 ? 0 : ((page * 2 * a.c.Hkv + kvh) << a.c.ps_log2) + ((b << 4) & ((1 << a.c.ps_log2) - 1));
-                int good = 1;
-                if (lane == 0 && j >= 2) good = mbar_wait(b_kf + 8 * st, ((j >> 1) - 1) & 1, abortp, &s_err) ? 1 : 0;
-                if (lane == 0 && good) mbar_expect_tx(b_k + 8 * st, bytes);
-                if (!__shfl_sync(0xffffffffu, good, 0)) break;
-                if (page >= 0) tma_load_2d(smem_u32(sk) + (st * NB + half) * KB + blk * 2048, &tmap, 64 * half, row, b_k + 8 * st);
-                if (lane == 0 && j >= 2) good = mbar_wait(b_vf + 8 * st, ((j >> 1) - 1) & 1, abortp, &s_err) ? 1 : 0;
-                if (lane == 0 && good) {
-                    uint32_t valid = 0;  // blocks that are there, for the softmax
+                const int row = page < 0 ? 0 : ((page * 2 * a.c.Hkv + kvh) << a.c.ps_log2) + ((block_of(j) << 4) & ((1 << a.c.ps_log2) - 1));
+                if (lane == 0) {
+                    uint32_t valid = 0;  // blocks that are there, for the softmax (four places: this warp is never four tiles ahead of it)
                     for (int i = 0; i < 8; ++i) valid |= ((got >> (i * NB)) & 1u) << i;
-                    s_valid[st] = valid;
-                    mbar_expect_tx(b_v + 8 * st, bytes);
+                    s_valid[j & 3] = valid;
+                    mbar_arrive(b_i + 8 * (j & 3));
                 }
-                if (!__shfl_sync(0xffffffffu, good, 0)) break;
-                if (page >= 0) tma_load_2d(smem_u32(sv) + (st * NB + half) * KB + blk * 2048, &tmap, 64 * half, row + (a.c.Hkv << a.c.ps_log2), b_v + 8 * st);
+                bool good = true;
+#pragma unroll
+                for (int v = 0; v < 2 && good; ++v) {  // K, V
+                    const int fill = 2 * j + v;
+                    const uint32_t slot = slot_of(fill);
+                    if (fill >= kWpSlots) good = __all_sync(0xffffffffu, mbar_wait(b_free + 8 * slot, turn_of(fill) ^ 1u, abortp, &s_err));
+                    if (!good) break;
+                    if (lane == 0) mbar_expect_tx(b_full + 8 * slot, bytes);
+                    __syncwarp();
+                    if (page >= 0) tma_load_2d(smem_u32(skv) + (slot * NB + half) * KB + blk * 2048, &tmap, 64 * half, row + v * (a.c.Hkv << a.c.ps_log2), b_full + 8 * slot);
+                }
+                if (!good) break;
             }
         } else if (warp == 1) {
-            const uint64_t dq = tc_smem_desc(smem_u32(sq)), dk = tc_smem_desc(smem_u32(sk)), dv = pt_desc_n(smem_u32(sv), KB);
+            const uint64_t dq = tc_smem_desc(smem_u32(sq)), dk = tc_smem_desc(smem_u32(skv)), dv = pt_desc_n(smem_u32(skv), KB);
             const int n_t = uniform(n_kt), n_q = uniform(nq);
             auto scores = [&](int q, int j) {
-                if (q == 0 && !__all_sync(0xffffffffu, mbar_wait(b_k + 8 * (j & 1), (j >> 1) & 1, abortp, &s_err))) return false;
+                const uint32_t slot = slot_of(2 * j);
+                if (q == 0 && !__all_sync(0xffffffffu, mbar_wait(b_full + 8 * slot, turn_of(2 * j), abortp, &s_err))) return false;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < DH / 16; ++k)
-                        tc_mma(tmem + 128u * q, dq + (q * NB + (k >> 2)) * (QB >> 4) + 2 * (k & 3), dk + ((j & 1) * NB + (k >> 2)) * (KB >> 4) + 2 * (k & 3), kIdS, k ? 1u : 0u);
+                        tc_mma(tmem + 128u * q, dq + (q * NB + (k >> 2)) * (QB >> 4) + 2 * (k & 3), dk + (slot * NB + (k >> 2)) * (KB >> 4) + 2 * (k & 3), kIdS, k ? 1u : 0u);
                     tc_commit(b_s + 8 * q);
-                    if (q == n_q - 1) tc_commit(b_kf + 8 * (j & 1));
+                    if (q == n_q - 1) tc_commit(b_free + 8 * slot);
                 }
                 __syncwarp();
                 return true;
             };
             auto values = [&](int q, int j) {
-                if (q == 0 && !__all_sync(0xffffffffu, mbar_wait(b_v + 8 * (j & 1), (j >> 1) & 1, abortp, &s_err))) return false;
+                const uint32_t slot = slot_of(2 * j + 1);
+                if (q == 0 && !__all_sync(0xffffffffu, mbar_wait(b_full + 8 * slot, turn_of(2 * j + 1), abortp, &s_err))) return false;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {  // half of the keys
                     if (!__all_sync(0xffffffffu, mbar_wait(b_p + 8 * (2 * q + h), j & 1, abortp, &s_err))) return false;
@@ -200,9 +277,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)  // 16 keys: 8 columns of P, 2048 bytes of V
-                            tc_mma_ts(tmem + kO + (uint32_t)DH * q, tmem + 128u * q + 32 * h + 8 * k, dv + (j & 1) * (NB * KB >> 4) + (4 * h + k) * (2048 >> 4), kIdO, (j | h | k) ? 1u : 0u);
+                            tc_mma_ts(tmem + kO + (uint32_t)DH * q, tmem + 128u * q + 32 * h + 8 * k, dv + slot * (NB * KB >> 4) + (4 * h + k) * (2048 >> 4), kIdO, (j | h | k) ? 1u : 0u);
                         if (h == 1) {
-                            if (q == n_q - 1) tc_commit(b_vf + 8 * (j & 1));
+                            if (q == n_q - 1) tc_commit(b_free + 8 * slot);
                             if (j == n_t - 1) tc_commit(b_o + 8 * q);
                         }
                     }
@@ -252,17 +329,19 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             float m = -CUDART_INF_F, l = 0.f;
             bool ok = true;
             for (int j = 0; j < n_kt; ++j) {
-                const int c0 = 128 * j, st = j & 1;
+                const int c0 = 128 * j;
                 bool part = !(c0 >= all_lo && c0 + 128 <= all_hi) && !(c0 + 128 <= all_sink);
-                uint32_t valid = 0xffu;
-                // (which blocks are there is written before the barrier of V; K's tells of nothing missing only together with it)
-                ok = __all_sync(0xffffffffu, mbar_wait(b_v + 8 * st, (j >> 1) & 1, abortp, &s_err));
+                ok = __all_sync(0xffffffffu, mbar_wait(b_i + 8 * (j & 3), (j >> 2) & 1, abortp, &s_err));
                 if (!ok) break;
-                valid = s_valid[st];
+                const uint32_t valid = s_valid[j & 3];
                 part = part || valid != 0xffu;
+                if (part && q == 0) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(b_full + 8 * slot_of(2 * j + 1), turn_of(2 * j + 1), abortp, &s_err));
+                    if (!ok) break;
+                }
                 if (part && q == 0) {  // thread = V row: those that nobody sees become zero, the others are looked through
                     const int cc = c0 + r;
-                    uint8_t *row = sv + st * NB * KB + r * 128;
+                    uint8_t *row = skv + slot_of(2 * j + 1) * NB * KB + r * 128;
                     if ((valid >> (r >> 4) & 1u) && (cc < any_sink || (cc >= any_lo && cc < any_hi))) {
                         // an exponent of ones (what is no number) and one more carries into the sign's place
                         constexpr uint32_t E = std::is_same<T, __nv_bfloat16>::value ? 0x7f807f80u : 0x7c007c00u, ONE = E & ~(E << 1);
@@ -298,16 +377,25 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                         for (int e = 0; e < 32; ++e) s[i][e] = see >> e & 1u ? s[i][e] : 0xff800000u;  // -inf
                     }
                 }
-                float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+                // The first half is made with the maximum as it stood; only where the tile's own maximum, found meanwhile, has grown too
+                // far past it (a first tile, a rare later one) it is made again.
+                uint64_t sum;
+                uint32_t w[32];
+                const uint64_t c2 = f2_pack(c, c);
+                while (true) {
+                    sum = 0ull;
+                    const float base = m == -CUDART_INF_F ? 0.f : m;
+                    wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), sum, w);
+                    float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e & 3] = fmaxf(x[e & 3], __uint_as_float(s[i][e]));
-                const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * c;
-                const bool grow = mx > m + kWpLazy || (m == -CUDART_INF_F && mx > m);
-                if (__any_sync(0xffffffffu, grow)) {
+                        for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
+                    const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
+                    const bool grow = !(mx <= m + kWpLazy) && !(m != m);  // (a maximum that is no number stays)
+                    if (!__any_sync(0xffffffffu, grow)) break;
                     const float corr = grow ? ex2(m - mx) : 1.f;
-                    if (grow) m = mx;
+                    if (grow) m = mx < CUDART_INF_F ? mx : CUDART_NAN_F;  // (inf - inf, as the formula has it)
                     l *= corr;
                     if (j > 0) {  // (the MMAs that wrote O are complete: S of these keys was issued behind them)
 #pragma unroll 1
@@ -322,26 +410,20 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                         }
                     }
                 }
-                const float base = m == -CUDART_INF_F ? 0.f : m;
-                const uint64_t c2 = f2_pack(c, c), m2 = f2_pack(-base, -base);
-                uint64_t sum = 0ull;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float p0, p1;
-                        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[2 * h + (e >> 4)][2 * (e & 15)]), __uint_as_float(s[2 * h + (e >> 4)][2 * (e & 15) + 1])), c2, m2), p0, p1);
-                        p0 = ex2(p0);
-                        p1 = ex2(p1);
-                        sum = f2_add(sum, f2_pack(p0, p1));
-                        w[e] = pack_pair<T>(p0, p1);
-                    }
+                auto hand_over = [&](int h) {
                     tc_st32(t_s + 32 * h, w);
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(b_p + 8 * (2 * q + h));
+                };
+                hand_over(0);
+                wp_pin(s[2]);  // (no probability of the second half before the first is handed over)
+                wp_pin(s[3]);
+                {
+                    const float base = m == -CUDART_INF_F ? 0.f : m;
+                    wp_exps<T>(s[2], s[3], c2, f2_pack(-base, -base), sum, w);
                 }
+                hand_over(1);
                 float l0, l1;
                 f2_unpack(sum, l0, l1);
                 l += l0 + l1;
@@ -349,7 +431,8 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             if (ok && n_kt > 0) ok = __all_sync(0xffffffffu, mbar_wait(b_o + 8 * q, 0, abortp, &s_err));
             tc_fence_after();
             if (ok) {
-                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const bool none = m == -CUDART_INF_F;  // (no key seen: O may be 0 x whatever)
+                const float inv = none ? 0.f : 1.f / l;
                 T *out = static_cast<T *>(a.out) + ((size_t)(tok0 + p) * a.Hq + kvh * gq + r % gq) * DH;
 #pragma unroll 1
                 for (int d = 0; d < DH; d += 32) {
@@ -363,7 +446,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                         uint32_t w[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) w[e] = n_kt > 0 ? pack_pair<T>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
-                        if (l == 0.f) {  // (no key seen: O may be 0 x whatever)
+                        if (none) {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) w[e] = 0u;
                         }
@@ -391,6 +474,6 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
 }
 
 // (the head dim of 64 asks for as much as 128 does: no CTA that wants tensor memory shares an SM with one that holds all of it)
-inline size_t window_attn_prompt_smem() { return 1024 + 6 * 2 * 128 * 128; }
+inline size_t window_attn_prompt_smem() { return 1024 + (2 + kWpSlots) * 2 * 128 * 128; }
 
 }  // namespace river
