@@ -5,7 +5,7 @@
 // blocks = 128 keys at a time.  Both tiles use the same K and V:
 //   S [128 x 128] = Q K^T     Q and K in shared memory, S in tensor memory
 //   O [128 x DH] += P V       P (rounded to the inputs' type) in tensor memory over the place of S, V as it lies in the cache
-//   warp 0        TMA: K and V pages, one 16 x 64 box per lane, five places
+//   warp 0        TMA: K and V pages, one 16 x 64 box per lane, three places for K, two for V
 //   warp 1        tensor memory; one lane issues the MMAs: P V of a tile, S of its next keys, then the other tile's, so that the softmax of
 //                 one tile runs under the MMAs of the other
 //   warps 4..11   softmax, four per tile: thread = query row = TMEM lane; online, base 2, fp32; all 128 scores of a row in registers; O is
@@ -24,7 +24,6 @@
 namespace river {
 
 constexpr int kWpRows = 128, kWpKeys = 128, kWpThreads = 384;
-constexpr int kWpSlots = 5;     // places of K and V tiles, K and V of a tile one after the other
 constexpr float kWpLazy = 8.f;  // growth of a row's maximum (log2) that O waits for before it is rescaled
 
 struct PromptArgs {
@@ -74,6 +73,16 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
     return r != 0;
 }
+// Bounded wait.  Where it runs out the kernel goes on with whatever is there, every later wait ends at once, and no result is stored:
+// nobody is left standing at a barrier.
+__device__ __forceinline__ void wp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
+    for (uint32_t it = 0; it < kWaitLimit; ++it) {
+        if (mbar_try_wait(bar, parity & 1u)) return;
+        if (*abort_flag) return;
+    }
+    *abort_flag = 1;
+    atomicExch(err, DEV_WAIT_TIMEOUT);
+}
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // bits lo .. hi - 1 of a word, whatever the ends
@@ -106,6 +115,11 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
 // 2^x of two values by arithmetic: x = n + f with n the nearest whole number (the low bits of x + 1.5 x 2^23), 2^f by its minimax polynomial
 // on [-1/2, 1/2] (found by exchange; relative error 7.5e-5 in degree 3, 2.6e-6 in degree 4: below a twentieth of the rounding of P in
 // either type), n added to the exponent.  x below -126 gives 2^-126.
+__device__ __forceinline__ float ex2_here(float x) {  // (volatile: stays where it is written)
+    float y;
+    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 template <class T>
 __device__ __forceinline__ uint64_t f2_ex2(uint64_t x) {
     float x0, x1, t0, t1, p0, p1;
@@ -131,25 +145,44 @@ __device__ __forceinline__ uint64_t f2_ex2(uint64_t x) {
 // Probabilities of 64 keys: w = 2^(s c - m) in pairs, their sum on top of `sum`.  Every fourth pair by arithmetic: the special-function units
 // (4 lanes a cycle and quarter of an SM) would else take as long as the MMAs.
 constexpr int kWpByHand = 99;
-template <class T>
-__device__ __forceinline__ void wp_exps(const uint32_t (&a)[32], const uint32_t (&b)[32], uint64_t c2, uint64_t m2, uint64_t &sum, uint32_t (&w)[32]) {
-    uint64_t part[2] = {sum, 0ull};
+// The steps of neighbouring pairs are interleaved by hand, and with them (MAX) the maximum of all 128 scores: left in program order they
+// queue for one unit after the other.
+template <class T, bool MAX>
+__device__ __forceinline__ void wp_exps(const uint32_t (&s)[4][32], int half, uint64_t c2, uint64_t m2, uint64_t &sum, uint32_t (&w)[32], float &mx) {
+    uint64_t part[2] = {sum, 0ull}, x[34];
+    float p[34][2], top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
-        const uint32_t *s = e < 16 ? a + 2 * e : b + 2 * e - 32;
-        const uint64_t x = f2_fma(f2_pack(__uint_as_float(s[0]), __uint_as_float(s[1])), c2, m2);
-        float p0, p1;
-        if (e % kWpByHand == kWpByHand - 1) {
-            f2_unpack(f2_ex2<T>(x), p0, p1);
-        } else {
-            f2_unpack(x, p0, p1);
-            p0 = ex2(p0);
-            p1 = ex2(p1);
+    for (int e = 0; e < 34; ++e) {
+        if (e < 32) {
+            const uint32_t *v = s[2 * half + (e >> 4)] + 2 * (e & 15);
+            x[e] = f2_fma(f2_pack(__uint_as_float(v[0]), __uint_as_float(v[1])), c2, m2);
         }
-        part[e & 1] = f2_add(part[e & 1], f2_pack(p0, p1));
-        w[e] = pack_pair<T>(p0, p1);
+        if (e >= 1 && e < 33) {
+            const int k = e - 1;
+            if (k % kWpByHand == kWpByHand - 1) {
+                f2_unpack(f2_ex2<T>(x[k]), p[k][0], p[k][1]);
+            } else {
+                f2_unpack(x[k], p[k][0], p[k][1]);
+                p[k][0] = ex2_here(p[k][0]);
+            }
+        }
+        if (MAX && e < 32) {
+            const uint32_t *v = s[e >> 3] + 4 * (e & 7);
+            top[e & 3] = max3_nan(top[e & 3], __uint_as_float(v[0]), __uint_as_float(v[1]));
+            top[(e + 2) & 3] = max3_nan(top[(e + 2) & 3], __uint_as_float(v[2]), __uint_as_float(v[3]));
+        }
+        if (e >= 1 && e < 33) {
+            const int k = e - 1;
+            if (k % kWpByHand != kWpByHand - 1) p[k][1] = ex2_here(p[k][1]);
+        }
+        if (e >= 2) {
+            const int k = e - 2;
+            part[k & 1] = f2_add(part[k & 1], f2_pack(p[k][0], p[k][1]));
+            w[k] = pack_pair<T>(p[k][0], p[k][1]);
+        }
     }
     sum = f2_add(part[0], part[1]);
+    if (MAX) mx = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]);
 }
 
 template <class T, int DH>
@@ -163,10 +196,12 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     constexpr uint32_t kIdO = (kIdS & ~(0x3Fu << 17)) | ((uint32_t)(DH >> 3) << 17) | (1u << 16);  // (B of the second product: N-major)
     extern __shared__ uint8_t wp_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(wp_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t *const sq = smem, *const skv = sq + 2 * NB * QB;  // [tile] / [slot] [NB][128 rows][128 bytes]
-    __shared__ uint64_t bars[2 * kWpSlots + 13];  // slots: landed, free; per tile: S done (1 each), P written (2 each), O done; Q there; blocks known (4)
-    __shared__ uint32_t s_tmem, s_valid[4];
-    __shared__ int s_abort, s_err, s_poison;
+    uint8_t *const sq = smem, *const sv = sq + 2 * NB * QB, *const sk = sv + 2 * NB * KB;  // [tile], [2 places of V], [3 of K] [NB][128 rows][128 bytes]
+    // K of the first tile there; V of tile j and K of tile j + 1 there (4, in turn); V of tile j and K before free (2); per query tile:
+    // S done, P written (2), O done; Q there
+    __shared__ uint64_t bars[16];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort, s_err, s_poison, s_missing;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int gq = a.Hq / a.c.Hkv, per = kWpRows / gq;  // tokens of a tile
     // heavy tiles, those behind a long history, first
@@ -182,18 +217,11 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     const int n_tok = min(n - at, per * pa.tiles), tok0 = first + at, pos0 = a.c.lens[seq] - n + at, last_pos = pos0 + n_tok - 1;
     const int nq = n_tok > per ? 2 : 1;
 
-    const uint32_t b_full = smem_u32(&bars[0]), b_free = smem_u32(&bars[kWpSlots]), b_s = smem_u32(&bars[2 * kWpSlots]), b_p = b_s + 16, b_o = b_p + 32,
-                   b_q = b_o + 16, b_i = b_q + 8;
-    // K of tile j: fill 2 j of the slots, V: fill 2 j + 1
-    auto slot_of = [](int fill) { return (uint32_t)fill % kWpSlots; };
-    auto turn_of = [](int fill) { return ((uint32_t)fill / kWpSlots) & 1u; };
+    const uint32_t b_first = smem_u32(&bars[0]), b_full = b_first + 8, b_free = b_full + 32, b_s = b_free + 16, b_p = b_s + 16, b_o = b_p + 32, b_q = b_o + 16;
     volatile int *abortp = &s_abort;
     if (tid == 0) {
-        s_abort = s_err = s_poison = 0;
-        for (int i = 0; i < 2 * kWpSlots + 13; ++i) {
-            const int k = i - 2 * kWpSlots;
-            mbar_init(smem_u32(&bars[i]), k >= 2 && k < 6 ? 4 : k == 8 ? 8 : 1);
-        }
+        s_abort = s_err = s_poison = s_missing = 0;
+        for (int i = 0; i < 16; ++i) mbar_init(smem_u32(&bars[i]), i >= 9 && i < 13 ? 4 : i == 15 ? 8 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -206,6 +234,13 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     const int low0 = window_low(pos0, a.window), wb0 = low0 >> 4, n_sb = min((min(a.sinks, low0) + 15) >> 4, wb0), shift = 16 * (wb0 - n_sb);
     const int nb = last_pos < 0 ? 0 : n_sb + (last_pos >> 4) - wb0 + 1, n_kt = (nb + 7) / 8;
 
+    const int32_t *const tbl = a.c.table + (size_t)seq * a.c.max_pages;
+    auto block_of = [&](int u) { return u < n_sb ? u : wb0 + u - n_sb; };
+    auto page_of = [&](int u) {  // of the u-th block; -1: none
+        const int col = block_of(u) >> (a.c.ps_log2 - 4), page = u < nb && col < a.c.max_pages ? tbl[col] : -1;
+        return page < a.c.n_pages ? max(page, -1) : -1;
+    };
+
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = uniform(s_tmem);
@@ -213,111 +248,105 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
-            const int32_t *tbl = a.c.table + (size_t)seq * a.c.max_pages;
-            const int blk = lane / NB, half = lane % NB, bpp = a.c.ps_log2 - 4;
-            auto block_of = [&](int j) { const int u = 8 * j + blk; return u < n_sb ? u : wb0 + u - n_sb; };
-            auto page_of = [&](int j) {
-                const int col = block_of(j) >> bpp;
-                return blk < 8 && 8 * j + blk < nb && col < a.c.max_pages ? tbl[col] : -1;
+            const int blk = lane / NB, half = lane % NB;
+            int ahead = blk < 8 ? page_of(blk) : -1, place = 0;
+            auto load = [&](uint8_t *dst, int page, int j, int v, uint32_t bar) {
+                const int row = ((page * 2 * a.c.Hkv + kvh + v * a.c.Hkv) << a.c.ps_log2) + ((block_of(8 * j + blk) << 4) & ((1 << a.c.ps_log2) - 1));
+                if (page >= 0) tma_load_2d(smem_u32(dst) + half * KB + blk * 2048, &tmap, 64 * half, row, bar);
             };
-            int ahead = page_of(0);
-            for (int j = 0; j < n_kt; ++j) {
-                int page = ahead;
-                ahead = page_of(j + 1);  // (under way while this tile waits for its place)
-                if (page < 0 || page >= a.c.n_pages) {
-                    if (blk < 8 && 8 * j + blk < nb) s_err = DEV_BAD_PAGE;
-                    page = -1;
-                }
-                const unsigned got = __ballot_sync(0xffffffffu, page >= 0);
-                const uint32_t bytes = (uint32_t)__popc(got) * 16 * 128;
-                const int row = page < 0 ? 0 : ((page * 2 * a.c.Hkv + kvh) << a.c.ps_log2) + ((block_of(j) << 4) & ((1 << a.c.ps_log2) - 1));
-                if (lane == 0) {
-                    uint32_t valid = 0;  // blocks that are there, for the softmax (four places: this warp is never four tiles ahead of it)
-                    for (int i = 0; i < 8; ++i) valid |= ((got >> (i * NB)) & 1u) << i;
-                    s_valid[j & 3] = valid;
-                    mbar_arrive(b_i + 8 * (j & 3));
-                }
-                bool good = true;
-#pragma unroll
-                for (int v = 0; v < 2 && good; ++v) {  // K, V
-                    const int fill = 2 * j + v;
-                    const uint32_t slot = slot_of(fill);
-                    if (fill >= kWpSlots) good = __all_sync(0xffffffffu, mbar_wait(b_free + 8 * slot, turn_of(fill) ^ 1u, abortp, &s_err));
-                    if (!good) break;
-                    if (lane == 0) mbar_expect_tx(b_full + 8 * slot, bytes);
-                    __syncwarp();
-                    if (page >= 0) tma_load_2d(smem_u32(skv) + (slot * NB + half) * KB + blk * 2048, &tmap, 64 * half, row + v * (a.c.Hkv << a.c.ps_log2), b_full + 8 * slot);
-                }
-                if (!good) break;
+            // K of tile j + 1 comes together with V of tile j
+            int page = -1;  // of tile j
+            uint32_t bytes = 0;
+            for (int j = -1; j < n_kt; ++j) {
+                const int next = ahead;  // of tile j + 1
+                ahead = blk < 8 ? page_of(8 * (j + 2) + blk) : -1;  // (under way while this tile waits for its place)
+                if (blk < 8 && 8 * (j + 1) + blk < nb && next < 0) s_err = DEV_BAD_PAGE;
+                const uint32_t k_bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, next >= 0)) * 2048u, bar = j < 0 ? b_first : b_full + 8 * (j & 3);
+                if (j >= 2) wp_wait(b_free + 8 * (j & 1), (j >> 1) - 1, abortp, &s_err);
+                if (lane == 0) mbar_expect_tx(bar, bytes + k_bytes);
+                __syncwarp();
+                load(sk + place * NB * KB, next, j + 1, 0, bar);
+                if (j >= 0) load(sv + (j & 1) * NB * KB, page, j, 1, bar);
+                page = next;
+                bytes = k_bytes;
+                place = place == 2 ? 0 : place + 1;
             }
         } else if (warp == 1) {
-            const uint64_t dq = tc_smem_desc(smem_u32(sq)), dk = tc_smem_desc(smem_u32(skv)), dv = pt_desc_n(smem_u32(skv), KB);
+            const uint64_t dq = tc_smem_desc(smem_u32(sq)), dk = tc_smem_desc(smem_u32(sk)), dv = pt_desc_n(smem_u32(sv), KB);
             const int n_t = uniform(n_kt), n_q = uniform(nq);
-            auto scores = [&](int q, int j) {
-                const uint32_t slot = slot_of(2 * j);
-                if (q == 0 && !__all_sync(0xffffffffu, mbar_wait(b_full + 8 * slot, turn_of(2 * j), abortp, &s_err))) return false;
+            const bool leader = elect_one();
+            auto scores = [&](int q, uint64_t k_desc) {
+#pragma unroll
+                for (int k = 0; k < DH / 16; ++k)
+                    tc_mma(tmem + 128u * q, dq + (q * NB + (k >> 2)) * (QB >> 4) + 2 * (k & 3), k_desc + (k >> 2) * (KB >> 4) + 2 * (k & 3), kIdS, k ? 1u : 0u);
+                tc_commit(b_s + 8 * q);
+            };
+            if (n_t > 0) {
+                wp_wait(b_q, 0, abortp, &s_err);
+                wp_wait(b_first, 0, abortp, &s_err);
                 tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < DH / 16; ++k)
-                        tc_mma(tmem + 128u * q, dq + (q * NB + (k >> 2)) * (QB >> 4) + 2 * (k & 3), dk + (slot * NB + (k >> 2)) * (KB >> 4) + 2 * (k & 3), kIdS, k ? 1u : 0u);
-                    tc_commit(b_s + 8 * q);
-                    if (q == n_q - 1) tc_commit(b_free + 8 * slot);
+                if (leader) {
+                    scores(0, dk);
+                    if (n_q == 2) scores(1, dk);
                 }
-                __syncwarp();
-                return true;
-            };
-            auto values = [&](int q, int j) {
-                const uint32_t slot = slot_of(2 * j + 1);
-                if (q == 0 && !__all_sync(0xffffffffu, mbar_wait(b_full + 8 * slot, turn_of(2 * j + 1), abortp, &s_err))) return false;
+            }
+            int place = 0;
+            for (int j = 0; j < n_t; ++j) {
+                place = place == 2 ? 0 : place + 1;  // of K of the next tile
+                const uint64_t v = dv + (j & 1) * (NB * KB >> 4), k_desc = dk + place * (NB * KB >> 4);
+                wp_wait(b_full + 8 * (j & 3), j >> 2, abortp, &s_err);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {  // half of the keys
-                    if (!__all_sync(0xffffffffu, mbar_wait(b_p + 8 * (2 * q + h), j & 1, abortp, &s_err))) return false;
-                    tc_fence_after();
-                    if (elect_one()) {
+                for (int q = 0; q < 2; ++q) {
+                    if (q == 1 && n_q == 1) break;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)  // 16 keys: 8 columns of P, 2048 bytes of V
-                            tc_mma_ts(tmem + kO + (uint32_t)DH * q, tmem + 128u * q + 32 * h + 8 * k, dv + slot * (NB * KB >> 4) + (4 * h + k) * (2048 >> 4), kIdO, (j | h | k) ? 1u : 0u);
-                        if (h == 1) {
-                            if (q == n_q - 1) tc_commit(b_free + 8 * slot);
-                            if (j == n_t - 1) tc_commit(b_o + 8 * q);
+                    for (int h = 0; h < 2; ++h) {  // half of the keys
+                        wp_wait(b_p + 8 * (2 * q + h), j, abortp, &s_err);
+                        tc_fence_after();
+                        if (leader) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)  // 16 keys: 8 columns of P, 2048 bytes of V
+                                tc_mma_ts(tmem + kO + (uint32_t)DH * q, tmem + 128u * q + 32 * h + 8 * k, v + (4 * h + k) * (2048 >> 4), kIdO, (j | h | k) ? 1u : 0u);
+                            if (h == 1) {
+                                if (q == n_q - 1) tc_commit(b_free + 8 * (j & 1));
+                                if (j + 1 < n_t) scores(q, k_desc);
+                                else tc_commit(b_o + 8 * q);
+                            }
                         }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
-                return true;
-            };
-            bool ok = n_t > 0 && __all_sync(0xffffffffu, mbar_wait(b_q, 0, abortp, &s_err));
-            for (int q = 0; q < n_q && ok; ++q) ok = scores(q, 0);
-            for (int j = 0; j < n_t && ok; ++j)
-                for (int q = 0; q < n_q && ok; ++q) ok = values(q, j) && (j + 1 == n_t || scores(q, j + 1));
+            }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         {  // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
             const uint32_t turn = a.scale_log2 < 0.f ? 0x80008000u : 0u;
             constexpr int C8 = DH / 8, U = C8;  // 16-byte chunks of a row; all of a thread's are under way together
-            const int u0 = tid - 128, n_u = nq * kWpRows * C8;
+            const int u0 = tid - 128, c8 = u0 % C8, inv_gq = 65536 / gq + 1;  // (r * inv_gq >> 16 = r / gq for r < 128)
+            const T *src = static_cast<const T *>(a.q) + tok0 * a.q_tok + kvh * gq * a.q_head + 8 * c8;
             uint4 x[U];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int u = u0 + 256 * i, rr = u / C8 % kWpRows, p = u / (C8 * kWpRows) * per + rr / gq, g = rr % gq;
+                const int rr = u0 / C8 + i * (256 / C8), r = rr % kWpRows, pp = r * inv_gq >> 16, p = rr / kWpRows * per + pp, g = r - pp * gq;
                 x[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (u < n_u && rr < per * gq && p < n_tok)
-                    x[i] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + (tok0 + p) * a.q_tok + (kvh * gq + g) * a.q_head + 8 * (u % C8));
+                if (pp < per && p < n_tok) x[i] = *reinterpret_cast<const uint4 *>(src + p * a.q_tok + g * a.q_head);
             }
+            bool missing = false;
+            for (int u = u0; u < nb; u += 256) missing = missing || page_of(u) < 0;
+            if (missing) s_missing = 1;
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int u = u0 + 256 * i, c8 = u % C8, rr = u / C8 % kWpRows;
+                const int rr = u0 / C8 + i * (256 / C8), r = rr % kWpRows;
                 x[i].x ^= turn; x[i].y ^= turn; x[i].z ^= turn; x[i].w ^= turn;
-                if (u < n_u) *reinterpret_cast<uint4 *>(sq + u / (C8 * kWpRows) * NB * QB + (c8 >> 3) * QB + rr * 128 + (((c8 & 7) ^ (rr & 7)) * 16)) = x[i];
+                *reinterpret_cast<uint4 *>(sq + rr / kWpRows * NB * QB + (c8 >> 3) * QB + r * 128 + (((c8 & 7) ^ (r & 7)) * 16)) = x[i];
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(b_q);
+            asm volatile("bar.sync 1, 256;" ::: "memory");  // (s_missing)
         }
         const int q = (warp - 4) >> 2, r = 32 * (warp & 3) + lane, p = q * per + r / gq;
-        const bool live = r < per * gq && p < n_tok;
+        bool live = r < per * gq && p < n_tok;
         if (q < nq) {
             const int pos = pos0 + min(p, n_tok - 1);
             const int c_sink = min(a.sinks, max(pos + 1, 0)), c_lo = window_low(pos, a.window) - shift, c_hi = pos + 1 - shift;  // columns seen: [0, c_sink), [c_lo, c_hi)
@@ -327,21 +356,21 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + 128u * q + quarter, t_o = tmem + kO + (uint32_t)DH * q + quarter;
             const float c = fmaxf(fabsf(a.scale_log2), 1e-30f);  // (a scale of 0: every score 0, hidden ones -inf still)
             float m = -CUDART_INF_F, l = 0.f;
-            bool ok = true;
+            const bool missing = s_missing != 0;
             for (int j = 0; j < n_kt; ++j) {
                 const int c0 = 128 * j;
+                uint32_t valid = 0xffu;  // blocks that are there
                 bool part = !(c0 >= all_lo && c0 + 128 <= all_hi) && !(c0 + 128 <= all_sink);
-                ok = __all_sync(0xffffffffu, mbar_wait(b_i + 8 * (j & 3), (j >> 2) & 1, abortp, &s_err));
-                if (!ok) break;
-                const uint32_t valid = s_valid[j & 3];
-                part = part || valid != 0xffu;
-                if (part && q == 0) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(b_full + 8 * slot_of(2 * j + 1), turn_of(2 * j + 1), abortp, &s_err));
-                    if (!ok) break;
+                if (missing) {
+#pragma unroll 1
+                    for (int i = 0; i < 8; ++i)
+                        if (8 * j + i < nb && page_of(8 * j + i) < 0) valid &= ~(1u << i);
+                    part = part || valid != 0xffu;
                 }
                 if (part && q == 0) {  // thread = V row: those that nobody sees become zero, the others are looked through
+                    wp_wait(b_full + 8 * (j & 3), j >> 2, abortp, &s_err);
                     const int cc = c0 + r;
-                    uint8_t *row = skv + slot_of(2 * j + 1) * NB * KB + r * 128;
+                    uint8_t *row = sv + (j & 1) * NB * KB + r * 128;
                     if ((valid >> (r >> 4) & 1u) && (cc < any_sink || (cc >= any_lo && cc < any_hi))) {
                         // an exponent of ones (what is no number) and one more carries into the sign's place
                         constexpr uint32_t E = std::is_same<T, __nv_bfloat16>::value ? 0x7f807f80u : 0x7c007c00u, ONE = E & ~(E << 1);
@@ -358,8 +387,8 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                ok = __all_sync(0xffffffffu, mbar_wait(b_s + 8 * q, j & 1, abortp, &s_err));
-                if (!ok) break;
+                wp_wait(b_s + 8 * q, j, abortp, &s_err);
+                __syncwarp();
                 tc_fence_after();
                 uint32_t s[4][32];
 #pragma unroll
@@ -385,13 +414,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 while (true) {
                     sum = 0ull;
                     const float base = m == -CUDART_INF_F ? 0.f : m;
-                    wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), sum, w);
-                    float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
-                    const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
+                    float mx;
+                    wp_exps<T, true>(s, 0, c2, f2_pack(-base, -base), sum, w, mx);
+                    mx *= c;
                     const bool grow = !(mx <= m + kWpLazy) && !(m != m);  // (a maximum that is no number stays)
                     if (!__any_sync(0xffffffffu, grow)) break;
                     const float corr = grow ? ex2(m - mx) : 1.f;
@@ -421,17 +446,20 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 wp_pin(s[3]);
                 {
                     const float base = m == -CUDART_INF_F ? 0.f : m;
-                    wp_exps<T>(s[2], s[3], c2, f2_pack(-base, -base), sum, w);
+                    float none;
+                    wp_exps<T, false>(s, 1, c2, f2_pack(-base, -base), sum, w, none);
                 }
                 hand_over(1);
                 float l0, l1;
                 f2_unpack(sum, l0, l1);
                 l += l0 + l1;
             }
-            if (ok && n_kt > 0) ok = __all_sync(0xffffffffu, mbar_wait(b_o + 8 * q, 0, abortp, &s_err));
+            if (n_kt > 0) wp_wait(b_o + 8 * q, 0, abortp, &s_err);
+            __syncwarp();
             tc_fence_after();
-            if (ok) {
+            {
                 const bool none = m == -CUDART_INF_F;  // (no key seen: O may be 0 x whatever)
+                live = live && !*abortp;
                 const float inv = none ? 0.f : 1.f / l;
                 T *out = static_cast<T *>(a.out) + ((size_t)(tok0 + p) * a.Hq + kvh * gq + r % gq) * DH;
 #pragma unroll 1
@@ -474,6 +502,6 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
 }
 
 // (the head dim of 64 asks for as much as 128 does: no CTA that wants tensor memory shares an SM with one that holds all of it)
-inline size_t window_attn_prompt_smem() { return 1024 + (2 + kWpSlots) * 2 * 128 * 128; }
+inline size_t window_attn_prompt_smem() { return 1024 + 7 * 2 * 128 * 128; }
 
 }  // namespace river
