@@ -101,88 +101,32 @@ __device__ __forceinline__ int prompt_seq(const int32_t *q_start, int n_seqs, in
     return lo;
 }
 
-__device__ __forceinline__ uint64_t f2_sub(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 // max of three that hands on what is no number
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// 2^x of two values by arithmetic: x = n + f with n the nearest whole number (the low bits of x + 1.5 x 2^23), 2^f by its minimax polynomial
-// on [-1/2, 1/2] (found by exchange; relative error 7.5e-5 in degree 3, 2.6e-6 in degree 4: below a twentieth of the rounding of P in
-// either type), n added to the exponent.  x below -126 gives 2^-126.
-__device__ __forceinline__ float ex2_here(float x) {  // (volatile: stays where it is written)
-    float y;
-    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
+// Probabilities of 64 keys, w = 2^(s c - m) in pairs, and their sum on top of `sum`.  (The special-function units give 4 of them a cycle
+// and quarter of an SM: 1024 of a tile's 1900 cycles.  A quarter, an eighth of them by a polynomial instead cost more than they saved,
+// 160 -> 171, 167 us: with one warp of a query tile per quarter it is the length of its program that counts, not a unit's rate.)
 template <class T>
-__device__ __forceinline__ uint64_t f2_ex2(uint64_t x) {
-    float x0, x1, t0, t1, p0, p1;
-    f2_unpack(x, x0, x1);
-    x = f2_pack(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-    const uint64_t t = f2_add(x, f2_pack(12582912.f, 12582912.f)), f = f2_sub(x, f2_sub(t, f2_pack(12582912.f, 12582912.f)));
-    uint64_t p;
-    auto two = [](float a) { return f2_pack(a, a); };
-    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        p = f2_fma(f, two(0.0551716685295105f), two(0.2426111251115799f));
-        p = f2_fma(f, p, two(0.6932609677314758f));
-        p = f2_fma(f, p, two(0.9999280571937561f));
-    } else {
-        p = f2_fma(f, two(0.009570102207362652f), two(0.05591785907745361f));
-        p = f2_fma(f, p, two(0.240247443318367f));
-        p = f2_fma(f, p, two(0.6931217908859253f));
-        p = f2_fma(f, p, two(0.9999992847442627f));
-    }
-    f2_unpack(t, t0, t1);
-    f2_unpack(p, p0, p1);
-    return f2_pack(__uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23)), __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23)));
-}
-// Probabilities of 64 keys: w = 2^(s c - m) in pairs, their sum on top of `sum`.  Every fourth pair by arithmetic: the special-function units
-// (4 lanes a cycle and quarter of an SM) would else take as long as the MMAs.
-constexpr int kWpByHand = 99;
-// The steps of neighbouring pairs are interleaved by hand, and with them (MAX) the maximum of all 128 scores: left in program order they
-// queue for one unit after the other.
-template <class T, bool MAX>
-__device__ __forceinline__ void wp_exps(const uint32_t (&s)[4][32], int half, uint64_t c2, uint64_t m2, uint64_t &sum, uint32_t (&w)[32], float &mx) {
-    uint64_t part[2] = {sum, 0ull}, x[34];
-    float p[34][2], top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+__device__ __forceinline__ void wp_exps(const uint32_t (&a)[32], const uint32_t (&b)[32], uint64_t c2, uint64_t m2, uint64_t &sum, uint32_t (&w)[32]) {
+    uint64_t part[2] = {sum, 0ull};
+    float p[32][2];
 #pragma unroll
-    for (int e = 0; e < 34; ++e) {
-        if (e < 32) {
-            const uint32_t *v = s[2 * half + (e >> 4)] + 2 * (e & 15);
-            x[e] = f2_fma(f2_pack(__uint_as_float(v[0]), __uint_as_float(v[1])), c2, m2);
-        }
-        if (e >= 1 && e < 33) {
-            const int k = e - 1;
-            if (k % kWpByHand == kWpByHand - 1) {
-                f2_unpack(f2_ex2<T>(x[k]), p[k][0], p[k][1]);
-            } else {
-                f2_unpack(x[k], p[k][0], p[k][1]);
-                p[k][0] = ex2_here(p[k][0]);
-            }
-        }
-        if (MAX && e < 32) {
-            const uint32_t *v = s[e >> 3] + 4 * (e & 7);
-            top[e & 3] = max3_nan(top[e & 3], __uint_as_float(v[0]), __uint_as_float(v[1]));
-            top[(e + 2) & 3] = max3_nan(top[(e + 2) & 3], __uint_as_float(v[2]), __uint_as_float(v[3]));
-        }
-        if (e >= 1 && e < 33) {
-            const int k = e - 1;
-            if (k % kWpByHand != kWpByHand - 1) p[k][1] = ex2_here(p[k][1]);
-        }
-        if (e >= 2) {
-            const int k = e - 2;
-            part[k & 1] = f2_add(part[k & 1], f2_pack(p[k][0], p[k][1]));
-            w[k] = pack_pair<T>(p[k][0], p[k][1]);
-        }
+    for (int e = 0; e < 32; ++e) {
+        const uint32_t *s = e < 16 ? a + 2 * e : b + 2 * e - 32;
+        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[0]), __uint_as_float(s[1])), c2, m2), p[e][0], p[e][1]);
+        p[e][0] = ex2(p[e][0]);
+        p[e][1] = ex2(p[e][1]);
+    }
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+        part[e & 1] = f2_add(part[e & 1], f2_pack(p[e][0], p[e][1]));
+        w[e] = pack_pair<T>(p[e][0], p[e][1]);
     }
     sum = f2_add(part[0], part[1]);
-    if (MAX) mx = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]);
 }
 
 template <class T, int DH>
@@ -414,9 +358,13 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 while (true) {
                     sum = 0ull;
                     const float base = m == -CUDART_INF_F ? 0.f : m;
-                    float mx;
-                    wp_exps<T, true>(s, 0, c2, f2_pack(-base, -base), sum, w, mx);
-                    mx *= c;
+                    float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
+                    const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
+                    wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), sum, w);
                     const bool grow = !(mx <= m + kWpLazy) && !(m != m);  // (a maximum that is no number stays)
                     if (!__any_sync(0xffffffffu, grow)) break;
                     const float corr = grow ? ex2(m - mx) : 1.f;
@@ -446,8 +394,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 wp_pin(s[3]);
                 {
                     const float base = m == -CUDART_INF_F ? 0.f : m;
-                    float none;
-                    wp_exps<T, false>(s, 1, c2, f2_pack(-base, -base), sum, w, none);
+                    wp_exps<T>(s[2], s[3], c2, f2_pack(-base, -base), sum, w);
                 }
                 hand_over(1);
                 float l0, l1;
