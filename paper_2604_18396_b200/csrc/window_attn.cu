@@ -9,8 +9,9 @@ namespace river {
 namespace {
 
 template <class T, int DH>
-void launch_step(const WindowArgs &a, cudaStream_t st) {
+int launch_step(const WindowArgs &a, cudaStream_t st) {
     const int splits = step_splits(a, 148);
+    if (splits > 8 && cudaFuncSetAttribute(window_attn_step_kernel<T, DH>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return RIVER_E_DEVICE;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim = {(unsigned)splits, 1, 1};
@@ -20,7 +21,7 @@ void launch_step(const WindowArgs &a, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, window_attn_step_kernel<T, DH>, a, splits);
+    return cudaLaunchKernelEx(&cfg, window_attn_step_kernel<T, DH>, a, splits) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
 }
 
 template <class T, int DH>
@@ -43,10 +44,7 @@ int launch_prompt(const WindowArgs &a, cudaStream_t st) {
 template <class T, int DH>
 int launch(const WindowArgs &a, cudaStream_t st) {
     const int gq = a.Hq / a.c.Hkv;
-    if (a.max_q <= 4 || gq > kWpRows) {
-        launch_step<T, DH>(a, st);
-        return RIVER_OK;
-    }
+    if (a.max_q <= 4 || gq > kWpRows) return launch_step<T, DH>(a, st);
     return launch_prompt<T, DH>(a, st);
 }
 

@@ -1,7 +1,7 @@
 // Windowed attention of single tokens: split over the visible positions and joined inside a cluster (sm_100a, internal).
 //
 // A cluster owns one query token and up to eight query heads of one KV head; its CTAs share out the visible blocks of 16 positions
-// (those of the sinks, then those of the window), a warp takes every eighth block of its CTA.  Everything stays in registers:
+// (those of the sinks, then those of the window), a warp takes every fourth block of its CTA.  Everything stays in registers:
 //   S [8 heads x 16 keys] = Q K^T      mma.sync m16n8k16, rows = heads (the upper eight are zero).  Products of a sum may come in any order,
 //                                      so a lane's 16 consecutive bytes of a key row are the B operand of two steps as they are loaded, and
 //                                      Q is loaded in the same order: no shared memory, no transposition.
@@ -20,8 +20,9 @@
 
 namespace river {
 
-constexpr int kStepWarps = 8;
-constexpr int kStepMaxSplits = 8;  // CTAs of a cluster (the portable size)
+constexpr int kStepWarps = 4;
+constexpr int kStepCtas = 3;         // resident per SM (168 registers)
+constexpr int kStepMaxSplits = 16;   // CTAs of a cluster
 
 template <class T> __device__ __forceinline__ void mma_16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
 template <> __device__ __forceinline__ void mma_16<__nv_bfloat16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -58,7 +59,7 @@ template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float a, float
 
 // grid: splits x (Hkv * tiles of eight heads) x (max_q * n_seqs), linear, clusters of `splits`
 template <class T, int DH>
-__global__ void __launch_bounds__(32 * kStepWarps, 2) window_attn_step_kernel(const WindowArgs a, int splits) {
+__global__ void __launch_bounds__(32 * kStepWarps, kStepCtas) window_attn_step_kernel(const WindowArgs a, int splits) {
     namespace cg = cooperative_groups;
     constexpr int C = DH / 32, H = DH / 64;  // 16-byte chunks of a K row per lane; of a V row
     __shared__ float s_o[kStepWarps][8][DH];
@@ -209,39 +210,39 @@ __global__ void __launch_bounds__(32 * kStepWarps, 2) window_attn_step_kernel(co
         }
     }
     __syncthreads();
-    // the warps' parts: warp = head, lane = dims
+    // the warps' parts: a warp per head, lane = dims
     constexpr int E = DH / 32;
-    float mm = -CUDART_INF_F, ll = 0.f, acc[E];
+    for (int h = warp; h < heads; h += kStepWarps) {
+        float mm = -CUDART_INF_F, ll = 0.f, acc[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < kStepWarps; ++w) mm = fmaxf(mm, s_ml[w][warp].x);
-    const float mb = mm == -CUDART_INF_F ? 0.f : mm;
+        for (int w = 0; w < kStepWarps; ++w) mm = fmaxf(mm, s_ml[w][h].x);
+        const float mb = mm == -CUDART_INF_F ? 0.f : mm;
 #pragma unroll
-    for (int w = 0; w < kStepWarps; ++w) {
-        const float2 x = s_ml[w][warp];
-        const float f = ex2(x.x - mb);
-        ll += x.y * f;
+        for (int w = 0; w < kStepWarps; ++w) {
+            const float2 x = s_ml[w][h];
+            const float f = ex2(x.x - mb);
+            ll += x.y * f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += s_o[w][warp][E * lane + e] * f;
-    }
-    if (splits == 1) {
-        if (warp < heads) {
+            for (int e = 0; e < E; ++e) acc[e] += s_o[w][h][E * lane + e] * f;
+        }
+        if (splits == 1) {
             const float inv = ll == 0.f ? 0.f : 1.f / ll;
 #pragma unroll
-            for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(out + warp * DH + E * lane + e) = pack_pair<T>(acc[e] * inv, acc[e + 1] * inv);
-        }
-        return;
-    }
-    // the cluster's parts: a CTA finishes 8 / splits heads
+            for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(out + h * DH + E * lane + e) = pack_pair<T>(acc[e] * inv, acc[e + 1] * inv);
+        } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_c[warp][E * lane + e] = acc[e];
-    if (lane == 0) s_cml[warp] = make_float2(mm, ll);
+            for (int e = 0; e < E; ++e) s_c[h][E * lane + e] = acc[e];
+            if (lane == 0) s_cml[h] = make_float2(mm, ll);
+        }
+    }
+    if (splits == 1) return;
+    // the cluster's parts: every CTA finishes its share of the heads' dims
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
-    const int per = 8 * DH / 2 / splits;  // pairs of dims
-    for (int x = threadIdx.x; x < per; x += 32 * kStepWarps) {
-        const int e = 2 * (split * per + x), head = e / DH, d = e % DH;
+    for (int x = split * 32 * kStepWarps + threadIdx.x; x < heads * DH / 2; x += splits * 32 * kStepWarps) {  // pairs of dims
+        const int e = 2 * x, head = e / DH, d = e % DH;
         float2 ml[kStepMaxSplits], v[kStepMaxSplits];
         float top = -CUDART_INF_F;
 #pragma unroll
@@ -265,19 +266,29 @@ __global__ void __launch_bounds__(32 * kStepWarps, 2) window_attn_step_kernel(co
             x1 += v[r].y * f;
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        if (head < heads) *reinterpret_cast<uint32_t *>(out + e) = pack_pair<T>(x0 * inv, x1 * inv);
+        *reinterpret_cast<uint32_t *>(out + e) = pack_pair<T>(x0 * inv, x1 * inv);
     }
     cluster.sync();  // (peers read this CTA's part)
 }
 
-// CTAs per cluster: enough that the grid fills the SMs several times over (a last round that is not full costs less then), at
-// least a block per warp.
+// CTAs per cluster, by an estimate of the time in us.  A round of CTAs takes what HBM needs for its blocks, or 1.4 for each block
+// that a warp has one after the other (a fetch and the products behind it), and 2 + s / 4 for its start and the joining.  Clusters of more
+// than four leave places free: a GPC, of about 16 SMs, takes whole ones.  (8B-class heads, us with 3, 4, 6, 8, 16 CTAs: window 4096, 64
+// rows 185, 184, 203, 218, 304; 16 rows 48, 67, 53, 61, 84; 4 rows 35, 28, 22, 19, 26; window 8192, one row 60, 47, 33, 27, 17.)
 inline int step_splits(const WindowArgs &a, int num_sms) {
-    const int64_t rows = (int64_t)a.c.n_seqs * a.max_q * a.c.Hkv * ((a.Hq / a.c.Hkv + 7) / 8);
-    const int64_t cap = (int64_t)a.c.max_pages << a.c.ps_log2, blocks = (std::min<int64_t>(cap, (int64_t)a.window + a.sinks) >> 4) + 2;
-    int s = 1;
-    while (s < kStepMaxSplits && rows * s < 8 * num_sms && blocks > 2 * s * kStepWarps / 2) s *= 2;
-    return s;
+    const double units = (double)a.c.n_seqs * a.max_q * a.c.Hkv * ((a.Hq / a.c.Hkv + 7) / 8);
+    const int64_t cap = (int64_t)a.c.max_pages << a.c.ps_log2, blocks = (std::min<int64_t>(cap, (int64_t)a.window + a.sinks) >> 4) + 1;
+    const double block_us = 64.0 * a.c.dh / 6.4e6;  // K and V of a block at 6.4 TB/s
+    int best = 1;
+    double best_t = 1e300;
+    for (int s = 1; s <= kStepMaxSplits; ++s) {
+        const double places = s <= 4 ? num_sms * kStepCtas : num_sms / 18 * (16 * kStepCtas / s) * s;
+        const double turns = 1.4 * (double)((blocks + s * kStepWarps - 1) / (s * kStepWarps)), stream = places * (double)blocks / s * block_us, fixed = 2.0 + 0.25 * s;
+        const double rounds = units * s / places, full = std::floor(rounds), rest = rounds - full;
+        const double t = full * (std::max(stream, turns) + fixed) + (rest > 0 ? std::max(stream * rest, turns) + fixed : 0.0);
+        if (t < 0.99 * best_t) { best_t = t; best = s; }
+    }
+    return best;
 }
 
 }  // namespace river
