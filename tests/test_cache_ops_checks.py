@@ -173,3 +173,12 @@ def test_frequencies_per_pair(lib):
 def test_frequencies_refusals(lib, a, kw):
     with pytest.raises(RiverError):
         rope_frequencies(*a, **kw)
+
+
+def test_packed_structs_are_the_headers():
+    assert cache_ops._PAGED.size == C.sizeof(cache_ops.river_paged) and cache_ops._ROWS.size == C.sizeof(cache_ops.river_rows)
+    b = cache_ops._PAGED.pack(11, 12, 13, *range(1, 9))
+    s = cache_ops.river_paged.from_buffer_copy(b)
+    assert [getattr(s, n) for n, _ in s._fields_] == [11, 12, 13] + list(range(1, 9))
+    r = cache_ops.river_rows.from_buffer_copy(cache_ops._ROWS.pack(5, -6, 1 << 40))
+    assert (r.p, r.token, r.head) == (5, -6, 1 << 40)
