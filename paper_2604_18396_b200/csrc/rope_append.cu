@@ -61,33 +61,7 @@ struct RopeRow {
     }
 };
 
-// Any strides and sizes: a CTA per token, a thread per pair and, for the dims that stay, per dim.
-template <class TI, class TC, bool INTER>
-__global__ void __launch_bounds__(128) rope_append_any_kernel(const RopeArgs a) {
-    __shared__ float2 cs[64];
-    const int t = blockIdx.x, dh = a.c.dh, half = a.rot / 2, pos = a.positions[t], seq = a.seqs[t];
-    for (int i = threadIdx.x; i < half; i += blockDim.x) cs[i] = rope_turn(pos, a.inv_freq[i], a.scale);
-    bool bad;
-    const int page = rope_page(a, pos, seq, bad), inpage = pos & ((1 << a.c.ps_log2) - 1);
-    if (bad && threadIdx.x == 0) flag(a.status, RIVER_E_BADARG);
-    __syncthreads();
-    const int rows = a.Hq + 2 * a.c.Hkv, per = dh - half;
-    for (int u = threadIdx.x; u < rows * per; u += blockDim.x) {
-        const int r = u / per, i = u % per;
-        const RopeRow<TI, TC> row(a, t, r, page, inpage);
-        if (!row.dst) continue;
-        if (i < half) {
-            const int d0 = INTER ? 2 * i : i, d1 = INTER ? 2 * i + 1 : i + half;
-            const float x = to_f(row.src[d0]), y = to_f(row.src[d1]);
-            const float2 w = row.turn ? cs[i] : make_float2(1.f, 0.f);
-            row.dst[d0] = from_f<TC>(seq < 0 ? 0.f : row.turn ? x * w.x - y * w.y : x);
-            row.dst[d1] = from_f<TC>(seq < 0 ? 0.f : row.turn ? y * w.x + x * w.y : y);
-        } else {
-            row.dst[i + half] = from_f<TC>(seq < 0 ? 0.f : to_f(row.src[i + half]));
-        }
-    }
-}
-
+constexpr int kRopeTokens = 4;  // at most, of a CTA
 // Eight values of a row, 16 or 32 bytes as they come.
 template <class TI> struct Eight {
     uint4 w[sizeof(TI) / 2];
@@ -118,65 +92,113 @@ __device__ __forceinline__ void store_eight(TC *p, const float (&x)[8]) {
     *reinterpret_cast<uint4 *>(p) = w;
 }
 
-// 16-byte rows: thread (x, y) of a token's CTA takes unit x of every row y, y + blockDim.y, ..  A unit is eight dims (interleaved: four
-// pairs, or dims that stay), or eight pairs and their partners half a turned part further (half layout).  kRopeRows rows of a
-// thread are fetched before sines and cosines are there.  Bound by HBM for prompts: 8192 tokens of 48 heads of 128, three quarters
-// turned, bf16: 114.8 us with a thread per pair, see the launch for now; a single token by its chain of three loads.
-constexpr int kRopeRows = 2;
+// Any strides and sizes: a CTA per token, a thread per pair and, for the dims that stay, per dim - or per eight of them, from the first
+// multiple of eight on, where the rows allow it (`wide`).
 template <class TI, class TC, bool INTER>
-__global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
+__global__ void __launch_bounds__(256) rope_append_any_kernel(const RopeArgs a, int wide) {
     __shared__ float2 cs[64];
-    const int t = blockIdx.x, half = a.rot / 2, x = threadIdx.x, tid = threadIdx.y * blockDim.x + x, rows = a.Hq + 2 * a.c.Hkv;
-    const int pos = a.positions[t], seq = a.seqs[t];
-    // dims of this unit: d0 .. d0 + 7, and in the half layout d1 .. d1 + 7
-    const bool pairs = x < a.rot / (INTER ? 8 : 16);
-    const int d0 = INTER || pairs ? 8 * x : 8 * x + half, d1 = d0 + half;
+    const int t = blockIdx.x, dh = a.c.dh, half = a.rot / 2, pos = a.positions[t], seq = a.seqs[t];
+    for (int i = threadIdx.x; i < half; i += blockDim.x) cs[i] = rope_turn(pos, a.inv_freq[i], a.scale);
     bool bad;
     const int page = rope_page(a, pos, seq, bad), inpage = pos & ((1 << a.c.ps_log2) - 1);
-    if (bad && tid == 0) flag(a.status, RIVER_E_BADARG);
-    for (int r0 = threadIdx.y; r0 - (int)threadIdx.y < rows; r0 += kRopeRows * blockDim.y) {
-        Eight<TI> u[kRopeRows], v[kRopeRows];
-        TC *dst[kRopeRows];
-        bool turn[kRopeRows];
+    if (bad && threadIdx.x == 0) flag(a.status, RIVER_E_BADARG);
+    __syncthreads();
+    const int rows = a.Hq + 2 * a.c.Hkv, eights = wide ? (a.rot + 7) / 8 * 8 : dh, single = half + eights - a.rot, per = single + (dh - eights) / 8;
+    for (int u = threadIdx.x; u < rows * per; u += blockDim.x) {
+        const int r = u / per, i = u - r * per;
+        const RopeRow<TI, TC> row(a, t, r, page, inpage);
+        if (!row.dst) continue;
+        if (i < half) {
+            const int d0 = INTER ? 2 * i : i, d1 = INTER ? 2 * i + 1 : i + half;
+            const float x = to_f(row.src[d0]), y = to_f(row.src[d1]);
+            const float2 w = row.turn ? cs[i] : make_float2(1.f, 0.f);
+            row.dst[d0] = from_f<TC>(seq < 0 ? 0.f : row.turn ? x * w.x - y * w.y : x);
+            row.dst[d1] = from_f<TC>(seq < 0 ? 0.f : row.turn ? y * w.x + x * w.y : y);
+        } else if (i < single) {
+            row.dst[i + half] = from_f<TC>(seq < 0 ? 0.f : to_f(row.src[i + half]));
+        } else {
+            const int d = eights + 8 * (i - single);
+            Eight<TI> e;
+            float p[8];
+            e.load(row.src + d);
+            e.get(p);
 #pragma unroll
-        for (int k = 0; k < kRopeRows; ++k) {
-            const int r = r0 + k * blockDim.y;
-            dst[k] = nullptr;
-            if (r < rows) {
-                const RopeRow<TI, TC> row(a, t, r, page, inpage);
-                dst[k] = row.dst;
-                turn[k] = row.turn && pairs;
-                if (row.dst) {
-                    u[k].load(row.src + d0);
-                    if (!INTER && pairs) v[k].load(row.src + d1);
-                }
+            for (int k = 0; k < 8; ++k) p[k] = seq < 0 ? 0.f : p[k];
+            store_eight(row.dst + d, p);
+        }
+    }
+}
+
+// 16-byte rows.  A CTA takes blockDim.z tokens; thread (x, y, z) unit x of the rows y, y + blockDim.y, .. of token z.  A unit is eight dims
+// (interleaved: four pairs, or dims that stay), or eight pairs and their partners half a turned part further (half layout).  UNITS rows of
+// a thread, 192 bytes, are under way before place and angles are known; a thread's sines and cosines are the same for all its rows.
+template <class TI, class TC, bool INTER, int UNITS>
+__global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
+    __shared__ float4 cs[kRopeTokens][32];  // two pairs' (cos, sin)
+    const int x = threadIdx.x, y = threadIdx.y, z = threadIdx.z, ny = blockDim.y, rows = a.Hq + 2 * a.c.Hkv, half = a.rot / 2;
+    const int t = blockIdx.x * blockDim.z + z;
+    const bool live = t < a.n_tokens;
+    // dims of this unit: d0 .. d0 + 7, and in the half layout d0 + half ..
+    const bool pairs = x < a.rot / (INTER ? 8 : 16);
+    const int d0 = INTER || pairs ? 8 * x : 8 * x + half;
+    const int pos = live ? a.positions[t] : 0, seq = live ? a.seqs[t] : -1;
+    // this thread's units of the token's first heads, in bytes; heads are a 32-bit step apart (the launch has looked)
+    const char *const q_at = static_cast<const char *>(a.q) + (t * a.q_tok + d0) * (int64_t)sizeof(TI);
+    const char *const k_at = static_cast<const char *>(a.k) + (t * a.k_tok + d0) * (int64_t)sizeof(TI);
+    const char *const v_at = static_cast<const char *>(a.v) + (t * a.v_tok + d0) * (int64_t)sizeof(TI) - (int64_t)a.c.Hkv * (int)a.v_head * (int)sizeof(TI);
+    const int q_step = (int)a.q_head * (int)sizeof(TI), k_step = (int)a.k_head * (int)sizeof(TI), v_step = (int)a.v_head * (int)sizeof(TI), dh = a.c.dh;
+    char *const q_to = static_cast<char *>(a.q_out) + ((size_t)t * a.Hq * dh + d0) * sizeof(TC);
+    char *kv_to = nullptr;  // the token's place in the K half of head 0; the heads of K, then of V, follow a page's rows apart
+    const int to_step = dh * (int)sizeof(TC), kv_step = to_step << a.c.ps_log2;
+    float2 w[INTER ? 4 : 8];
+    for (int r0 = y; r0 - y < rows; r0 += UNITS * ny) {
+        Eight<TI> u[UNITS], v[INTER ? 1 : UNITS];
+#pragma unroll
+        for (int k = 0; k < UNITS; ++k) {
+            const int r = r0 + k * ny, h = r - a.Hq;
+            if (!live || r >= rows) continue;
+            const char *base = h < 0 ? q_at : h < a.c.Hkv ? k_at : v_at;
+            const int step = h < 0 ? q_step : h < a.c.Hkv ? k_step : v_step;
+            const TI *src = reinterpret_cast<const TI *>(base + (int64_t)(h < 0 ? r : h) * step);
+            u[k].load(src);
+            if (!INTER && pairs) v[k].load(src + half);
+        }
+        if (r0 == y) {
+            for (int i = y * blockDim.x + x; i < half; i += blockDim.x * ny) reinterpret_cast<float2 *>(cs[z])[i] = rope_turn(pos, a.inv_freq[i], a.scale);
+            bool bad;
+            const int page = rope_page(a, pos, seq, bad);
+            if (bad && x == 0 && y == 0) flag(a.status, RIVER_E_BADARG);
+            if (page >= 0) kv_to = reinterpret_cast<char *>(a.c.pool) + (a.c.row(a.layer0, page, 0, 0, pos & ((1 << a.c.ps_log2) - 1)) + d0) * sizeof(TC);
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < (INTER ? 4 : 8); e += 2) {
+                const float4 c = pairs ? cs[z][(INTER ? 2 : 4) * x + e / 2] : make_float4(1.f, 0.f, 1.f, 0.f);
+                w[e] = make_float2(c.x, c.y);
+                w[e + 1] = make_float2(c.z, c.w);
             }
         }
-        if (r0 == (int)threadIdx.y) {
-            for (int i = tid; i < half; i += blockDim.x * blockDim.y) cs[i] = rope_turn(pos, a.inv_freq[i], a.scale);
-            __syncthreads();
-        }
 #pragma unroll
-        for (int k = 0; k < kRopeRows; ++k) {
-            if (!dst[k]) continue;
+        for (int k = 0; k < UNITS; ++k) {
+            const int r = r0 + k * ny, h = r - a.Hq;
+            char *base = h < 0 ? q_to : kv_to;
+            if (!live || r >= rows || !base) continue;
+            TC *const dst = reinterpret_cast<TC *>(base + (int64_t)(h < 0 ? r : h) * (h < 0 ? to_step : kv_step));
             float p[8], q[8];
             u[k].get(p);
             if (!INTER && pairs) v[k].get(q);
-            if (turn[k]) {
+            if (h < a.c.Hkv && pairs) {
                 if constexpr (INTER) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float2 w = cs[4 * x + e];
-                        const float y0 = p[2 * e] * w.x - p[2 * e + 1] * w.y;
-                        p[2 * e + 1] = p[2 * e + 1] * w.x + p[2 * e] * w.y;
+                        const float y0 = p[2 * e] * w[e].x - p[2 * e + 1] * w[e].y;
+                        p[2 * e + 1] = p[2 * e + 1] * w[e].x + p[2 * e] * w[e].y;
                         p[2 * e] = y0;
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float2 w = cs[8 * x + e];
-                        const float y0 = p[e] * w.x - q[e] * w.y;
-                        q[e] = q[e] * w.x + p[e] * w.y;
+                        const float y0 = p[e] * w[e].x - q[e] * w[e].y;
+                        q[e] = q[e] * w[e].x + p[e] * w[e].y;
                         p[e] = y0;
                     }
                 }
@@ -185,26 +207,30 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) p[e] = q[e] = 0.f;
             }
-            store_eight(dst[k] + d0, p);
-            if (!INTER && pairs) store_eight(dst[k] + d1, q);
+            store_eight(dst, p);
+            if (!INTER && pairs) store_eight(dst + half, q);
         }
     }
 }
 
-// Rows that can be taken 16 bytes at a time: addresses and strides, and the turned part in whole units.
-bool rope_in_units(const RopeArgs &a, size_t es, bool inter) {
-    auto ok = [&](const void *p, int64_t tok, int64_t head) { return aligned_to(p, 16) && tok * (int64_t)es % 16 == 0 && head * (int64_t)es % 16 == 0; };
-    return ok(a.q, a.q_tok, a.q_head) && ok(a.k, a.k_tok, a.k_head) && ok(a.v, a.v_tok, a.v_head) && a.rot % (inter ? 8 : 16) == 0;
+// Rows that can be taken 16 bytes at a time: addresses and strides, a token's heads within 2 GB.
+bool rope_wide(const RopeArgs &a, size_t es) {
+    auto ok = [&](const void *p, int64_t tok, int64_t head) { return aligned_to(p, 16) && tok * (int64_t)es % 16 == 0 && head * (int64_t)es % 16 == 0 && head < (1 << 20) && head > -(1 << 20); };
+    return ok(a.q, a.q_tok, a.q_head) && ok(a.k, a.k_tok, a.k_head) && ok(a.v, a.v_tok, a.v_head);
 }
 
 template <class TI, class TC, bool INTER>
 void launch_rope(const RopeArgs &a, cudaStream_t st) {
-    if (!rope_in_units(a, sizeof(TI), INTER)) {
-        rope_append_any_kernel<TI, TC, INTER><<<a.n_tokens, 128, 0, st>>>(a);
+    const bool wide = rope_wide(a, sizeof(TI));
+    if (!wide || a.rot % (INTER ? 8 : 16)) {  // (8192 tokens of 48 heads of 128, bf16, a turned part of 34: 93 us; of 128, in units, 40)
+        rope_append_any_kernel<TI, TC, INTER><<<a.n_tokens, 256, 0, st>>>(a, wide);
         return;
     }
+    constexpr int UNITS = (INTER ? 24 : 12) / (int)sizeof(TI);
     const int per = INTER ? a.c.dh / 8 : a.rot / 16 + (a.c.dh - a.rot) / 8, rows = a.Hq + 2 * a.c.Hkv;
-    rope_append_kernel<TI, TC, INTER><<<a.n_tokens, dim3(per, std::min(256 / per, rows)), 0, st>>>(a);
+    // few tokens: a CTA each, with all the threads that its rows keep busy
+    const int y = a.n_tokens < 148 * 4 ? std::min(256 / per, rows) : std::min(256 / per, (rows + UNITS - 1) / UNITS), z = std::min(std::max(1, 256 / (per * y)), a.n_tokens < 148 * 4 ? 1 : kRopeTokens);
+    rope_append_kernel<TI, TC, INTER, UNITS><<<(a.n_tokens + z - 1) / z, dim3(per, y, z), 0, st>>>(a);
 }
 template <class TI, class TC>
 void launch_rope(const RopeArgs &a, bool inter, cudaStream_t st) {
