@@ -1,15 +1,23 @@
 // river_pages_advance, river_pages_reorder, river_pages_compact: the pages of a paged cache, kept on the device.
 //
-// Which page goes where is decided by one CTA: a few prefix sums over sequences and page ids.  Free pages are those with refs 0 after
-// what the call gives back; the k-th page that is wanted, in order of (sequence, position), receives the k-th free id.  The values
-// then move in a kernel of their own that reads the list of copies.
+// Which page goes where is decided by one cluster of CTAs: a few prefix sums over sequences (every CTA for itself, in shared memory)
+// and over page ids (a range of ids per CTA, the ranges' counts through distributed shared memory).  Free pages are those with refs
+// 0 after what the call gives back; the k-th page that is wanted, in order of (sequence, position), receives the k-th free id.  The
+// values then move in a kernel of their own, over all SMs, that reads the list of copies.
+#include <algorithm>
+
+#include <cooperative_groups.h>
+
 #include "paged_common.cuh"
 
 namespace river {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kPgThreads = 1024;
-constexpr int kPgSeqs = 8192;  // sequences whose prefix sums are held in shared memory
+constexpr int kPgSeqs = 8192;    // sequences whose prefix sums are held in shared memory
+constexpr int kPgCtas = 8;       // of the deciding cluster (a portable size)
 
 struct PagesArgs {
     Paged c;
@@ -17,6 +25,14 @@ struct PagesArgs {
     int window, sinks;
     int32_t *table_out, *lens_out, *refs_out, *list, *status;  // list: of copies or moves
     int32_t *remap, *n_used;
+};
+
+// Shared memory of a deciding CTA; `count` is read and the first one's `odd` written by the other CTAs of the cluster.
+struct PagesShared {
+    int part[33], count[2];
+    int bad, full;  // what every CTA finds for itself: a sequence or length out of range, a row too long
+    int odd;        // a page out of range: the first CTA's tells, behind a barrier of the cluster
+    int prefix[kPgSeqs];
 };
 
 // Exclusive prefix sum over the CTA's threads (`part`: 33 ints); `total` gets the sum.  Ends with a barrier behind every read.
@@ -61,20 +77,65 @@ __device__ int scan_shared(int *s, int n, int *part) {
     return base;
 }
 
-// give(k, id) for the `want` lowest ids with refs 0, ascending; returns how many there were (at most want).
-template <class F>
-__device__ int lowest_free(const volatile int32_t *refs, int n_pages, int want, int *part, F give) {
-    int got = 0;
-    for (int p0 = 0; p0 < n_pages && got < want; p0 += kPgThreads) {
-        const int p = p0 + threadIdx.x;
-        const bool free_ = p < n_pages && refs[p] == 0;
-        int total;
-        const int k = got + cta_scan(free_, part, total);
-        if (free_ && k < want) give(k, p);
-        got += total;
+// The cluster's view of the page ids: this CTA's range, in runs of four per thread.
+struct Ids {
+    int lo, hi;
+    __device__ __forceinline__ Ids(int n, int rank, int ctas) {
+        const int per = ((n + ctas - 1) / ctas + 3) & ~3;
+        lo = min(n, rank * per);
+        hi = min(n, lo + per);
     }
-    __syncthreads();
-    return min(got, want);
+};
+// f(ids of a thread's run, of which `n` are in range) for the range's ids in ascending order over the threads; every thread takes part in
+// every round.
+template <class F>
+__device__ __forceinline__ void for_ids(const Ids &ids, F f) {
+    for (int p0 = ids.lo; p0 < ids.hi; p0 += 4 * kPgThreads) {
+        const int p = p0 + 4 * threadIdx.x;
+        f(p, max(0, min(4, ids.hi - p)));
+    }
+}
+__device__ __forceinline__ void load_refs(const int32_t *refs, int p, int n, int (&r)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = e < n ? __ldcg(refs + p + e) : 0x7fffffff;
+}
+
+// give(k, id) for the `want` lowest ids with refs 0, ascending, if there are as many; returns whether there are.  All CTAs of the cluster.
+template <class F>
+__device__ bool lowest_free(const int32_t *refs, int n_pages, int want, PagesShared &s, cg::cluster_group &cluster, F give) {
+    const int rank = cluster.block_rank(), ctas = cluster.num_blocks();
+    const Ids ids(n_pages, rank, ctas);
+    int mine = 0;
+    for_ids(ids, [&](int p, int n) {
+        int r[4], total;
+        load_refs(refs, p, n, r);
+        cta_scan((r[0] == 0) + (r[1] == 0) + (r[2] == 0) + (r[3] == 0), s.part, total);
+        mine += total;
+    });
+    if (threadIdx.x == 0) s.count[0] = mine;
+    cluster.sync();
+    int before = 0, all = 0;
+    for (int c = 0; c < ctas; ++c) {
+        const int x = *cluster.map_shared_rank(&s.count[0], c);
+        if (c < rank) before += x;
+        all += x;
+    }
+    cluster.sync();  // (counts have been read)
+    if (all < want) return false;
+    for_ids(ids, [&](int p, int n) {
+        if (before >= want) return;  // (uniform)
+        int r[4], total;
+        load_refs(refs, p, n, r);
+        int k = before + cta_scan((r[0] == 0) + (r[1] == 0) + (r[2] == 0) + (r[3] == 0), s.part, total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (r[e] == 0) {
+                if (k < want) give(k, p + e);
+                ++k;
+            }
+        before += total;
+    });
+    return true;
 }
 // the last i < n with prefix[i] <= k (prefix[0] = 0): whose want number k is
 __device__ __forceinline__ int owner_of(const int *prefix, int n, int k) {
@@ -85,187 +146,287 @@ __device__ __forceinline__ int owner_of(const int *prefix, int n, int k) {
     }
     return lo;
 }
+// n ints, by all threads of the cluster
+__device__ __forceinline__ void copy_ints(int32_t *to, const int32_t *from, size_t n, int thread, int threads) {
+    if (((reinterpret_cast<uintptr_t>(to) | reinterpret_cast<uintptr_t>(from)) & 15) == 0) {
+        int4 *t = reinterpret_cast<int4 *>(to);
+        const int4 *f = reinterpret_cast<const int4 *>(from);
+        size_t i = thread;
+        for (; i + 3 * (size_t)threads < n / 4; i += 4 * (size_t)threads) {
+            int4 v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = f[i + e * (size_t)threads];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[i + e * (size_t)threads] = v[e];
+        }
+        for (; i < n / 4; i += threads) t[i] = f[i];
+        for (i = n / 4 * 4 + thread; i < n; i += threads) to[i] = from[i];
+    } else {
+        for (size_t i = thread; i < n; i += threads) to[i] = from[i];
+    }
+}
 
 __global__ void __launch_bounds__(kPgThreads) pages_advance_kernel(const PagesArgs a) {
-    __shared__ int part[33], s_bad, s_full, prefix[kPgSeqs];
-    const int S = a.c.n_seqs, P = a.c.max_pages, N = a.c.n_pages, lg = a.c.ps_log2, lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) s_bad = s_full = 0;
-    if (a.table_out != a.c.table)
-        for (size_t i = threadIdx.x; i < (size_t)S * P; i += kPgThreads) a.table_out[i] = a.c.table[i];
-    if (a.refs_out != a.refs)
-        for (int p = threadIdx.x; p < N; p += kPgThreads) a.refs_out[p] = a.refs[p];
+    __shared__ PagesShared s;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int S = a.c.n_seqs, P = a.c.max_pages, N = a.c.n_pages, lg = a.c.ps_log2, up = (1 << lg) - 1, lane = threadIdx.x & 31;
+    const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
+    if (threadIdx.x == 0) s.bad = s.full = s.odd = 0;
+    if (a.table_out != a.c.table) copy_ints(a.table_out, a.c.table, (size_t)S * P, thread, threads);
+    if (a.refs_out != a.refs) copy_ints(a.refs_out, a.refs, N, thread, threads);
     __syncthreads();
+    // every CTA: how many pages the sequences want
+    for (int i = threadIdx.x; i < S; i += kPgThreads) {
+        const int len = a.c.lens[i], n = a.n_new[i], cap = P << lg;
+        int want = 0;
+        if (len < 0 || len > cap || n < 0) s.bad = 1;
+        else if (n > cap - len) s.full = 1;
+        else want = ((len + n + up) >> lg) - ((len + up) >> lg);
+        s.prefix[i] = want;
+    }
+    __syncthreads();
+    const int want = scan_shared(s.prefix, S, s.part);
+    cluster.sync();  // (the copies)
     // pages that no query needs any longer: a warp per sequence, from the window's first page backwards to the first that is gone
     if (a.window > 0)
-        for (int s = threadIdx.x >> 5; s < S; s += kPgThreads / 32) {
-            const int64_t past = (int64_t)a.c.lens[s] - a.window + 1;
-            const int lo = (a.sinks + (1 << lg) - 1) >> lg;
+        for (int i = thread >> 5; i < S; i += threads / 32) {
+            const int64_t past = (int64_t)a.c.lens[i] - a.window + 1;
+            const int lo = (int)(((int64_t)a.sinks + up) >> lg);
             int hi = past <= 0 ? 0 : (int)min(past >> lg, (int64_t)P);
-            int32_t *row = a.table_out + (size_t)s * P;
+            int32_t *row = a.table_out + (size_t)i * P;
             while (hi > lo) {
-                const int j = hi - 1 - lane, page = j >= lo ? row[j] : -1;
+                const int j = hi - 1 - lane, page = j >= lo ? __ldcg(row + j) : -1;
                 const unsigned gone = __ballot_sync(0xffffffffu, page < 0);
                 if (page >= 0 && (gone & ((1u << lane) - 1u)) == 0) {
                     row[j] = -1;
                     if (page < N) atomicSub(a.refs_out + page, 1);
-                    else s_bad = 1;
+                    else atomicExch(cluster.map_shared_rank(&s.odd, 0), 1);
                 }
                 if (gone) break;
                 hi -= 32;
             }
         }
-    for (int s = threadIdx.x; s < S; s += kPgThreads) {
-        const int len = a.c.lens[s], n = a.n_new[s], cap = P << lg;
-        int want = 0;
-        if (len < 0 || len > cap || n < 0) s_bad = 1;
-        else if (n > cap - len) s_full = 1;
-        else want = ((len + n + (1 << lg) - 1) >> lg) - ((len + (1 << lg) - 1) >> lg);
-        prefix[s] = want;
+    cluster.sync();
+    int code = s.bad || *cluster.map_shared_rank(&s.odd, 0) ? RIVER_E_BADARG : s.full ? RIVER_E_NOPAGE : RIVER_OK;
+    if (code == RIVER_OK && want > 0 &&
+        !lowest_free(a.refs_out, N, want, s, cluster, [&](int k, int p) {
+            const int i = owner_of(s.prefix, S, k);
+            a.table_out[(size_t)i * P + ((a.c.lens[i] + up) >> lg) + k - s.prefix[i]] = p;
+            a.refs_out[p] = 1;
+        }))
+        code = RIVER_E_NOPAGE;
+    cluster.sync();  // (lens_out may be lens; `odd` has been read)
+    for (int i = thread; i < S; i += threads) {
+        const int len = a.c.lens[i];
+        a.lens_out[i] = code == RIVER_OK ? len + a.n_new[i] : len;
     }
-    __syncthreads();
-    const int bad = s_bad, full = s_full, want = scan_shared(prefix, S, part);
-    int code = bad ? RIVER_E_BADARG : full ? RIVER_E_NOPAGE : RIVER_OK;
-    if (code == RIVER_OK) {
-        auto entry = [&](int k) {
-            const int s = owner_of(prefix, S, k);
-            return a.table_out + (size_t)s * P + ((a.c.lens[s] + (1 << lg) - 1) >> lg) + k - prefix[s];
-        };
-        const int got = lowest_free(a.refs_out, N, want, part, [&](int k, int p) { *entry(k) = p; });
-        for (int k = threadIdx.x; k < got; k += kPgThreads) {  // (behind the scan, which reads refs)
-            if (got == want) a.refs_out[*entry(k)] = 1;
-            else *entry(k) = -1;
-        }
-        if (got < want) code = RIVER_E_NOPAGE;
-    }
-    __syncthreads();
-    for (int s = threadIdx.x; s < S; s += kPgThreads) {
-        const int len = a.c.lens[s];
-        a.lens_out[s] = code == RIVER_OK ? len + a.n_new[s] : len;
-    }
-    if (threadIdx.x == 0) *a.status = code;
+    if (thread == 0) *a.status = code;
 }
 
 __global__ void __launch_bounds__(kPgThreads) pages_reorder_kernel(const PagesArgs a) {
-    __shared__ int part[33], s_bad, elder[kPgSeqs];  // elder: the lowest child of a parent, then prefix sums of the copies
-    const int S = a.c.n_seqs, P = a.c.max_pages, N = a.c.n_pages, lg = a.c.ps_log2, ps = 1 << lg;
-    if (threadIdx.x == 0) s_bad = 0;
-    for (int s = threadIdx.x; s < S; s += kPgThreads) elder[s] = S;
-    for (int p = threadIdx.x; p < N; p += kPgThreads) a.refs_out[p] = a.refs[p];
+    __shared__ PagesShared s;  // prefix: the lowest child of a parent, then prefix sums of the copies
+    cg::cluster_group cluster = cg::this_cluster();
+    const int S = a.c.n_seqs, P = a.c.max_pages, N = a.c.n_pages, lg = a.c.ps_log2, up = (1 << lg) - 1;
+    const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
+    pdl_launch();
+    if (threadIdx.x == 0) s.bad = s.odd = 0;
+    copy_ints(a.refs_out, a.refs, N, thread, threads);
+    for (int i = threadIdx.x; i < S; i += kPgThreads) s.prefix[i] = S;
     __syncthreads();
     for (int i = threadIdx.x; i < S; i += kPgThreads) {
         const int p = a.parents[i], len = a.c.lens[i];
-        if (p < -1 || p >= S || len < 0 || len > (P << lg)) s_bad = 1;
-        else if (p >= 0) atomicMin(&elder[p], i);
+        if (p < -1 || p >= S || len < 0 || len > (P << lg)) s.bad = 1;
+        else if (p >= 0) atomicMin(&s.prefix[p], i);
     }
-    __syncthreads();
-    int code = s_bad ? RIVER_E_BADARG : RIVER_OK;
+    cluster.sync();
+    int code = s.bad ? RIVER_E_BADARG : RIVER_OK;  // (the same in every CTA)
     if (code == RIVER_OK) {
-        // a sequence that copies its last page, filled in part
-        auto copies = [&](int i, int p) { return p >= 0 && (a.c.lens[p] & (ps - 1)) && elder[p] != i; };
-        for (size_t e = threadIdx.x; e < (size_t)S * P; e += kPgThreads) {
-            const int i = (int)(e / P), j = (int)(e % P), p = a.parents[i];
-            const int old = j < (a.c.lens[i] + ps - 1) >> lg ? a.c.table[e] : -1;
-            int page = -1;
-            if (p >= 0 && j < (a.c.lens[p] + ps - 1) >> lg) page = a.c.table[(size_t)p * P + j];
-            if (page >= N || old >= N) { s_bad = 1; continue; }
-            const bool own_copy = j == (p >= 0 ? a.c.lens[p] >> lg : -1) && copies(i, p);
-            if (own_copy) page = page < 0 ? -1 : -2 - page;  // (the page to copy from, until its copy has an id)
-            a.table_out[e] = page;
-            if (page == old) continue;  // (a sequence that goes on as it was)
-            if (page >= 0) atomicAdd(a.refs_out + page, 1);
-            if (old >= 0) atomicSub(a.refs_out + old, 1);
+        // a warp per sequence
+        for (int i = thread >> 5; i < S; i += threads / 32) {
+            const int p = a.parents[i], old_n = (a.c.lens[i] + up) >> lg, len = p >= 0 ? a.c.lens[p] : 0, n = (len + up) >> lg;
+            const int copied = p >= 0 && (len & up) && s.prefix[p] != i ? len >> lg : -1;  // the last page, where another child keeps it
+            const int32_t *old_row = a.c.table + (size_t)i * P, *row = a.c.table + (size_t)max(p, 0) * P;
+            int32_t *to = a.table_out + (size_t)i * P;
+            for (int j = threadIdx.x & 31; j < P; j += 32) {
+                const int old = j < old_n ? old_row[j] : -1;
+                int page = j < n ? row[j] : -1;
+                if (page >= N || old >= N) {
+                    atomicExch(cluster.map_shared_rank(&s.odd, 0), 1);
+                    continue;
+                }
+                if (j == copied) page = page < 0 ? -1 : -2 - page;  // (the page to copy from, until its copy has an id)
+                to[j] = page;
+                if (page == old) continue;  // (a sequence that goes on as it was)
+                if (page >= 0) atomicAdd(a.refs_out + page, 1);
+                if (old >= 0) atomicSub(a.refs_out + old, 1);
+            }
         }
-        __syncthreads();
-        code = s_bad ? RIVER_E_BADARG : RIVER_OK;
-        __syncthreads();
+        cluster.sync();
+        code = *cluster.map_shared_rank(&s.odd, 0) ? RIVER_E_BADARG : RIVER_OK;
+        // every CTA: who copies
         for (int i = threadIdx.x; i < S; i += kPgThreads) {
             const int p = a.parents[i];
-            elder[i] = p >= 0 && (a.c.lens[p] & (ps - 1)) && a.table_out[(size_t)i * P + (a.c.lens[p] >> lg)] < -1;
+            s.prefix[i] = code == RIVER_OK && p >= 0 && (a.c.lens[p] & up) && __ldcg(a.table_out + (size_t)i * P + (a.c.lens[p] >> lg)) < -1;
         }
         __syncthreads();
+        const int want = scan_shared(s.prefix, S, s.part);
+        cluster.sync();  // (the places of copies have been read, and `odd`)
+        if (code == RIVER_OK && want > 0 &&
+            !lowest_free(a.refs_out, N, want, s, cluster, [&](int k, int id) {
+                const int i = owner_of(s.prefix, S, k), p = a.parents[i];
+                int32_t *e = a.table_out + (size_t)i * P + (a.c.lens[p] >> lg), *l = a.list + 1 + 3 * k;
+                l[0] = -2 - __ldcg(e);
+                l[1] = id;
+                l[2] = a.c.lens[p] & up;
+                *e = id;
+                a.refs_out[id] = 1;
+            }))
+            code = RIVER_E_NOPAGE;
+        if (thread == 0) a.list[0] = code == RIVER_OK ? want : 0;
+    } else if (thread == 0) {
+        a.list[0] = 0;
     }
-    if (code == RIVER_OK) {
-        const int want = scan_shared(elder, S, part);
-        const int got = lowest_free(a.refs_out, N, want, part, [&](int k, int id) {
-            const int i = owner_of(elder, S, k), p = a.parents[i];
-            int32_t *e = a.table_out + (size_t)i * P + (a.c.lens[p] >> lg), *l = a.list + 1 + 3 * k;
-            l[0] = -2 - *e;
-            l[1] = id;
-            l[2] = a.c.lens[p] & (ps - 1);
-            *e = id;
-        });
-        for (int k = threadIdx.x; k < got; k += kPgThreads) a.refs_out[a.list[2 + 3 * k]] = 1;
-        if (threadIdx.x == 0) a.list[0] = got == want ? got : 0;
-        if (got < want) code = RIVER_E_NOPAGE;
+    if (code != RIVER_OK) {  // the state as it was
+        cluster.sync();
+        copy_ints(a.table_out, a.c.table, (size_t)S * P, thread, threads);
+        copy_ints(a.refs_out, a.refs, N, thread, threads);
     }
-    if (code != RIVER_OK) {
-        __syncthreads();
-        for (size_t e = threadIdx.x; e < (size_t)S * P; e += kPgThreads) a.table_out[e] = a.c.table[e];
-        for (int p = threadIdx.x; p < N; p += kPgThreads) a.refs_out[p] = a.refs[p];
-        if (threadIdx.x == 0) a.list[0] = 0;
-    }
-    for (int i = threadIdx.x; i < S; i += kPgThreads) {
+    for (int i = thread; i < S; i += threads) {
         const int p = a.parents[i];
         a.lens_out[i] = code != RIVER_OK ? a.c.lens[i] : p >= 0 ? a.c.lens[p] : 0;
     }
-    if (threadIdx.x == 0) *a.status = code;
+    if (thread == 0) *a.status = code;
+    cluster.sync();  // (nobody leaves while its shared memory may be read)
 }
 
 __global__ void __launch_bounds__(kPgThreads) pages_compact_kernel(const PagesArgs a) {
-    __shared__ int part[33];
-    const int N = a.c.n_pages;
+    __shared__ PagesShared s;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int N = a.c.n_pages, rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
+    const Ids ids(N, rank, ctas);
     int32_t *to = a.list + 1, *from = to + N / 2;
-    int used = 0;
-    for (int p0 = 0; p0 < N; p0 += kPgThreads) {
-        const int p = p0 + threadIdx.x;
-        int total;
-        cta_scan(p < N && a.refs[p] > 0, part, total);
-        used += total;
+    pdl_launch();
+    int mine = 0;
+    for_ids(ids, [&](int p, int n) {
+        int r[4], total;
+        load_refs(a.refs, p, n, r);
+        int c = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c += e < n && r[e] > 0;
+        cta_scan(c, s.part, total);
+        mine += total;
+    });
+    if (threadIdx.x == 0) s.count[0] = mine;
+    cluster.sync();
+    int used = 0, before = 0;  // pages in use; those of the ranges before
+    for (int c = 0; c < ctas; ++c) {
+        const int x = *cluster.map_shared_rank(&s.count[0], c);
+        if (c < rank) before += x;
+        used += x;
     }
-    int holes = 0, movers = 0;
-    for (int p0 = 0; p0 < N; p0 += kPgThreads) {
-        const int p = p0 + threadIdx.x, r = p < N ? a.refs[p] : 0;
-        const bool hole = p < used && r <= 0, mover = p >= used && r > 0;
-        int nh, nm;
-        const int h = cta_scan(hole, part, nh), m = cta_scan(mover, part, nm);
-        if (hole) to[holes + h] = p;
-        if (mover) from[movers + m] = p;
-        if (p < N) {
-            a.remap[p] = r > 0 ? p : -1;
-            if (a.refs_out != a.refs) a.refs_out[p] = r;
+    // Page p has u used ones before it: a hole below `used` is hole number p - u, a used page from there on mover number u - (used ones
+    // below `used`), which is u - (used - holes).  The holes are counted from the ids: used - (used ones below `used`).
+    __syncthreads();
+    for_ids(ids, [&](int p, int n) {
+        int r[4], total, c = 0;
+        load_refs(a.refs, p, n, r);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c += e < n && r[e] > 0;
+        int u = before + cta_scan(c, s.part, total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e >= n) continue;
+            const int q = p + e;
+            const bool in_use = r[e] > 0;
+            if (q < used && !in_use) to[q - u] = q;
+            // (movers are numbered from behind: the last used page is the last mover; how many there are is known at the end)
+            if (q >= used && in_use) from[N / 2 - (used - u)] = q;
+            a.remap[q] = in_use ? q : -1;
+            if (a.refs_out != a.refs) a.refs_out[q] = r[e];
+            u += in_use;
+            if (q == used - 1) *cluster.map_shared_rank(&s.count[1], 0) = used - u;  // holes
         }
-        holes += nh;
-        movers += nm;
+        before += total;
+    });
+    if (used == 0 && thread == 0) s.count[1] = 0;
+    cluster.sync();
+    const int moves = *cluster.map_shared_rank(&s.count[1], 0);
+    const int32_t *last = from + N / 2 - moves;  // the movers, ascending
+    for (int k = thread; k < moves; k += threads) {
+        const int f = __ldcg(last + k), t = __ldcg(to + k);
+        a.remap[f] = t;
+        a.refs_out[t] = __ldcg(a.refs + f);
     }
-    __syncthreads();
-    for (int k = threadIdx.x; k < movers; k += kPgThreads) {
-        a.remap[from[k]] = to[k];
-        a.refs_out[to[k]] = a.refs_out[from[k]];
-        a.refs_out[from[k]] = 0;
+    cluster.sync();
+    // the list's second part begins at its first place (a copy to itself where nothing is left over)
+    for (int k0 = 0; k0 < moves; k0 += threads) {
+        const int k = k0 + thread, f = k < moves ? __ldcg(last + k) : 0;
+        cluster.sync();
+        if (k < moves) {
+            from[k] = f;
+            a.refs_out[f] = 0;
+        }
+        cluster.sync();
     }
-    __syncthreads();
-    for (size_t e = threadIdx.x; e < (size_t)a.c.n_seqs * a.c.max_pages; e += kPgThreads) {
-        const int page = a.c.table[e];
-        a.table_out[e] = page >= 0 && page < N ? a.remap[page] : -1;
-    }
-    if (threadIdx.x == 0) { *a.n_used = used; a.list[0] = movers; }
+    if (thread == 0) { *a.n_used = used; a.list[0] = moves; }
 }
 
-// The values of the pages on the list, layer by layer.  triples: (from, to, positions) entries, of which the first `positions` of every
-// head move; else whole pages, to[] and from[] apart.
-__global__ void __launch_bounds__(256) pages_copy_kernel(const Paged c, const int32_t *list, int triples) {
-    const int n = list[0], heads = 2 * c.Hkv;
-    for (int u = blockIdx.x; u < n * c.n_layers; u += gridDim.x) {
-        const int k = u / c.n_layers, l = u % c.n_layers;
-        const int src = triples ? list[1 + 3 * k] : list[1 + c.n_pages / 2 + k], dst = triples ? list[2 + 3 * k] : list[1 + k];
-        const int fill = triples ? list[3 + 3 * k] : 1 << c.ps_log2, chunks = fill * (c.dh / 8);  // 16-byte chunks of a head
-        const uint4 *s = reinterpret_cast<const uint4 *>(c.pool) + c.row(l, src, 0, 0, 0) / 8;
-        uint4 *d = reinterpret_cast<uint4 *>(c.pool) + c.row(l, dst, 0, 0, 0) / 8;
-        for (int i = threadIdx.x; i < heads * chunks; i += blockDim.x) {
-            const int at = i / chunks * ((c.dh / 8) << c.ps_log2) + i % chunks;
-            d[at] = s[at];
+// The values of the pages on the list, a warp per (page, block, head): its filled positions are consecutive.  triples: (from, to, positions)
+// entries; else whole pages, to[] and from[] apart, and the table's entries follow `remap`.  Every warp has 4 KB under way.
+constexpr int kCopyCtas = 8;  // per SM
+__global__ void __launch_bounds__(256) pages_copy_kernel(const PagesArgs a, int triples) {
+    pdl_wait();
+    const int n = a.list[0], heads = 2 * a.c.Hkv, lane = threadIdx.x & 31, warps = gridDim.x * 8, L = a.c.n_layers, row16 = a.c.dh / 8;
+    uint4 *const pool = reinterpret_cast<uint4 *>(a.c.pool);
+    for (int64_t w = blockIdx.x * 8 + (threadIdx.x >> 5); w < (int64_t)n * L * heads; w += warps) {
+        const int head = (int)(w % heads), l = (int)(w / heads % L), k = (int)(w / heads / L);
+        const int src = triples ? a.list[1 + 3 * k] : a.list[1 + a.c.n_pages / 2 + k], dst = triples ? a.list[2 + 3 * k] : a.list[1 + k];
+        const int chunks = (triples ? a.list[3 + 3 * k] : 1 << a.c.ps_log2) * row16;
+        const uint4 *f = pool + a.c.row(l, src, 0, head, 0) / 8;  // (a page's heads of V follow those of K)
+        uint4 *t = pool + a.c.row(l, dst, 0, head, 0) / 8;
+        for (int c0 = lane; c0 < chunks; c0 += 8 * 32) {
+            uint4 v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c0 + 32 * e < chunks) v[e] = ldg_stream16(f + c0 + 32 * e);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c0 + 32 * e < chunks) t[c0 + 32 * e] = v[e];
         }
     }
+    if (triples) return;
+    const size_t entries = (size_t)a.c.n_seqs * a.c.max_pages;
+    for (size_t e = blockIdx.x * 256 + threadIdx.x; e < entries; e += (size_t)gridDim.x * 256) {
+        const int page = a.c.table[e];
+        a.table_out[e] = page >= 0 && page < a.c.n_pages ? a.remap[page] : -1;
+    }
+}
+
+template <class K>
+int launch_deciding(K kernel, const PagesArgs &a, size_t work, cudaStream_t st) {
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim = {work > 4 * kPgThreads ? (unsigned)kPgCtas : 1u, 1, 1};  // (a few thousand entries are one CTA's)
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(at.val.clusterDim.x);
+    cfg.blockDim = dim3(kPgThreads);
+    cfg.stream = st;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
+}
+// `most`: heads' worth of copies that there may be
+int launch_copy(const PagesArgs &a, int triples, int64_t most, cudaStream_t st) {
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;  // (its CTAs stand ready when the list is there)
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<int64_t>(148 * kCopyCtas, std::max<int64_t>(1, (most + 7) / 8)));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, pages_copy_kernel, a, triples) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
 }
 
 }  // namespace
@@ -287,8 +448,7 @@ extern "C" int river_pages_advance(const river_paged *c, const int32_t *refs, co
     a.lens_out = lens_out;
     a.refs_out = refs_out;
     a.status = status;
-    pages_advance_kernel<<<1, kPgThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
-    return launch_rc();
+    return launch_deciding(pages_advance_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, const int32_t *parents, int32_t *table_out, int32_t *lens_out,
@@ -306,9 +466,8 @@ extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, co
     a.list = copies;
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    pages_reorder_kernel<<<1, kPgThreads, 0, st>>>(a);
-    pages_copy_kernel<<<148 * 8, 256, 0, st>>>(a.c, copies, 1);
-    return launch_rc();
+    if (const int rc = launch_deciding(pages_reorder_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, st)) return rc;
+    return launch_copy(a, 1, (int64_t)std::min(c->n_seqs, c->n_pages) * c->n_layers * 2 * c->Hkv, st);
 }
 
 extern "C" int river_pages_compact(const river_paged *c, const int32_t *refs, int32_t *table_out, int32_t *refs_out, int32_t *remap,
@@ -323,7 +482,6 @@ extern "C" int river_pages_compact(const river_paged *c, const int32_t *refs, in
     a.n_used = n_used;
     a.list = moves;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    pages_compact_kernel<<<1, kPgThreads, 0, st>>>(a);
-    pages_copy_kernel<<<148 * 8, 256, 0, st>>>(a.c, moves, 0);
-    return launch_rc();
+    if (const int rc = launch_deciding(pages_compact_kernel, a, c->n_pages, st)) return rc;
+    return launch_copy(a, 0, (int64_t)c->n_pages / 2 * c->n_layers * 2 * c->Hkv + (int64_t)c->n_seqs * c->max_pages / 32, st);
 }
