@@ -34,6 +34,9 @@ struct PagesShared {
     int odd;        // a page out of range: the first CTA's tells, behind a barrier of the cluster
     int prefix[kPgSeqs];
 };
+struct ReorderShared : PagesShared {  // prefix: the lowest child of a parent
+    int start[kPgSeqs];  // copies before a sequence's own
+};
 
 // Exclusive prefix sum over the CTA's threads (`part`: 33 ints); `total` gets the sum.  Ends with a barrier behind every read.
 __device__ __forceinline__ int cta_scan(int x, int *part, int &total) {
@@ -77,64 +80,62 @@ __device__ int scan_shared(int *s, int n, int *part) {
     return base;
 }
 
-// The cluster's view of the page ids: this CTA's range, in runs of four per thread.
-struct Ids {
+// The page ids of a thread: a range per CTA, in it a run of whole fours per thread.
+struct Run {
     int lo, hi;
-    __device__ __forceinline__ Ids(int n, int rank, int ctas) {
-        const int per = ((n + ctas - 1) / ctas + 3) & ~3;
-        lo = min(n, rank * per);
+    __device__ __forceinline__ Run(int n, int rank, int ctas) {
+        const int per = (int)(((int64_t)n + (int64_t)ctas * kPgThreads - 1) / ((int64_t)ctas * kPgThreads) + 3) & ~3;
+        lo = (int)min((int64_t)n, ((int64_t)rank * kPgThreads + threadIdx.x) * per);
         hi = min(n, lo + per);
     }
-};
-// f(ids of a thread's run, of which `n` are in range) for the range's ids in ascending order over the threads; every thread takes part in
-// every round.
-template <class F>
-__device__ __forceinline__ void for_ids(const Ids &ids, F f) {
-    for (int p0 = ids.lo; p0 < ids.hi; p0 += 4 * kPgThreads) {
-        const int p = p0 + 4 * threadIdx.x;
-        f(p, max(0, min(4, ids.hi - p)));
+    // f(id, refs of it) in ascending order
+    template <class F>
+    __device__ __forceinline__ void each(const int32_t *refs, F f) const {
+        if ((reinterpret_cast<uintptr_t>(refs) & 15) == 0) {
+            for (int p = lo; p + 4 <= hi; p += 4) {
+                const int4 r = __ldcg(reinterpret_cast<const int4 *>(refs + p));
+                f(p, r.x); f(p + 1, r.y); f(p + 2, r.z); f(p + 3, r.w);
+            }
+            for (int p = lo + ((hi - lo) & ~3); p < hi; ++p) f(p, __ldcg(refs + p));
+        } else {
+            for (int p = lo; p < hi; ++p) f(p, __ldcg(refs + p));
+        }
     }
-}
-__device__ __forceinline__ void load_refs(const int32_t *refs, int p, int n, int (&r)[4]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = e < n ? __ldcg(refs + p + e) : 0x7fffffff;
-}
-
-// give(k, id) for the `want` lowest ids with refs 0, ascending, if there are as many; returns whether there are.  All CTAs of the cluster.
-template <class F>
-__device__ bool lowest_free(const int32_t *refs, int n_pages, int want, PagesShared &s, cg::cluster_group &cluster, F give) {
+};
+// Of the ids that `mine` counts per thread: how many there are before this thread's, and (all) in the whole cluster.  All threads.
+__device__ __forceinline__ int cluster_scan(int mine, PagesShared &s, cg::cluster_group &cluster, int &all) {
     const int rank = cluster.block_rank(), ctas = cluster.num_blocks();
-    const Ids ids(n_pages, rank, ctas);
-    int mine = 0;
-    for_ids(ids, [&](int p, int n) {
-        int r[4], total;
-        load_refs(refs, p, n, r);
-        cta_scan((r[0] == 0) + (r[1] == 0) + (r[2] == 0) + (r[3] == 0), s.part, total);
-        mine += total;
-    });
-    if (threadIdx.x == 0) s.count[0] = mine;
+    int total;
+    int before = cta_scan(mine, s.part, total);
+    all = total;
+    if (ctas == 1) return before;
+    if (threadIdx.x == 0) s.count[0] = total;
     cluster.sync();
-    int before = 0, all = 0;
+    all = 0;
     for (int c = 0; c < ctas; ++c) {
         const int x = *cluster.map_shared_rank(&s.count[0], c);
         if (c < rank) before += x;
         all += x;
     }
     cluster.sync();  // (counts have been read)
+    return before;
+}
+
+// give(k, id) for the `want` lowest ids with refs 0, ascending, if there are as many; returns whether there are.  All threads of the cluster.
+template <class F>
+__device__ bool lowest_free(const int32_t *refs, int n_pages, int want, PagesShared &s, cg::cluster_group &cluster, F give) {
+    const Run run(n_pages, cluster.block_rank(), cluster.num_blocks());
+    int mine = 0, all;
+    run.each(refs, [&](int, int r) { mine += r == 0; });
+    int k = cluster_scan(mine, s, cluster, all);
     if (all < want) return false;
-    for_ids(ids, [&](int p, int n) {
-        if (before >= want) return;  // (uniform)
-        int r[4], total;
-        load_refs(refs, p, n, r);
-        int k = before + cta_scan((r[0] == 0) + (r[1] == 0) + (r[2] == 0) + (r[3] == 0), s.part, total);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (r[e] == 0) {
-                if (k < want) give(k, p + e);
+    if (mine > 0 && k < want)
+        run.each(refs, [&](int p, int r) {
+            if (r == 0) {
+                if (k < want) give(k, p);
                 ++k;
             }
-        before += total;
-    });
+        });
     return true;
 }
 // the last i < n with prefix[i] <= k (prefix[0] = 0): whose want number k is
@@ -224,7 +225,8 @@ __global__ void __launch_bounds__(kPgThreads) pages_advance_kernel(const PagesAr
 }
 
 __global__ void __launch_bounds__(kPgThreads) pages_reorder_kernel(const PagesArgs a) {
-    __shared__ PagesShared s;  // prefix: the lowest child of a parent, then prefix sums of the copies
+    extern __shared__ int pg_raw[];  // (over the 48 KB that a kernel may have by itself)
+    ReorderShared &s = *reinterpret_cast<ReorderShared *>(pg_raw);
     cg::cluster_group cluster = cg::this_cluster();
     const int S = a.c.n_seqs, P = a.c.max_pages, N = a.c.n_pages, lg = a.c.ps_log2, up = (1 << lg) - 1;
     const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
@@ -241,10 +243,17 @@ __global__ void __launch_bounds__(kPgThreads) pages_reorder_kernel(const PagesAr
     cluster.sync();
     int code = s.bad ? RIVER_E_BADARG : RIVER_OK;  // (the same in every CTA)
     if (code == RIVER_OK) {
+        // The page that sequence i copies: its parent's last one, filled in part, where another child keeps it (-1: none).
+        auto copied = [&](int i, int p, int &at) {
+            const int len = p >= 0 ? a.c.lens[p] : 0;
+            at = len >> lg;
+            return p >= 0 && (len & up) && s.prefix[p] != i ? a.c.table[(size_t)p * P + at] : -1;
+        };
         // a warp per sequence
         for (int i = thread >> 5; i < S; i += threads / 32) {
-            const int p = a.parents[i], old_n = (a.c.lens[i] + up) >> lg, len = p >= 0 ? a.c.lens[p] : 0, n = (len + up) >> lg;
-            const int copied = p >= 0 && (len & up) && s.prefix[p] != i ? len >> lg : -1;  // the last page, where another child keeps it
+            const int p = a.parents[i], old_n = (a.c.lens[i] + up) >> lg, n = ((p >= 0 ? a.c.lens[p] : 0) + up) >> lg;
+            int at;
+            if (copied(i, p, at) < 0) at = -1;
             const int32_t *old_row = a.c.table + (size_t)i * P, *row = a.c.table + (size_t)max(p, 0) * P;
             int32_t *to = a.table_out + (size_t)i * P;
             for (int j = threadIdx.x & 31; j < P; j += 32) {
@@ -254,31 +263,33 @@ __global__ void __launch_bounds__(kPgThreads) pages_reorder_kernel(const PagesAr
                     atomicExch(cluster.map_shared_rank(&s.odd, 0), 1);
                     continue;
                 }
-                if (j == copied) page = page < 0 ? -1 : -2 - page;  // (the page to copy from, until its copy has an id)
+                if (j == at) page = -1;  // (until the copy has an id)
                 to[j] = page;
                 if (page == old) continue;  // (a sequence that goes on as it was)
                 if (page >= 0) atomicAdd(a.refs_out + page, 1);
                 if (old >= 0) atomicSub(a.refs_out + old, 1);
             }
         }
+        // every CTA: the copies before a sequence's (the lowest children give way to them)
+        int want = 0;
+        for (int i0 = 0; i0 < S; i0 += kPgThreads) {
+            const int i = i0 + threadIdx.x;
+            int at, total;
+            const int before = cta_scan(i < S && copied(i, a.parents[i], at) >= 0, s.part, total);
+            if (i < S) s.start[i] = want + before;
+            want += total;
+        }
         cluster.sync();
         code = *cluster.map_shared_rank(&s.odd, 0) ? RIVER_E_BADARG : RIVER_OK;
-        // every CTA: who copies
-        for (int i = threadIdx.x; i < S; i += kPgThreads) {
-            const int p = a.parents[i];
-            s.prefix[i] = code == RIVER_OK && p >= 0 && (a.c.lens[p] & up) && __ldcg(a.table_out + (size_t)i * P + (a.c.lens[p] >> lg)) < -1;
-        }
-        __syncthreads();
-        const int want = scan_shared(s.prefix, S, s.part);
-        cluster.sync();  // (the places of copies have been read, and `odd`)
         if (code == RIVER_OK && want > 0 &&
             !lowest_free(a.refs_out, N, want, s, cluster, [&](int k, int id) {
-                const int i = owner_of(s.prefix, S, k), p = a.parents[i];
-                int32_t *e = a.table_out + (size_t)i * P + (a.c.lens[p] >> lg), *l = a.list + 1 + 3 * k;
-                l[0] = -2 - __ldcg(e);
+                const int i = owner_of(s.start, S, k), p = a.parents[i];
+                int at;
+                int32_t *l = a.list + 1 + 3 * k;
+                l[0] = copied(i, p, at);
                 l[1] = id;
                 l[2] = a.c.lens[p] & up;
-                *e = id;
+                a.table_out[(size_t)i * P + at] = id;
                 a.refs_out[id] = 1;
             }))
             code = RIVER_E_NOPAGE;
@@ -303,50 +314,22 @@ __global__ void __launch_bounds__(kPgThreads) pages_compact_kernel(const PagesAr
     __shared__ PagesShared s;
     cg::cluster_group cluster = cg::this_cluster();
     const int N = a.c.n_pages, rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
-    const Ids ids(N, rank, ctas);
+    const Run run(N, rank, ctas);
     int32_t *to = a.list + 1, *from = to + N / 2;
     pdl_launch();
-    int mine = 0;
-    for_ids(ids, [&](int p, int n) {
-        int r[4], total;
-        load_refs(a.refs, p, n, r);
-        int c = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c += e < n && r[e] > 0;
-        cta_scan(c, s.part, total);
-        mine += total;
-    });
-    if (threadIdx.x == 0) s.count[0] = mine;
-    cluster.sync();
-    int used = 0, before = 0;  // pages in use; those of the ranges before
-    for (int c = 0; c < ctas; ++c) {
-        const int x = *cluster.map_shared_rank(&s.count[0], c);
-        if (c < rank) before += x;
-        used += x;
-    }
-    // Page p has u used ones before it: a hole below `used` is hole number p - u, a used page from there on mover number u - (used ones
-    // below `used`), which is u - (used - holes).  The holes are counted from the ids: used - (used ones below `used`).
-    __syncthreads();
-    for_ids(ids, [&](int p, int n) {
-        int r[4], total, c = 0;
-        load_refs(a.refs, p, n, r);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c += e < n && r[e] > 0;
-        int u = before + cta_scan(c, s.part, total);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (e >= n) continue;
-            const int q = p + e;
-            const bool in_use = r[e] > 0;
-            if (q < used && !in_use) to[q - u] = q;
-            // (movers are numbered from behind: the last used page is the last mover; how many there are is known at the end)
-            if (q >= used && in_use) from[N / 2 - (used - u)] = q;
-            a.remap[q] = in_use ? q : -1;
-            if (a.refs_out != a.refs) a.refs_out[q] = r[e];
-            u += in_use;
-            if (q == used - 1) *cluster.map_shared_rank(&s.count[1], 0) = used - u;  // holes
-        }
-        before += total;
+    int mine = 0, used;
+    run.each(a.refs, [&](int, int r) { mine += r > 0; });
+    int u = cluster_scan(mine, s, cluster, used);
+    // Page q has u used ones before it.  Below `used` a page that is free is hole number q - u; from there on the used ones are the movers,
+    // numbered from behind for now: how many they are is known when page used - 1 has been seen.
+    run.each(a.refs, [&](int q, int r) {
+        const bool in_use = r > 0;
+        if (q < used && !in_use) to[q - u] = q;
+        if (q >= used && in_use) from[N / 2 - (used - u)] = q;
+        a.remap[q] = in_use ? q : -1;
+        if (a.refs_out != a.refs) a.refs_out[q] = r;
+        u += in_use;
+        if (q == used - 1) *cluster.map_shared_rank(&s.count[1], 0) = used - u;
     });
     if (used == 0 && thread == 0) s.count[1] = 0;
     cluster.sync();
@@ -373,7 +356,7 @@ __global__ void __launch_bounds__(kPgThreads) pages_compact_kernel(const PagesAr
 
 // The values of the pages on the list, a warp per (page, block, head): its filled positions are consecutive.  triples: (from, to, positions)
 // entries; else whole pages, to[] and from[] apart, and the table's entries follow `remap`.  Every warp has 4 KB under way.
-constexpr int kCopyCtas = 8;  // per SM
+constexpr int kCopyCtas = 64;  // of the grid, per SM (8 are resident; grids of 8, 32 and 64 take 330, 312, 309 us for 2 GB)
 __global__ void __launch_bounds__(256) pages_copy_kernel(const PagesArgs a, int triples) {
     pdl_wait();
     const int n = a.list[0], heads = 2 * a.c.Hkv, lane = threadIdx.x & 31, warps = gridDim.x * 8, L = a.c.n_layers, row16 = a.c.dh / 8;
@@ -402,14 +385,20 @@ __global__ void __launch_bounds__(256) pages_copy_kernel(const PagesArgs a, int 
     }
 }
 
+// work: table entries and page ids.  A few thousand are one CTA's; from 2^18 on twice the portable cluster pays (256 sequences of 2048
+// pages, 65536 ids: 24 -> 17 us).
 template <class K>
-int launch_deciding(K kernel, const PagesArgs &a, size_t work, cudaStream_t st) {
+int launch_deciding(K kernel, const PagesArgs &a, size_t work, size_t smem, cudaStream_t st) {
+    const unsigned ctas = work <= 4 * kPgThreads ? 1 : work < (1u << 18) ? kPgCtas : 2 * kPgCtas;
+    if (ctas > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return RIVER_E_DEVICE;
+    if (smem && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return RIVER_E_DEVICE;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim = {work > 4 * kPgThreads ? (unsigned)kPgCtas : 1u, 1, 1};  // (a few thousand entries are one CTA's)
+    at.val.clusterDim = {ctas, 1, 1};
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(at.val.clusterDim.x);
+    cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(kPgThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
@@ -448,7 +437,7 @@ extern "C" int river_pages_advance(const river_paged *c, const int32_t *refs, co
     a.lens_out = lens_out;
     a.refs_out = refs_out;
     a.status = status;
-    return launch_deciding(pages_advance_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, static_cast<cudaStream_t>(cuda_stream));
+    return launch_deciding(pages_advance_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, 0, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, const int32_t *parents, int32_t *table_out, int32_t *lens_out,
@@ -466,7 +455,7 @@ extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, co
     a.list = copies;
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (const int rc = launch_deciding(pages_reorder_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, st)) return rc;
+    if (const int rc = launch_deciding(pages_reorder_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, sizeof(ReorderShared), st)) return rc;
     return launch_copy(a, 1, (int64_t)std::min(c->n_seqs, c->n_pages) * c->n_layers * 2 * c->Hkv, st);
 }
 
@@ -482,6 +471,6 @@ extern "C" int river_pages_compact(const river_paged *c, const int32_t *refs, in
     a.n_used = n_used;
     a.list = moves;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (const int rc = launch_deciding(pages_compact_kernel, a, c->n_pages, st)) return rc;
+    if (const int rc = launch_deciding(pages_compact_kernel, a, c->n_pages, 0, st)) return rc;
     return launch_copy(a, 0, (int64_t)c->n_pages / 2 * c->n_layers * 2 * c->Hkv + (int64_t)c->n_seqs * c->max_pages / 32, st);
 }
