@@ -28,14 +28,13 @@ struct PagesArgs {
 };
 
 // Shared memory of a deciding CTA; `count` is read and the first one's `odd` written by the other CTAs of the cluster.
-struct PagesShared {
+struct PagesScan {
     int part[33], count[2];
     int bad, full;  // what every CTA finds for itself: a sequence or length out of range, a row too long
     int odd;        // a page out of range: the first CTA's tells, behind a barrier of the cluster
-    int prefix[kPgSeqs];
 };
-struct ReorderShared : PagesShared {  // prefix: the lowest child of a parent
-    int start[kPgSeqs];  // copies before a sequence's own
+struct PagesShared : PagesScan {
+    int prefix[kPgSeqs];
 };
 
 // Exclusive prefix sum over the CTA's threads (`part`: 33 ints); `total` gets the sum.  Ends with a barrier behind every read.
@@ -103,7 +102,7 @@ struct Run {
     }
 };
 // Of the ids that `mine` counts per thread: how many there are before this thread's, and (all) in the whole cluster.  All threads.
-__device__ __forceinline__ int cluster_scan(int mine, PagesShared &s, cg::cluster_group &cluster, int &all) {
+__device__ __forceinline__ int cluster_scan(int mine, PagesScan &s, cg::cluster_group &cluster, int &all) {
     const int rank = cluster.block_rank(), ctas = cluster.num_blocks();
     int total;
     int before = cta_scan(mine, s.part, total);
@@ -123,7 +122,7 @@ __device__ __forceinline__ int cluster_scan(int mine, PagesShared &s, cg::cluste
 
 // give(k, id) for the `want` lowest ids with refs 0, ascending, if there are as many; returns whether there are.  All threads of the cluster.
 template <class F>
-__device__ bool lowest_free(const int32_t *refs, int n_pages, int want, PagesShared &s, cg::cluster_group &cluster, F give) {
+__device__ bool lowest_free(const int32_t *refs, int n_pages, int want, PagesScan &s, cg::cluster_group &cluster, F give) {
     const Run run(n_pages, cluster.block_rank(), cluster.num_blocks());
     int mine = 0, all;
     run.each(refs, [&](int, int r) { mine += r == 0; });
@@ -225,35 +224,47 @@ __global__ void __launch_bounds__(kPgThreads) pages_advance_kernel(const PagesAr
 }
 
 __global__ void __launch_bounds__(kPgThreads) pages_reorder_kernel(const PagesArgs a) {
-    extern __shared__ int pg_raw[];  // (over the 48 KB that a kernel may have by itself)
-    ReorderShared &s = *reinterpret_cast<ReorderShared *>(pg_raw);
+    extern __shared__ int pg_raw[];
+    __shared__ PagesScan s;
     cg::cluster_group cluster = cg::this_cluster();
     const int S = a.c.n_seqs, P = a.c.max_pages, N = a.c.n_pages, lg = a.c.ps_log2, up = (1 << lg) - 1;
     const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
+    // every CTA for itself: parents, lengths, the lowest child of a parent, the page that a sequence copies (-1: none), copies before its own
+    int *const parent = pg_raw, *const len = parent + S, *const elder = len + S, *const src = elder + S, *const start = src + S;
     pdl_launch();
     if (threadIdx.x == 0) s.bad = s.odd = 0;
     copy_ints(a.refs_out, a.refs, N, thread, threads);
-    for (int i = threadIdx.x; i < S; i += kPgThreads) s.prefix[i] = S;
+    for (int i = threadIdx.x; i < S; i += kPgThreads) {
+        parent[i] = a.parents[i];
+        len[i] = a.c.lens[i];
+        elder[i] = S;
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < S; i += kPgThreads) {
-        const int p = a.parents[i], len = a.c.lens[i];
-        if (p < -1 || p >= S || len < 0 || len > (P << lg)) s.bad = 1;
-        else if (p >= 0) atomicMin(&s.prefix[p], i);
+        const int p = parent[i], n = len[i];
+        if (p < -1 || p >= S || n < 0 || n > (P << lg)) s.bad = 1;
+        else if (p >= 0) atomicMin(&elder[p], i);
     }
-    cluster.sync();
+    __syncthreads();
     int code = s.bad ? RIVER_E_BADARG : RIVER_OK;  // (the same in every CTA)
+    int want = 0;
+    if (code == RIVER_OK)
+        for (int i0 = 0; i0 < S; i0 += kPgThreads) {
+            const int i = i0 + threadIdx.x, p = i < S ? parent[i] : -1;
+            int page = -1, total;
+            if (p >= 0 && (len[p] & up) && elder[p] != i) page = a.c.table[(size_t)p * P + (len[p] >> lg)];  // the last page, another child keeps it
+            const int before = cta_scan(page >= 0, s.part, total);
+            if (i < S) {
+                src[i] = page;
+                start[i] = want + before;
+            }
+            want += total;
+        }
+    cluster.sync();  // (refs are copied)
     if (code == RIVER_OK) {
-        // The page that sequence i copies: its parent's last one, filled in part, where another child keeps it (-1: none).
-        auto copied = [&](int i, int p, int &at) {
-            const int len = p >= 0 ? a.c.lens[p] : 0;
-            at = len >> lg;
-            return p >= 0 && (len & up) && s.prefix[p] != i ? a.c.table[(size_t)p * P + at] : -1;
-        };
         // a warp per sequence
         for (int i = thread >> 5; i < S; i += threads / 32) {
-            const int p = a.parents[i], old_n = (a.c.lens[i] + up) >> lg, n = ((p >= 0 ? a.c.lens[p] : 0) + up) >> lg;
-            int at;
-            if (copied(i, p, at) < 0) at = -1;
+            const int p = parent[i], old_n = (len[i] + up) >> lg, n = ((p >= 0 ? len[p] : 0) + up) >> lg, at = src[i] >= 0 ? len[p] >> lg : -1;
             const int32_t *old_row = a.c.table + (size_t)i * P, *row = a.c.table + (size_t)max(p, 0) * P;
             int32_t *to = a.table_out + (size_t)i * P;
             for (int j = threadIdx.x & 31; j < P; j += 32) {
@@ -270,26 +281,16 @@ __global__ void __launch_bounds__(kPgThreads) pages_reorder_kernel(const PagesAr
                 if (old >= 0) atomicSub(a.refs_out + old, 1);
             }
         }
-        // every CTA: the copies before a sequence's (the lowest children give way to them)
-        int want = 0;
-        for (int i0 = 0; i0 < S; i0 += kPgThreads) {
-            const int i = i0 + threadIdx.x;
-            int at, total;
-            const int before = cta_scan(i < S && copied(i, a.parents[i], at) >= 0, s.part, total);
-            if (i < S) s.start[i] = want + before;
-            want += total;
-        }
         cluster.sync();
         code = *cluster.map_shared_rank(&s.odd, 0) ? RIVER_E_BADARG : RIVER_OK;
         if (code == RIVER_OK && want > 0 &&
             !lowest_free(a.refs_out, N, want, s, cluster, [&](int k, int id) {
-                const int i = owner_of(s.start, S, k), p = a.parents[i];
-                int at;
+                const int i = owner_of(start, S, k), n = len[parent[i]];
                 int32_t *l = a.list + 1 + 3 * k;
-                l[0] = copied(i, p, at);
+                l[0] = src[i];
                 l[1] = id;
-                l[2] = a.c.lens[p] & up;
-                a.table_out[(size_t)i * P + at] = id;
+                l[2] = n & up;
+                a.table_out[(size_t)i * P + (n >> lg)] = id;
                 a.refs_out[id] = 1;
             }))
             code = RIVER_E_NOPAGE;
@@ -303,15 +304,15 @@ __global__ void __launch_bounds__(kPgThreads) pages_reorder_kernel(const PagesAr
         copy_ints(a.refs_out, a.refs, N, thread, threads);
     }
     for (int i = thread; i < S; i += threads) {
-        const int p = a.parents[i];
-        a.lens_out[i] = code != RIVER_OK ? a.c.lens[i] : p >= 0 ? a.c.lens[p] : 0;
+        const int p = parent[i];
+        a.lens_out[i] = code != RIVER_OK ? len[i] : p >= 0 ? len[p] : 0;
     }
     if (thread == 0) *a.status = code;
     cluster.sync();  // (nobody leaves while its shared memory may be read)
 }
 
 __global__ void __launch_bounds__(kPgThreads) pages_compact_kernel(const PagesArgs a) {
-    __shared__ PagesShared s;
+    __shared__ PagesScan s;
     cg::cluster_group cluster = cg::this_cluster();
     const int N = a.c.n_pages, rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
     const Run run(N, rank, ctas);
@@ -391,7 +392,7 @@ template <class K>
 int launch_deciding(K kernel, const PagesArgs &a, size_t work, size_t smem, cudaStream_t st) {
     const unsigned ctas = work <= 4 * kPgThreads ? 1 : work < (1u << 18) ? kPgCtas : 2 * kPgCtas;
     if (ctas > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return RIVER_E_DEVICE;
-    if (smem && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return RIVER_E_DEVICE;
+    if (smem > (32u << 10) && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return RIVER_E_DEVICE;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim = {ctas, 1, 1};
@@ -455,7 +456,7 @@ extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, co
     a.list = copies;
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (const int rc = launch_deciding(pages_reorder_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, sizeof(ReorderShared), st)) return rc;
+    if (const int rc = launch_deciding(pages_reorder_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, 5 * sizeof(int) * (size_t)c->n_seqs, st)) return rc;
     return launch_copy(a, 1, (int64_t)std::min(c->n_seqs, c->n_pages) * c->n_layers * 2 * c->Hkv, st);
 }
 

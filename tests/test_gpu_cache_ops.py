@@ -326,7 +326,7 @@ def state(rng, seqs, width, page, n_pages, shared=True):
     return table, lens, refs
 
 
-@pytest.mark.parametrize("seqs,width,page,n_pages", [(1, 1, 16, 1), (1, 5, 16, 9), (3, 40, 16, 90), (7, 33, 32, 200), (64, 20, 64, 1500), (300, 70, 16, 9000), (1100, 9, 16, 5000), (2, 900, 16, 70000)])
+@pytest.mark.parametrize("seqs,width,page,n_pages", [(1, 1, 16, 1), (1, 5, 16, 9), (3, 40, 16, 90), (7, 33, 32, 200), (64, 20, 64, 1500), (300, 70, 16, 9000), (1100, 9, 16, 5000), (2, 900, 16, 70000), (8192, 3, 16, 9000), (3, 7, 16, 700001)])
 def test_pages_advance(seqs, width, page, n_pages):
     rng = random.Random(seqs * width)
     for window, sinks in ((0, 0), (1, 0), (page, 1), (3 * page + 5, page + 1), (10 ** 9, 4)):
@@ -359,7 +359,7 @@ def test_pages_advance_says_when_there_are_too_few_pages():
 
 
 @pytest.mark.parametrize("seqs,width,page,n_pages,layers,hkv,dh,dtype", [
-    (1, 3, 16, 4, 1, 1, 64, BF), (4, 12, 16, 90, 3, 2, 64, BF), (9, 7, 32, 120, 2, 1, 128, F16), (65, 9, 16, 900, 2, 8, 128, BF), (40, 4, 64, 300, 1, 3, 64, F16), (1500, 3, 16, 7000, 1, 1, 64, BF)])
+    (1, 3, 16, 4, 1, 1, 64, BF), (4, 12, 16, 90, 3, 2, 64, BF), (9, 7, 32, 120, 2, 1, 128, F16), (65, 9, 16, 900, 2, 8, 128, BF), (40, 4, 64, 300, 1, 3, 64, F16), (1500, 3, 16, 7000, 1, 1, 64, BF), (8192, 2, 16, 9000, 1, 1, 64, BF)])
 def test_pages_reorder(seqs, width, page, n_pages, layers, hkv, dh, dtype):
     rng = random.Random(seqs)
     for kind in ("beams", "identity", "all of one", "ends", "reversed"):
