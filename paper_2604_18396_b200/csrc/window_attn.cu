@@ -24,21 +24,34 @@ int launch_step(const WindowArgs &a, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, window_attn_step_kernel<T, DH>, a, splits) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
 }
 
+template <class T, int DH, bool SPLIT>
+int launch_prompt(const PromptArgs &pa, const CUtensorMap &map, cudaStream_t st) {
+    const WindowArgs &a = pa.w;
+    const size_t smem = window_attn_prompt_smem();
+    if (cudaFuncSetAttribute(window_attn_prompt_kernel<T, DH, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return RIVER_E_DEVICE;
+    const int span = kWpRows / (a.Hq / a.c.Hkv) * pa.tiles;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim = {(unsigned)pa.splits, 1, 1};
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.n_tokens / span + a.c.n_seqs) * a.c.Hkv * pa.splits));
+    cfg.blockDim = dim3(kWpThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &at;
+    cfg.numAttrs = SPLIT ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, window_attn_prompt_kernel<T, DH, SPLIT>, map, pa) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
+}
 template <class T, int DH>
 int launch_prompt(const WindowArgs &a, cudaStream_t st) {
-    const int per = kWpRows / (a.Hq / a.c.Hkv);
-    PromptArgs pa = {a, 2};
-    auto ctas = [&] { return (int64_t)(a.n_tokens / (per * pa.tiles) + a.c.n_seqs) * a.c.Hkv; };
-    if (ctas() < 148) pa.tiles = 1;
+    PromptArgs pa = {a, 1, 1};
+    prompt_shape(pa, 148);
     // the pages of this block, as rows of a head's dims
     CUtensorMap map;
     const size_t rows = (size_t)a.c.n_pages * 2 * a.c.Hkv << a.c.ps_log2;
     if (rows >= (1ull << 31)) return RIVER_E_SHAPE;
     if (!make_map_bf16(&map, a.c.pool + rows * DH * 2 * a.layer0, DH, rows, 16)) return RIVER_E_DEVICE;
-    const size_t smem = window_attn_prompt_smem();
-    if (cudaFuncSetAttribute(window_attn_prompt_kernel<T, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return RIVER_E_DEVICE;
-    window_attn_prompt_kernel<T, DH><<<(unsigned)ctas(), kWpThreads, smem, st>>>(map, pa);
-    return RIVER_OK;
+    return pa.splits > 1 ? launch_prompt<T, DH, true>(pa, map, st) : launch_prompt<T, DH, false>(pa, map, st);
 }
 
 template <class T, int DH>

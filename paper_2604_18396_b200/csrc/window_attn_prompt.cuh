@@ -23,12 +23,13 @@
 
 namespace river {
 
-constexpr int kWpRows = 128, kWpKeys = 128, kWpThreads = 384;
+constexpr int kWpRows = 128, kWpKeys = 128, kWpThreads = 384, kWpMaxSplits = 4;
 constexpr float kWpLazy = 8.f;  // growth of a row's maximum (log2) that O waits for before it is rescaled
 
 struct PromptArgs {
     WindowArgs w;
-    int tiles;  // query tiles of a CTA: 2, or 1 where there are few
+    int tiles;   // query tiles of a CTA: 1 or 2
+    int splits;  // CTAs that share out the keys of a row, a cluster
 };
 
 __device__ __forceinline__ void wp_ld32(uint32_t taddr, uint32_t (&r)[32]) {  // left under way (wp_ld_wait)
@@ -129,8 +130,10 @@ __device__ __forceinline__ void wp_exps(const uint32_t (&a)[32], const uint32_t 
     sum = f2_add(part[0], part[1]);
 }
 
-template <class T, int DH>
+// SPLIT: the key tiles of a row are shared out over a cluster, whose CTAs join their parts through distributed shared memory.
+template <class T, int DH, bool SPLIT>
 __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const __grid_constant__ CUtensorMap tmap, const PromptArgs pa) {
+    namespace cg = cooperative_groups;
     const WindowArgs &a = pa.w;
     constexpr int NB = DH / 64;                                          // blocks of 64 dims
     constexpr uint32_t QB = kWpRows * 128, KB = kWpKeys * 128;           // bytes of one block of Q / of K or V
@@ -141,6 +144,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     extern __shared__ uint8_t wp_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(wp_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *const sq = smem, *const sv = sq + 2 * NB * QB, *const sk = sv + 2 * NB * KB;  // [tile], [2 places of V], [3 of K] [NB][128 rows][128 bytes]
+    float2 *const s_ml = reinterpret_cast<float2 *>(sk);  // SPLIT, at the end: a row's maximum and sum, for its cluster
     // K of the first tile there; V of tile j and K of tile j + 1 there (4, in turn); V of tile j and K before free (2); per query tile:
     // S done, P written (2), O done; Q there
     __shared__ uint64_t bars[16];
@@ -149,7 +153,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int gq = a.Hq / a.c.Hkv, per = kWpRows / gq;  // tokens of a tile
     // heavy tiles, those behind a long history, first
-    const int kvh = blockIdx.x % a.c.Hkv, slot = gridDim.x / a.c.Hkv - 1 - blockIdx.x / a.c.Hkv;
+    const int splits = SPLIT ? pa.splits : 1, unit = blockIdx.x / splits, kvh = unit % a.c.Hkv, slot = gridDim.x / splits / a.c.Hkv - 1 - unit / a.c.Hkv;
     const int seq = prompt_seq(a.q_start, a.c.n_seqs, per * pa.tiles, slot);
     const int first = a.q_start[seq], n = a.q_start[seq + 1] - first, at = (slot - (first / (per * pa.tiles) + seq)) * per * pa.tiles;
     if (blockIdx.x == 0)
@@ -176,7 +180,10 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     // blocks of 16 positions: n_sb of the sinks, then wb0 .. last_pos / 16; a column is a place on that list, of position column
     // (sinks) or column + shift
     const int low0 = window_low(pos0, a.window), wb0 = low0 >> 4, n_sb = min((min(a.sinks, low0) + 15) >> 4, wb0), shift = 16 * (wb0 - n_sb);
-    const int nb = last_pos < 0 ? 0 : n_sb + (last_pos >> 4) - wb0 + 1, n_kt = (nb + 7) / 8;
+    const int nb_all = last_pos < 0 ? 0 : n_sb + (last_pos >> 4) - wb0 + 1, n_all = (nb_all + 7) / 8;
+    // this CTA's tiles of 128 columns: t0 .. t0 + n_kt - 1, of its blocks 8 t0 .. nb - 1
+    const int split = SPLIT ? blockIdx.x % splits : 0, t0 = SPLIT ? n_all * split / splits : 0, n_kt = SPLIT ? n_all * (split + 1) / splits - t0 : n_all;
+    const int nb = SPLIT ? min(nb_all, 8 * (t0 + n_kt)) : nb_all;
 
     const int32_t *const tbl = a.c.table + (size_t)seq * a.c.max_pages;
     auto block_of = [&](int u) { return u < n_sb ? u : wb0 + u - n_sb; };
@@ -193,9 +200,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
             const int blk = lane / NB, half = lane % NB;
-            int ahead = blk < 8 ? page_of(blk) : -1, place = 0;
+            int ahead = blk < 8 ? page_of(8 * t0 + blk) : -1, place = 0;
             auto load = [&](uint8_t *dst, int page, int j, int v, uint32_t bar) {
-                const int row = ((page * 2 * a.c.Hkv + kvh + v * a.c.Hkv) << a.c.ps_log2) + ((block_of(8 * j + blk) << 4) & ((1 << a.c.ps_log2) - 1));
+                const int row = ((page * 2 * a.c.Hkv + kvh + v * a.c.Hkv) << a.c.ps_log2) + ((block_of(8 * (t0 + j) + blk) << 4) & ((1 << a.c.ps_log2) - 1));
                 if (page >= 0) tma_load_2d(smem_u32(dst) + half * KB + blk * 2048, &tmap, 64 * half, row, bar);
             };
             // K of tile j + 1 comes together with V of tile j
@@ -203,8 +210,8 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             uint32_t bytes = 0;
             for (int j = -1; j < n_kt; ++j) {
                 const int next = ahead;  // of tile j + 1
-                ahead = blk < 8 ? page_of(8 * (j + 2) + blk) : -1;  // (under way while this tile waits for its place)
-                if (blk < 8 && 8 * (j + 1) + blk < nb && next < 0) s_err = DEV_BAD_PAGE;
+                ahead = blk < 8 ? page_of(8 * (t0 + j + 2) + blk) : -1;  // (under way while this tile waits for its place)
+                if (blk < 8 && 8 * (t0 + j + 1) + blk < nb && next < 0) s_err = DEV_BAD_PAGE;
                 const uint32_t k_bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, next >= 0)) * 2048u, bar = j < 0 ? b_first : b_full + 8 * (j & 3);
                 if (j >= 2) wp_wait(b_free + 8 * (j & 1), (j >> 1) - 1, abortp, &s_err);
                 if (lane == 0) mbar_expect_tx(bar, bytes + k_bytes);
@@ -276,7 +283,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 if (pp < per && p < n_tok) x[i] = *reinterpret_cast<const uint4 *>(src + p * a.q_tok + g * a.q_head);
             }
             bool missing = false;
-            for (int u = u0; u < nb; u += 256) missing = missing || page_of(u) < 0;
+            for (int u = 8 * t0 + u0; u < nb; u += 256) missing = missing || page_of(u) < 0;
             if (missing) s_missing = 1;
 #pragma unroll
             for (int i = 0; i < U; ++i) {
@@ -291,6 +298,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
         }
         const int q = (warp - 4) >> 2, r = 32 * (warp & 3) + lane, p = q * per + r / gq;
         bool live = r < per * gq && p < n_tok;
+        float m = -CUDART_INF_F, l = 0.f;
         if (q < nq) {
             const int pos = pos0 + min(p, n_tok - 1);
             const int c_sink = min(a.sinks, max(pos + 1, 0)), c_lo = window_low(pos, a.window) - shift, c_hi = pos + 1 - shift;  // columns seen: [0, c_sink), [c_lo, c_hi)
@@ -299,16 +307,15 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             const int all_sink = min(a.sinks, max(pos0 + 1, 0)), any_sink = min(a.sinks, last_pos + 1);
             const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + 128u * q + quarter, t_o = tmem + kO + (uint32_t)DH * q + quarter;
             const float c = fmaxf(fabsf(a.scale_log2), 1e-30f);  // (a scale of 0: every score 0, hidden ones -inf still)
-            float m = -CUDART_INF_F, l = 0.f;
             const bool missing = s_missing != 0;
             for (int j = 0; j < n_kt; ++j) {
-                const int c0 = 128 * j;
+                const int c0 = 128 * (t0 + j);
                 uint32_t valid = 0xffu;  // blocks that are there
                 bool part = !(c0 >= all_lo && c0 + 128 <= all_hi) && !(c0 + 128 <= all_sink);
                 if (missing) {
 #pragma unroll 1
                     for (int i = 0; i < 8; ++i)
-                        if (8 * j + i < nb && page_of(8 * j + i) < 0) valid &= ~(1u << i);
+                        if (8 * (t0 + j) + i < nb && page_of(8 * (t0 + j) + i) < 0) valid &= ~(1u << i);
                     part = part || valid != 0xffu;
                 }
                 if (part && q == 0) {  // thread = V row: those that nobody sees become zero, the others are looked through
@@ -404,7 +411,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             if (n_kt > 0) wp_wait(b_o + 8 * q, 0, abortp, &s_err);
             __syncwarp();
             tc_fence_after();
-            {
+            if constexpr (!SPLIT) {
                 const bool none = m == -CUDART_INF_F;  // (no key seen: O may be 0 x whatever)
                 live = live && !*abortp;
                 const float inv = none ? 0.f : 1.f / l;
@@ -432,6 +439,25 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 tc_fence_before();
             }
         }
+        if constexpr (SPLIT) {
+            asm volatile("bar.sync 1, 256;" ::: "memory");  // (both tiles' MMAs are complete: the places of Q and V are free, and those of K)
+            if (q < nq) {
+                s_ml[q * kWpRows + r] = make_float2(m, l);
+                float4 *const mine = reinterpret_cast<float4 *>(smem) + (q * kWpRows + r) * (DH / 4);
+                if (n_kt > 0)
+#pragma unroll 1
+                    for (int d = 0; d < DH; d += 32) {
+                        uint32_t o[32];
+                        wp_ld32(tmem + kO + (uint32_t)DH * q + ((uint32_t)(32 * (warp & 3)) << 16) + d, o);
+                        wp_ld_wait();
+                        wp_pin(o);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            mine[(d / 4 + e) ^ (r & (DH / 4 - 1))] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
+                    }
+            }
+            tc_fence_before();
+        }
     }
     __syncwarp();
     if (*abortp) {  // a wait ran out: what this CTA has asked for lands within microseconds; do not leave before
@@ -443,6 +469,44 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
         tc_dealloc(tmem, 512u);
     }
     if (tid == 0 && s_err) flag(a.status, s_err == DEV_WAIT_TIMEOUT ? RIVER_E_TIMEOUT : RIVER_E_BADARG);
+    if constexpr (SPLIT) {
+        // ---- the cluster's parts of a row, a row (dh 64: two) per warp: every CTA finishes its share of the rows.  (Not warps 0 .. 3, which have
+        // few registers left.)
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        constexpr int L = DH / 4;  // lanes of a row
+        const int rows = nq * kWpRows, mine = (rows + splits - 1) / splits;
+        for (int i = (warp - 4) * (32 / L) + lane / L; warp >= 4 && i < mine; i += 256 / L) {
+            const int rr = split * mine + i, r = rr % kWpRows, t = rr / kWpRows * per + r / gq;
+            if (rr >= rows || r >= per * gq || t >= n_tok) continue;
+            const int chunk = lane % L;
+            float2 ml[kWpMaxSplits];
+            float4 o[kWpMaxSplits];
+#pragma unroll
+            for (int k = 0; k < kWpMaxSplits; ++k) {
+                ml[k] = make_float2(-CUDART_INF_F, 0.f);
+                if (k >= splits) continue;
+                ml[k] = *cluster.map_shared_rank(&s_ml[rr], k);
+                o[k] = *cluster.map_shared_rank(reinterpret_cast<const float4 *>(smem) + rr * (DH / 4) + (chunk ^ (r & (DH / 4 - 1))), k);
+            }
+            float top = -CUDART_INF_F, sum = 0.f;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kWpMaxSplits; ++k) top = fmaxf(top, ml[k].x);
+            const float base = top == -CUDART_INF_F ? 0.f : top;
+#pragma unroll
+            for (int k = 0; k < kWpMaxSplits; ++k) {
+                if (ml[k].x == -CUDART_INF_F) continue;  // (that CTA has no key of this row: its O may be anything)
+                const float f = ex2(ml[k].x - base);
+                sum += ml[k].y * f;
+                y.x += o[k].x * f; y.y += o[k].y * f; y.z += o[k].z * f; y.w += o[k].w * f;
+            }
+            const float inv = top == -CUDART_INF_F && sum == 0.f ? 0.f : 1.f / sum;
+            *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + ((size_t)(tok0 + t) * a.Hq + kvh * gq + r % gq) * DH + 4 * chunk) =
+                make_uint2(pack_pair<T>(y.x * inv, y.y * inv), pack_pair<T>(y.z * inv, y.w * inv));
+        }
+        cluster.sync();  // (peers read this CTA's part; and no row is written any more)
+    }
     if (s_poison && warp >= 4)
 #pragma unroll 1
         for (int r = warp - 4; r < n_tok * gq; r += 8) window_attn_row<T, DH>(a, tok0 + r / gq, kvh * gq + r % gq, seq, pos0 + r / gq);
@@ -450,5 +514,28 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
 
 // (the head dim of 64 asks for as much as 128 does: no CTA that wants tensor memory shares an SM with one that holds all of it)
 inline size_t window_attn_prompt_smem() { return 1024 + 7 * 2 * 128 * 128; }
+
+// Query tiles of a CTA and CTAs of a cluster, by an estimate of the time in us: a CTA takes 8 for its start and end, 1.4 (one query
+// tile) or 1.7 (two) for each of its key tiles, and 4 for the joining where the keys are split; up to one CTA per SM at a time.  One
+// prompt, window 1024, 8B-class heads, 64 new tokens: 21 us with whole rows, 17 over four CTAs; 4096 positions of 8 heads without groups 111
+// us with one query tile to a CTA, 74 with two.
+inline void prompt_shape(PromptArgs &pa, int num_sms) {
+    const WindowArgs &a = pa.w;
+    const int per = kWpRows / (a.Hq / a.c.Hkv);
+    double best_t = 1e300;
+    for (int tiles = 2; tiles >= 1; --tiles)
+        for (int splits = 1; splits <= kWpMaxSplits; splits *= 2) {
+            const int span = per * tiles;
+            const double keys = (double)std::min<int64_t>((int64_t)a.c.max_pages << a.c.ps_log2, (int64_t)a.window + span + a.sinks), kt = std::ceil(keys / 128.0 + 0.5);
+            const double rounds = (std::ceil((double)a.n_tokens / span) + (a.c.n_seqs - 1) / 2) * a.c.Hkv * splits / num_sms;
+            const double one = 8.0 + std::ceil(kt / splits) * (tiles == 1 ? 1.4 : 1.7) + (splits > 1 ? 4.0 : 0.0);
+            const double t = one * (rounds <= 1.0 ? 1.0 : rounds <= 2.0 ? 2.0 : rounds + 0.3);
+            if (t < 0.97 * best_t) {
+                best_t = t;
+                pa.tiles = tiles;
+                pa.splits = splits;
+            }
+        }
+}
 
 }  // namespace river
