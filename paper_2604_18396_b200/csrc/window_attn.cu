@@ -9,8 +9,7 @@ namespace river {
 namespace {
 
 template <class T, int DH>
-int launch_step(const WindowArgs &a, cudaStream_t st) {
-    const int splits = step_splits(a, 148);
+int launch_step(const WindowArgs &a, int splits, cudaStream_t st) {
     if (splits > 8 && cudaFuncSetAttribute(window_attn_step_kernel<T, DH>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return RIVER_E_DEVICE;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
@@ -43,9 +42,8 @@ int launch_prompt(const PromptArgs &pa, const CUtensorMap &map, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, window_attn_prompt_kernel<T, DH, SPLIT>, map, pa) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
 }
 template <class T, int DH>
-int launch_prompt(const WindowArgs &a, cudaStream_t st) {
-    PromptArgs pa = {a, 1, 1};
-    prompt_shape(pa, 148);
+int launch_prompt(const PromptArgs &pa, cudaStream_t st) {
+    const WindowArgs &a = pa.w;
     // the pages of this block, as rows of a head's dims
     CUtensorMap map;
     const size_t rows = (size_t)a.c.n_pages * 2 * a.c.Hkv << a.c.ps_log2;
@@ -54,11 +52,17 @@ int launch_prompt(const WindowArgs &a, cudaStream_t st) {
     return pa.splits > 1 ? launch_prompt<T, DH, true>(pa, map, st) : launch_prompt<T, DH, false>(pa, map, st);
 }
 
+// Single tokens and prompts by the two estimates: a token by itself reads its window once for up to eight heads, query tiles once for
+// 128 rows.  (us, single tokens / query tiles, heads of 128; 32 query and 8 KV heads, one sequence, window 4096: 2 tokens 12 / 21, 6 22
+// / 22, 16 37 / 23; 64 sequences of 2: 283 / 219; window 1024, one sequence, 8 tokens 11 / 14, 16 15 / 15; 12 and 1 heads, 4 sequences of 8:
+// 12 / 16.)
 template <class T, int DH>
 int launch(const WindowArgs &a, cudaStream_t st) {
-    const int gq = a.Hq / a.c.Hkv;
-    if (a.max_q <= 4 || gq > kWpRows) return launch_step<T, DH>(a, st);
-    return launch_prompt<T, DH>(a, st);
+    double step_us, prompt_us = 1e300;
+    const int splits = step_splits(a, 148, step_us);
+    PromptArgs pa = {a, 1, 1};
+    if (a.Hq / a.c.Hkv <= kWpRows) prompt_shape(pa, 148, prompt_us);
+    return step_us <= prompt_us ? launch_step<T, DH>(a, splits, st) : launch_prompt<T, DH>(pa, st);
 }
 
 }  // namespace

@@ -322,7 +322,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                     wp_wait(b_full + 8 * (j & 3), j >> 2, abortp, &s_err);
                     const int cc = c0 + r;
                     uint8_t *row = sv + (j & 1) * NB * KB + r * 128;
-                    if ((valid >> (r >> 4) & 1u) && (cc < any_sink || (cc >= any_lo && cc < any_hi))) {
+                    if ((valid >> (r >> 4) & 1u) && (cc < all_sink || (cc >= all_lo && cc < all_hi))) {
+                        // (seen by every row: whatever it is, it belongs in every result)
+                    } else if ((valid >> (r >> 4) & 1u) && (cc < any_sink || (cc >= any_lo && cc < any_hi))) {
                         // an exponent of ones (what is no number) and one more carries into the sign's place
                         constexpr uint32_t E = std::is_same<T, __nv_bfloat16>::value ? 0x7f807f80u : 0x7c007c00u, ONE = E & ~(E << 1);
                         uint32_t odd = 0u;
@@ -362,6 +364,15 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 uint64_t sum;
                 uint32_t w[32];
                 const uint64_t c2 = f2_pack(c, c);
+                if (j == 0) {
+                    float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
+                    const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
+                    m = mx < CUDART_INF_F ? mx : CUDART_NAN_F;
+                }
                 while (true) {
                     sum = 0ull;
                     const float base = m == -CUDART_INF_F ? 0.f : m;
@@ -415,27 +426,30 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 const bool none = m == -CUDART_INF_F;  // (no key seen: O may be 0 x whatever)
                 live = live && !*abortp;
                 const float inv = none ? 0.f : 1.f / l;
-                T *out = static_cast<T *>(a.out) + ((size_t)(tok0 + p) * a.Hq + kvh * gq + r % gq) * DH;
+                uint4 *const mine = reinterpret_cast<uint4 *>(sq + q * NB * QB);  // (rows through the place of this tile's Q: whole lines of them go out)
+                constexpr int C8 = DH / 8;
 #pragma unroll 1
                 for (int d = 0; d < DH; d += 32) {
-                    uint32_t o[32];
+                    uint32_t o[32], w[16];
                     if (n_kt > 0) {
                         wp_ld32(t_o + d, o);
                         wp_ld_wait();
                         wp_pin(o);
                     }
-                    if (live) {
-                        uint32_t w[16];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = n_kt > 0 ? pack_pair<T>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
-                        if (none) {
+                    for (int e = 0; e < 16; ++e) w[e] = none ? 0u : pack_pair<T>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) w[e] = 0u;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4 *>(out + d + 2 * e) = make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]);
-                    }
+                    for (int e = 0; e < 4; ++e) mine[r * C8 + ((d / 8 + e) ^ (r & (C8 - 1)))] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
                 }
+                __syncwarp();
+                const int lr = lane / C8, lc = lane % C8, inv_gq = 65536 / gq + 1;
+                if (!*abortp)
+#pragma unroll 4
+                    for (int i = 0; i < 32; i += 32 / C8) {
+                        const int rr = 32 * (warp & 3) + i + lr, pp = rr * inv_gq >> 16, t = q * per + pp;
+                        if (pp < per && t < n_tok)
+                            *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + ((size_t)(tok0 + t) * a.Hq + kvh * gq + rr - pp * gq) * DH + 8 * lc) = mine[rr * C8 + (lc ^ (rr & (C8 - 1)))];
+                    }
                 tc_fence_before();
             }
         }
@@ -519,15 +533,16 @@ inline size_t window_attn_prompt_smem() { return 1024 + 7 * 2 * 128 * 128; }
 // tile) or 1.7 (two) for each of its key tiles, and 4 for the joining where the keys are split; up to one CTA per SM at a time.  One
 // prompt, window 1024, 8B-class heads, 64 new tokens: 21 us with whole rows, 17 over four CTAs; 4096 positions of 8 heads without groups 111
 // us with one query tile to a CTA, 74 with two.
-inline void prompt_shape(PromptArgs &pa, int num_sms) {
+inline void prompt_shape(PromptArgs &pa, int num_sms, double &best_t) {
     const WindowArgs &a = pa.w;
     const int per = kWpRows / (a.Hq / a.c.Hkv);
-    double best_t = 1e300;
+    best_t = 1e300;
     for (int tiles = 2; tiles >= 1; --tiles)
         for (int splits = 1; splits <= kWpMaxSplits; splits *= 2) {
             const int span = per * tiles;
             const double keys = (double)std::min<int64_t>((int64_t)a.c.max_pages << a.c.ps_log2, (int64_t)a.window + span + a.sinks), kt = std::ceil(keys / 128.0 + 0.5);
-            const double rounds = (std::ceil((double)a.n_tokens / span) + (a.c.n_seqs - 1) / 2) * a.c.Hkv * splits / num_sms;
+            const double parts = a.c.n_seqs == 1 ? std::ceil((double)a.n_tokens / span) : std::max((double)a.c.n_seqs, (double)a.n_tokens / span + 0.5 * a.c.n_seqs);
+            const double rounds = parts * a.c.Hkv * splits / num_sms;
             const double one = 8.0 + std::ceil(kt / splits) * (tiles == 1 ? 1.4 : 1.7) + (splits > 1 ? 4.0 : 0.0);
             const double t = one * (rounds <= 1.0 ? 1.0 : rounds <= 2.0 ? 2.0 : rounds + 0.3);
             if (t < 0.97 * best_t) {
