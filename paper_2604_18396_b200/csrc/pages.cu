@@ -402,7 +402,7 @@ int launch_deciding(K kernel, const PagesArgs &a, size_t work, size_t smem, cuda
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = &at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = ctas > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
 }
 // `most`: heads' worth of copies that there may be

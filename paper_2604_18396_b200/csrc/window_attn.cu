@@ -19,7 +19,7 @@ int launch_step(const WindowArgs &a, int splits, cudaStream_t st) {
     cfg.blockDim = dim3(32 * kStepWarps);
     cfg.stream = st;
     cfg.attrs = &at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = splits > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, window_attn_step_kernel<T, DH>, a, splits) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
 }
 
