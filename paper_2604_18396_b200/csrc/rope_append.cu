@@ -132,6 +132,8 @@ __global__ void __launch_bounds__(256) rope_append_any_kernel(const RopeArgs a, 
 // 16-byte rows.  A CTA takes blockDim.z tokens; thread (x, y, z) unit x of the rows y, y + blockDim.y, .. of token z.  A unit is eight dims
 // (interleaved: four pairs, or dims that stay), or eight pairs and their partners half a turned part further (half layout).  UNITS rows of
 // a thread, 192 bytes, are under way before place and angles are known; a thread's sines and cosines are the same for all its rows.
+// Prompts are bound by HBM and by the instructions beside it: 8192 tokens of 48 heads of 128, three quarters turned, bf16: 40 us, 5.0 TB/s (44 with
+// 64-bit products for every unit's address).
 template <class TI, class TC, bool INTER, int UNITS>
 __global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
     __shared__ float4 cs[kRopeTokens][32];  // two pairs' (cos, sin)

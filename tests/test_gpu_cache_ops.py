@@ -269,6 +269,22 @@ def test_window_attention_flags_a_wrong_max_q():
     assert status.item() == -1
 
 
+def test_window_attention_lengths_beyond_the_table():
+    pool, table, lens = ref.cache([64, 30], 16, 1, 64, BF, 4, width=4)
+    q = torch.randn(60, 2, 64, device="cuda").to(BF)
+    for new in (1, 60):
+        want, got = torch.zeros_like(q), torch.full_like(q, NAN)
+        window_attention(q, want, i32([0, new, new]), pool, 1, table, lens, window=20, sinks=2, max_q=new)
+        status = i32([0])
+        window_attention(q, got, i32([0, new, new]), pool, 1, table, i32([2 ** 31 - 1, 30]), window=20, sinks=2, max_q=new, status=status)
+        assert status.item() == -1 and torch.equal(got[:new], want[:new])
+
+
+@pytest.mark.parametrize("hq,hkv", [(160, 1), (129, 1), (128, 1)])
+def test_window_attention_many_heads_to_one(hq, hkv):
+    attn_case([20, 1], [100, 5], hq, hkv, 64, 16, 64, 4, BF)
+
+
 def test_offsets_past_32_bits():
     """A block that begins 5 GB into the pool."""
     hkv, dh, page = 8, 128, 16
