@@ -25,6 +25,7 @@ struct PagesArgs {
     int window, sinks;
     int32_t *table_out, *lens_out, *refs_out, *list, *status;  // list: of copies or moves
     int32_t *remap, *n_used;
+    int copy_here;  // the deciding cluster copies as well
 };
 
 // Shared memory of a deciding CTA; `count` is read and the first one's `odd` written by the other CTAs of the cluster.
@@ -163,6 +164,22 @@ __device__ __forceinline__ void copy_ints(int32_t *to, const int32_t *from, size
         for (i = n / 4 * 4 + thread; i < n; i += threads) to[i] = from[i];
     } else {
         for (size_t i = thread; i < n; i += threads) to[i] = from[i];
+    }
+}
+
+// One head's values of a page, of one block, by a warp: its filled positions are consecutive, and 4 KB are under way.
+__device__ __forceinline__ void copy_head(const Paged &c, int l, int head, int src, int dst, int positions) {
+    const int lane = threadIdx.x & 31, chunks = positions * (c.dh / 8);
+    const uint4 *f = reinterpret_cast<const uint4 *>(c.pool) + c.row(l, src, 0, head, 0) / 8;  // (a page's heads of V follow those of K)
+    uint4 *t = reinterpret_cast<uint4 *>(c.pool) + c.row(l, dst, 0, head, 0) / 8;
+    for (int c0 = lane; c0 < chunks; c0 += 8 * 32) {
+        uint4 v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c0 + 32 * e < chunks) v[e] = ldg_stream16(f + c0 + 32 * e);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c0 + 32 * e < chunks) t[c0 + 32 * e] = v[e];
     }
 }
 
@@ -308,7 +325,14 @@ __global__ void __launch_bounds__(kPgThreads) pages_reorder_kernel(const PagesAr
         a.lens_out[i] = code != RIVER_OK ? len[i] : p >= 0 ? len[p] : 0;
     }
     if (thread == 0) *a.status = code;
-    cluster.sync();  // (nobody leaves while its shared memory may be read)
+    cluster.sync();  // (nobody leaves while its shared memory may be read; the list is written)
+    if (a.copy_here && code == RIVER_OK) {
+        const int heads = 2 * a.c.Hkv, L = a.c.n_layers;
+        for (int w = thread >> 5; w < want * L * heads; w += threads / 32) {
+            const int *e = a.list + 1 + 3 * (w / heads / L);
+            copy_head(a.c, w / heads % L, w % heads, __ldcg(e), __ldcg(e + 1), __ldcg(e + 2));
+        }
+    }
 }
 
 __global__ void __launch_bounds__(kPgThreads) pages_compact_kernel(const PagesArgs a) {
@@ -355,28 +379,16 @@ __global__ void __launch_bounds__(kPgThreads) pages_compact_kernel(const PagesAr
     if (thread == 0) { *a.n_used = used; a.list[0] = moves; }
 }
 
-// The values of the pages on the list, a warp per (page, block, head): its filled positions are consecutive.  triples: (from, to, positions)
-// entries; else whole pages, to[] and from[] apart, and the table's entries follow `remap`.  Every warp has 4 KB under way.
+// The values of the pages on the list, a warp per (page, block, head): triples: (from, to, positions) entries; else whole
+// pages, to[] and from[] apart, and the table's entries follow `remap`.
 constexpr int kCopyCtas = 64;  // of the grid, per SM (8 are resident; grids of 8, 32 and 64 take 330, 312, 309 us for 2 GB)
 __global__ void __launch_bounds__(256) pages_copy_kernel(const PagesArgs a, int triples) {
     pdl_wait();
-    const int n = a.list[0], heads = 2 * a.c.Hkv, lane = threadIdx.x & 31, warps = gridDim.x * 8, L = a.c.n_layers, row16 = a.c.dh / 8;
-    uint4 *const pool = reinterpret_cast<uint4 *>(a.c.pool);
+    const int n = a.list[0], heads = 2 * a.c.Hkv, warps = gridDim.x * 8, L = a.c.n_layers;
     for (int64_t w = blockIdx.x * 8 + (threadIdx.x >> 5); w < (int64_t)n * L * heads; w += warps) {
         const int head = (int)(w % heads), l = (int)(w / heads % L), k = (int)(w / heads / L);
         const int src = triples ? a.list[1 + 3 * k] : a.list[1 + a.c.n_pages / 2 + k], dst = triples ? a.list[2 + 3 * k] : a.list[1 + k];
-        const int chunks = (triples ? a.list[3 + 3 * k] : 1 << a.c.ps_log2) * row16;
-        const uint4 *f = pool + a.c.row(l, src, 0, head, 0) / 8;  // (a page's heads of V follow those of K)
-        uint4 *t = pool + a.c.row(l, dst, 0, head, 0) / 8;
-        for (int c0 = lane; c0 < chunks; c0 += 8 * 32) {
-            uint4 v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c0 + 32 * e < chunks) v[e] = ldg_stream16(f + c0 + 32 * e);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c0 + 32 * e < chunks) t[c0 + 32 * e] = v[e];
-        }
+        copy_head(a.c, l, head, src, dst, triples ? a.list[3 + 3 * k] : 1 << a.c.ps_log2);
     }
     if (triples) return;
     const size_t entries = (size_t)a.c.n_seqs * a.c.max_pages;
@@ -456,8 +468,12 @@ extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, co
     a.list = copies;
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (const int rc = launch_deciding(pages_reorder_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, 5 * sizeof(int) * (size_t)c->n_seqs, st)) return rc;
-    return launch_copy(a, 1, (int64_t)std::min(c->n_seqs, c->n_pages) * c->n_layers * 2 * c->Hkv, st);
+    // A few sequences' last pages (up to 4 MB) are copied by the deciding cluster itself: four beams of the 1B class 14.2 us in two launches, 12.3 in one.
+    const int64_t most = (int64_t)std::min(c->n_seqs, c->n_pages) * c->n_layers * 2 * c->Hkv;
+    a.copy_here = most * c->page_size * c->dh * 2 <= (4 << 20);
+    const size_t work = std::max((size_t)c->n_seqs * c->max_pages + c->n_pages, a.copy_here && most > 32 ? (size_t)4 * kPgThreads + 1 : (size_t)0);
+    if (const int rc = launch_deciding(pages_reorder_kernel, a, work, 5 * sizeof(int) * (size_t)c->n_seqs, st)) return rc;
+    return a.copy_here ? RIVER_OK : launch_copy(a, 1, most, st);
 }
 
 extern "C" int river_pages_compact(const river_paged *c, const int32_t *refs, int32_t *table_out, int32_t *refs_out, int32_t *remap,

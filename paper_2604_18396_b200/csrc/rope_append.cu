@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
     const int t = blockIdx.x * blockDim.z + z;
     const bool live = t < a.n_tokens;
     // dims of this unit: d0 .. d0 + 7, and in the half layout d0 + half ..
-    const bool pairs = x < a.rot / (INTER ? 8 : 16);
+    const bool pairs = x < (a.rot + 7) / (INTER ? 8 : 16);
     const int d0 = INTER || pairs ? 8 * x : 8 * x + half;
     const int pos = live ? a.positions[t] : 0, seq = live ? a.seqs[t] : -1;
     // this thread's units of the token's first heads, in bytes; heads are a 32-bit step apart (the launch has looked)
@@ -192,6 +192,7 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
                 if constexpr (INTER) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
+                        if (4 * x + e >= half) continue;  // (the last unit may be turned in part)
                         const float y0 = p[2 * e] * w[e].x - p[2 * e + 1] * w[e].y;
                         p[2 * e + 1] = p[2 * e + 1] * w[e].x + p[2 * e] * w[e].y;
                         p[2 * e] = y0;
@@ -224,7 +225,7 @@ bool rope_wide(const RopeArgs &a, size_t es) {
 template <class TI, class TC, bool INTER>
 void launch_rope(const RopeArgs &a, cudaStream_t st) {
     const bool wide = rope_wide(a, sizeof(TI));
-    if (!wide || a.rot % (INTER ? 8 : 16)) {  // (8192 tokens of 48 heads of 128, bf16, a turned part of 34: 93 us; of 128, in units, 40)
+    if (!wide || (!INTER && a.rot % 16)) {  // (8192 tokens of 48 heads of 128, bf16, half layout, a turned part of 34: 93 us; of 128, in units, 40)
         rope_append_any_kernel<TI, TC, INTER><<<a.n_tokens, 256, 0, st>>>(a, wide);
         return;
     }
