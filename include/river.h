@@ -351,7 +351,7 @@ int river_rope_append(const river_paged *c, int layer, int n_tokens, int Hq, int
 /* Attention over a sliding window and a few first positions ("sinks"), for single tokens and for prompts.  Sequence s has the queries
  * q_start[s] .. q_start[s + 1] - 1, which are its LAST positions: query i of n stands at p = lens[s] - n + i and sees the positions
  * j <= p with j < sinks or j > p - window;  out = softmax(softmax_scale q K^T) V over those, zero where there are none.
- *   q             rows of Hq heads of the pool's type, Hq a multiple of Hkv;  n_tokens rows in all
+ *   q             rows of Hq heads of the pool's type, Hq a multiple of Hkv;  n_tokens rows in all; address and strides in whole 16 bytes
  *   max_q         at least the largest number of queries of a sequence (1: a decode step)
  *   q_start       [dev] int32 [n_seqs + 1], ascending from 0 to n_tokens
  *   window        >= 1 (one that reaches over the whole context is ordinary causal attention);  sinks >= 0

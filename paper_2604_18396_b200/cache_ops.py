@@ -1,7 +1,7 @@
 """Operators for long contexts on a paged cache (river_rope_append, river_window_attention, river_pages_*), over torch tensors.
 
 Argument marshalling and checks only, like binding.py: every operator is one call into the CUDA library, asynchronous on `stream`
-(default: torch's current stream); there is no fallback.  A cache is
+(default: torch's current stream; another one has been ordered behind the inputs' by the caller); there is no fallback.  A cache is
 
     pool   bf16 or f16 [n_layers, n_pages, 2 (K, V), Hkv, page_size, dh]   page_size 16, 32 or 64; dh 64 or 128
     table  int32 [n_seqs, max_pages]                                       page of positions page_size * j ..; -1: none
@@ -86,6 +86,14 @@ def _run(fn, device: int, stream, used: Sequence[Optional[torch.Tensor]], *args)
         for t in used:
             if t is not None:
                 t.record_stream(stream)
+
+
+def _scratch(n: int, device: torch.device, stream) -> torch.Tensor:
+    """n ints from the memory of the stream that uses them (what another stream hands out may be in use there still)."""
+    if stream is None:
+        return torch.empty(n, dtype=_I32, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=_I32, device=device)
 
 
 def rope_frequencies(rotary_dim: int, theta: float, kind: str = "none", *, factor: float = 1.0, original_context: int = 0, low_freq: float = 1.0,
@@ -180,7 +188,7 @@ def pages_reorder(pool: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, r
     c = _cache(pool, table, lens, dev)
     n, r = s[:1], pool.shape[1:2]
     if copies is None:
-        copies = torch.empty(1 + 3 * s[0], dtype=_I32, device=pool.device)
+        copies = _scratch(1 + 3 * s[0], pool.device, stream)
     _run(load().river_pages_reorder, dev, stream, (pool, table, lens, refs, parents, table_out, lens_out, refs_out, copies, status), c,
          _i32(refs, r, dev, "refs"), _i32(parents, n, dev, "parents"), _i32(table_out, s, dev, "table_out"), _i32(lens_out, n, dev, "lens_out"),
          _i32(refs_out, r, dev, "refs_out"), _i32(copies, (1 + 3 * s[0],), dev, "copies"), _i32(status, (1,), dev, "status"))
@@ -195,7 +203,7 @@ def pages_compact(pool: torch.Tensor, table: torch.Tensor, refs: torch.Tensor, t
     c = _cache(pool, table, None, dev)
     r = pool.shape[1:2]
     if moves is None:
-        moves = torch.empty(1 + r[0], dtype=_I32, device=pool.device)
+        moves = _scratch(1 + r[0], pool.device, stream)
     _run(load().river_pages_compact, dev, stream, (pool, table, refs, table_out, refs_out, remap, n_used, moves), c, _i32(refs, r, dev, "refs"),
          _i32(table_out, s, dev, "table_out"), _i32(refs_out, r, dev, "refs_out"), _i32(remap, r, dev, "remap"), _i32(n_used, (1,), dev, "n_used"),
          _i32(moves, (1 + r[0],), dev, "moves"))

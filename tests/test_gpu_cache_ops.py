@@ -466,6 +466,50 @@ def test_on_another_stream_and_in_a_graph():
         assert torch.equal(out, want)
 
 
+def test_moving_pages_in_a_graph_and_on_another_stream():
+    """Both kernels of a call, the second one under programmatic launch."""
+    rng = random.Random(5)
+    n, seqs = 300, 40
+    table, lens, refs = state(rng, seqs, 6, 16, n)
+    parents = [rng.randrange(seqs) for _ in range(seqs)]
+    pool0 = torch.randn(8, n, 2, 8, 16, 64, device="cuda").to(BF)
+    want = ref.reorder(table, lens, refs, parents, 16)
+    want_pool = pool0.clone()
+    for src, dst, fill in want[3]:
+        want_pool[:, dst, :, :, :fill] = pool0[:, src, :, :, :fill]
+    after = ref.compact(want[0], want[2])
+    for src, dst in after[4]:
+        want_pool[:, dst] = want_pool[:, src].clone()
+    pool = pool0.clone()
+    a = [i32(x) for x in (table, lens, refs, parents)]
+    outs, ends = [torch.empty_like(x) for x in a[:3]] + [i32([77])], [torch.empty_like(x) for x in (a[0], a[2], a[2])] + [i32([77])]
+
+    def both(stream=None):
+        pages_reorder(pool, *a, *outs, stream=stream)
+        pages_compact(pool, outs[0], outs[2], *ends, stream=stream)
+
+    def check():
+        assert [x.tolist() for x in outs] == [want[0], want[1], want[2], [0]]
+        assert [x.tolist() for x in ends] == [after[0], after[1], after[2], [after[3]]]
+        assert torch.equal(pool, want_pool)
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    both(st)
+    st.synchronize()
+    check()
+    pool.copy_(pool0)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    for _ in range(2):
+        pool.copy_(pool0)
+        g.replay()
+        torch.cuda.synchronize()
+        check()
+
+
 def test_pages_in_a_graph():
     a = [i32(x) for x in ([[0, -1, -1, -1], [1, 2, -1, -1]], [16, 30], [1, 1, 1, 0, 0, 0, 0, 0], [1, 1])]
     outs = [torch.empty_like(x) for x in a[:3]] + [i32([77])]
