@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(256) rope_append_any_kernel(const RopeArgs a, 
 // 16-byte rows.  A CTA takes blockDim.z tokens; thread (x, y, z) unit x of the rows y, y + blockDim.y, .. of token z.  A unit is eight dims
 // (interleaved: four pairs, or dims that stay), or eight pairs and their partners half a turned part further (half layout).  UNITS rows of
 // a thread, 192 bytes, are under way before place and angles are known; a thread's sines and cosines are the same for all its rows.
-// Prompts are bound by HBM and by the instructions beside it: 8192 tokens of 48 heads of 128, three quarters turned, bf16: 40 us, 5.0 TB/s (44 with
+// Prompts are bound by HBM and by the instructions beside it: 8192 tokens of 48 heads of 128, three quarters turned, bf16: 39 us, 5.1 TB/s (44 with
 // 64-bit products for every unit's address).
 template <class TI, class TC, bool INTER, int UNITS>
 __global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
@@ -225,14 +225,16 @@ bool rope_wide(const RopeArgs &a, size_t es) {
 template <class TI, class TC, bool INTER>
 void launch_rope(const RopeArgs &a, cudaStream_t st) {
     const bool wide = rope_wide(a, sizeof(TI));
-    if (!wide || (!INTER && a.rot % 16)) {  // (8192 tokens of 48 heads of 128, bf16, half layout, a turned part of 34: 93 us; of 128, in units, 40)
+    if (!wide || (!INTER && a.rot % 16)) {  // (8192 tokens of 48 heads of 128, bf16, half layout, a turned part of 34: 93 us; of 128, in units, 37)
         rope_append_any_kernel<TI, TC, INTER><<<a.n_tokens, 256, 0, st>>>(a, wide);
         return;
     }
     constexpr int UNITS = (INTER ? 24 : 12) / (int)sizeof(TI);
     const int per = INTER ? a.c.dh / 8 : a.rot / 16 + (a.c.dh - a.rot) / 8, rows = a.Hq + 2 * a.c.Hkv;
-    // few tokens: a CTA each, with all the threads that its rows keep busy
-    const int y = a.n_tokens < 148 * 4 ? std::min(256 / per, rows) : std::min(256 / per, (rows + UNITS - 1) / UNITS), z = std::min(std::max(1, 256 / (per * y)), a.n_tokens < 148 * 4 ? 1 : kRopeTokens);
+    // Few tokens: a CTA each, with all the threads that its rows keep busy.  Many: CTAs of 64 threads, which take turns at fetching, turning and
+    // storing (8192 tokens of 48 heads of 128, us with 64, 128, 256 threads: from fp32 49, 54, 58; interleaved bf16 39, 40, 42; half 41, 42, 40).
+    const bool few = a.n_tokens < 148 * 4;
+    const int most = few ? 256 : 64, y = few ? std::min(most / per, rows) : std::min(most / per, (rows + UNITS - 1) / UNITS), z = few ? 1 : std::min(std::max(1, most / (per * y)), kRopeTokens);
     rope_append_kernel<TI, TC, INTER, UNITS><<<(a.n_tokens + z - 1) / z, dim3(per, y, z), 0, st>>>(a);
 }
 template <class TI, class TC>
