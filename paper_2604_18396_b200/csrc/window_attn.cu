@@ -10,12 +10,14 @@ namespace {
 
 template <class T, int DH>
 int launch_step(const WindowArgs &a, int splits, cudaStream_t st) {
+    const int64_t ctas = (int64_t)splits * a.c.Hkv * ((a.Hq / a.c.Hkv + 7) / 8) * a.max_q * a.c.n_seqs;
+    if (ctas > INT32_MAX) return RIVER_E_SHAPE;
     if (splits > 8 && cudaFuncSetAttribute(window_attn_step_kernel<T, DH>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return RIVER_E_DEVICE;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim = {(unsigned)splits, 1, 1};
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(splits * a.c.Hkv * ((a.Hq / a.c.Hkv + 7) / 8) * a.max_q * a.c.n_seqs));
+    cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(32 * kStepWarps);
     cfg.stream = st;
     cfg.attrs = &at;

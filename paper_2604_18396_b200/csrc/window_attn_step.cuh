@@ -279,7 +279,8 @@ __global__ void __launch_bounds__(32 * kStepWarps, kStepCtas) window_attn_step_k
 // than four leave places free: a GPC, of about 16 SMs, takes whole ones.  (8B-class heads, us with 3, 4, 6, 8, 16 CTAs: window 4096, 64
 // rows 185, 184, 203, 218, 304; 16 rows 48, 67, 53, 61, 84; 4 rows 35, 28, 22, 19, 26; window 8192, one row 60, 47, 33, 27, 17.)
 inline int step_splits(const WindowArgs &a, int num_sms, double &best_t) {
-    const double units = (double)a.c.n_seqs * a.max_q * a.c.Hkv * ((a.Hq / a.c.Hkv + 7) / 8);
+    const double tiles = (double)a.c.Hkv * ((a.Hq / a.c.Hkv + 7) / 8), units = (double)a.n_tokens * tiles;
+    const double idle = std::max(0.0, (double)a.c.n_seqs * a.max_q - a.n_tokens) * tiles * 0.0015;  // places of queries that are none: a CTA each that leaves
     const int64_t cap = (int64_t)a.c.max_pages << a.c.ps_log2, blocks = (std::min<int64_t>(cap, (int64_t)a.window + a.sinks) >> 4) + 1;
     const double block_us = 64.0 * a.c.dh / 6.4e6;  // K and V of a block at 6.4 TB/s
     int best = 1;
@@ -288,7 +289,7 @@ inline int step_splits(const WindowArgs &a, int num_sms, double &best_t) {
         const double places = s <= 4 ? num_sms * kStepCtas : num_sms / 18 * (16 * kStepCtas / s) * s;
         const double turns = 1.4 * (double)((blocks + s * kStepWarps - 1) / (s * kStepWarps)), stream = places * (double)blocks / s * block_us, fixed = 2.0 + 0.25 * s;
         const double rounds = units * s / places, full = std::floor(rounds), rest = rounds - full;
-        const double t = full * (std::max(stream, turns) + fixed) + (rest > 0 ? std::max(stream * rest, turns) + fixed : 0.0);
+        const double t = full * (std::max(stream, turns) + fixed) + (rest > 0 ? std::max(stream * rest, turns) + fixed : 0.0) + idle * s;
         if (t < 0.99 * best_t) { best_t = t; best = s; }
     }
     return best;
