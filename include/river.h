@@ -296,7 +296,8 @@ int river_quantize_w4(const void *w, int out, int in, int group, int refine_iter
  * The calls below need no context.  They work on caller-owned device buffers, in the layout of river_kv_pool_bytes, so that they also
  * take a context's pool; they are asynchronous on cuda_stream, allocate nothing, read nothing back and can be captured in a graph.
  * What the host can see is refused before anything is queued: RIVER_E_BADARG (null or misaligned pointers, values out of range),
- * RIVER_E_SHAPE (a shape, type or combination that has no kernel).  What only the device can see goes to `status` ([dev] int32). */
+ * RIVER_E_SHAPE (a shape, type or combination that has no kernel).  A call with n_tokens 0 does nothing; addresses of its rows may be NULL.
+ * What only the device can see goes to `status` ([dev] int32). */
 enum { RIVER_BF16 = 0, RIVER_F16 = 1, RIVER_F32 = 2 };
 
 typedef struct river_paged {

@@ -76,12 +76,14 @@ extern "C" int river_window_attention(const river_paged *c, int layer, int n_tok
     using namespace river;
     WindowArgs a;
     if (const int rc = paged_check(c, true, true, &a.c)) return rc;
-    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || max_q < 0 || !q_start || !q || !q->p || !out || window < 1 || sinks < 0) return RIVER_E_BADARG;
-    if (Hq < 1 || Hq % c->Hkv || !std::isfinite(softmax_scale) || !aligned_to(out, 16)) return RIVER_E_BADARG;
+    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || max_q < 0 || !q_start || window < 1 || sinks < 0) return RIVER_E_BADARG;
+    if (Hq < 1 || Hq % c->Hkv || !std::isfinite(softmax_scale)) return RIVER_E_BADARG;
     if (c->n_seqs > 65535 || Hq > 8192 || (int64_t)c->n_seqs * Hq > (1 << 26)) return RIVER_E_SHAPE;  // (the kernels' grids)
+    if (n_tokens == 0) return RIVER_OK;  // (rows that are none may have no address)
+    if (!q || !q->p || !out || !aligned_to(out, 16)) return RIVER_E_BADARG;
     // heads are read 16 bytes at a time
     if (!aligned_to(q->p, 16) || q->token % 8 || q->head % 8) return RIVER_E_BADARG;
-    if (n_tokens == 0 || max_q == 0) return RIVER_OK;
+    if (max_q == 0) return RIVER_OK;
     a.layer0 = layer - 1;
     a.n_tokens = n_tokens;
     a.max_q = max_q < n_tokens ? max_q : n_tokens;

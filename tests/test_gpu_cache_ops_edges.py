@@ -1,0 +1,34 @@
+"""The operators on a caller's paged cache at their ends: calls without tokens, threads, errors left by others, small probabilities and infinities
+in f16, status words, lengths and starts that cannot be, and launches that only large or unaligned calls take (needs a B200)."""
+
+import pytest
+import torch
+
+from paper_2604_18396_b200 import rope_append, window_attention
+from tests import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def freq(rot):
+    return (10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).float().cuda()
+
+
+# ---------------------------------------------------------------- calls without tokens
+def test_empty_tensors_are_no_tokens():
+    """An idle step: torch gives tensors without elements the address 0."""
+    pool, table, lens = ref.cache([20], 16, 2, 64, BF, 1)
+    before, status = pool.clone(), i32([0])
+    rows = lambda h: torch.empty(0, h, 64, dtype=BF, device="cuda")  # noqa: E731
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert rows(2).data_ptr() == 0
+    rope_append(rows(4), rows(2), rows(2), none, none, freq(64), pool, 1, table, rows(4), status=status)
+    rope_append(None, rows(2), rows(2), none, none, freq(64), pool, 1, table, None, status=status)
+    for max_q in (0, 1):
+        window_attention(rows(4), rows(4), i32([0, 0]), pool, 1, table, lens, window=8, max_q=max_q, status=status)
+    assert status.item() == 0 and torch.equal(pool.view(torch.int16), before.view(torch.int16))
