@@ -17,6 +17,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kPgThreads = 1024;
 constexpr int kPgSeqs = 8192;    // sequences whose prefix sums are held in shared memory
+constexpr int kPgSeqInts = 5;    // of a reordering, per sequence in (dynamic) shared memory
 constexpr int kPgCtas = 8;       // of the deciding cluster (a portable size)
 
 struct PagesArgs {
@@ -409,7 +410,9 @@ template <class K>
 int launch_deciding(K kernel, const PagesArgs &a, size_t work, size_t smem, cudaStream_t st) {
     const unsigned ctas = work <= 4 * kPgThreads ? 1 : work < (1u << 18) ? kPgCtas : 2 * kPgCtas;
     if (ctas > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return RIVER_E_DEVICE;
-    if (smem > (32u << 10) && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return RIVER_E_DEVICE;
+    // the limit belongs to the kernel, not to the call: whoever sets it sets the same one, or a launch of another thread could fail by it
+    constexpr int most = kPgSeqInts * sizeof(int) * kPgSeqs;
+    if (smem > (32u << 10) && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return RIVER_E_DEVICE;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim = {ctas, 1, 1};
@@ -477,7 +480,7 @@ extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, co
     const int64_t most = (int64_t)std::min(c->n_seqs, c->n_pages) * c->n_layers * 2 * c->Hkv;
     a.copy_here = most * c->page_size * c->dh * 2 <= (4 << 20);
     const size_t work = std::max((size_t)c->n_seqs * c->max_pages + c->n_pages, a.copy_here && most > 32 ? (size_t)4 * kPgThreads + 1 : (size_t)0);
-    if (const int rc = launch_deciding(pages_reorder_kernel, a, work, 5 * sizeof(int) * (size_t)c->n_seqs, st)) return rc;
+    if (const int rc = launch_deciding(pages_reorder_kernel, a, work, kPgSeqInts * sizeof(int) * (size_t)c->n_seqs, st)) return rc;
     return a.copy_here ? RIVER_OK : launch_copy(a, 1, most, st);
 }
 

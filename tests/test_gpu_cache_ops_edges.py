@@ -1,10 +1,11 @@
 """The operators on a caller's paged cache at their ends: calls without tokens, threads, errors left by others, small probabilities and infinities
 in f16, status words, lengths and starts that cannot be, and launches that only large or unaligned calls take (needs a B200)."""
+import threading
 
 import pytest
 import torch
 
-from paper_2604_18396_b200 import rope_append, window_attention
+from paper_2604_18396_b200 import binding, cache_ops, rope_append, window_attention
 from tests import paged_reference as ref
 
 pytestmark = pytest.mark.gpu
@@ -32,3 +33,29 @@ def test_empty_tensors_are_no_tokens():
     for max_q in (0, 1):
         window_attention(rows(4), rows(4), i32([0, 0]), pool, 1, table, lens, window=8, max_q=max_q, status=status)
     assert status.item() == 0 and torch.equal(pool.view(torch.int16), before.view(torch.int16))
+
+
+# ---------------------------------------------------------------- threads and errors of others
+def test_reorderings_of_several_threads():
+    """Calls that need different amounts of shared memory, side by side."""
+    lib, failures = binding.load(), []
+
+    def work(seqs):
+        st = torch.cuda.Stream()
+        pool = torch.zeros(1, 1, 2, 1, 16, 64, dtype=BF, device="cuda")
+        a = [torch.full((seqs, 1), -1, dtype=torch.int32, device="cuda"), i32([0] * seqs), i32([0]), i32([-1] * seqs)]
+        outs = [torch.empty_like(x) for x in a[:3]] + [torch.empty(1 + 3 * seqs, dtype=torch.int32, device="cuda"), i32([77])]
+        torch.cuda.synchronize()
+        cache = cache_ops._PAGED.pack(pool.data_ptr(), a[0].data_ptr(), a[1].data_ptr(), 0, 1, 1, 1, 64, 16, seqs, 1)
+        args = (cache, a[2].data_ptr(), a[3].data_ptr(), *(x.data_ptr() for x in outs), st.cuda_stream)
+        codes = {lib.river_pages_reorder(*args) for _ in range(20000)}
+        st.synchronize()
+        if codes != {0} or outs[4].item():
+            failures.append((seqs, codes))
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in (8192, 2048, 8192, 2048)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
