@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <utility>
+
 #include "../../include/river.h"
 #include "river_common.cuh"
 
@@ -35,7 +37,21 @@ inline int paged_check(const river_paged *c, bool need_pool, bool need_lens, Pag
     return RIVER_OK;
 }
 
-inline int launch_rc() { return cudaGetLastError() == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE; }
+// What a runtime call of this call answered.  A failure is taken out of the runtime's record, where another call would find it as its own.
+inline int cuda_rc(cudaError_t e) {
+    if (e == cudaSuccess) return RIVER_OK;
+    cudaGetLastError();
+    return RIVER_E_DEVICE;
+}
+// grid x block threads of a kernel, with nothing else to its launch
+template <class... P, class... A>
+int launch_plain(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t st, A &&...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.stream = st;
+    return cuda_rc(cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...));
+}
 
 template <class T> __device__ __forceinline__ float to_f(T x);
 template <> __device__ __forceinline__ float to_f<float>(float x) { return x; }

@@ -409,10 +409,10 @@ __global__ void __launch_bounds__(256) pages_copy_kernel(const PagesArgs a, int 
 template <class K>
 int launch_deciding(K kernel, const PagesArgs &a, size_t work, size_t smem, cudaStream_t st) {
     const unsigned ctas = work <= 4 * kPgThreads ? 1 : work < (1u << 18) ? kPgCtas : 2 * kPgCtas;
-    if (ctas > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return RIVER_E_DEVICE;
+    if (ctas > 8 && cuda_rc(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1))) return RIVER_E_DEVICE;
     // the limit belongs to the kernel, not to the call: whoever sets it sets the same one, or a launch of another thread could fail by it
     constexpr int most = kPgSeqInts * sizeof(int) * kPgSeqs;
-    if (smem > (32u << 10) && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return RIVER_E_DEVICE;
+    if (smem > (32u << 10) && cuda_rc(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most))) return RIVER_E_DEVICE;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim = {ctas, 1, 1};
@@ -423,7 +423,7 @@ int launch_deciding(K kernel, const PagesArgs &a, size_t work, size_t smem, cuda
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = ctas > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
+    return cuda_rc(cudaLaunchKernelEx(&cfg, kernel, a));
 }
 // `most`: heads' worth of copies that there may be
 int launch_copy(const PagesArgs &a, int triples, int64_t most, cudaStream_t st) {
@@ -436,7 +436,7 @@ int launch_copy(const PagesArgs &a, int triples, int64_t most, cudaStream_t st) 
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, pages_copy_kernel, a, triples) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
+    return cuda_rc(cudaLaunchKernelEx(&cfg, pages_copy_kernel, a, triples));
 }
 
 }  // namespace

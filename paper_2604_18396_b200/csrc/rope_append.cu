@@ -223,24 +223,21 @@ bool rope_wide(const RopeArgs &a, size_t es) {
 }
 
 template <class TI, class TC, bool INTER>
-void launch_rope(const RopeArgs &a, cudaStream_t st) {
+int launch_rope(const RopeArgs &a, cudaStream_t st) {
     const bool wide = rope_wide(a, sizeof(TI));
-    if (!wide || (!INTER && a.rot % 16)) {  // (8192 tokens of 48 heads of 128, bf16, half layout, a turned part of 34: 93 us; of 128, in units, 37)
-        rope_append_any_kernel<TI, TC, INTER><<<a.n_tokens, 256, 0, st>>>(a, wide);
-        return;
-    }
+    if (!wide || (!INTER && a.rot % 16))  // (8192 tokens of 48 heads of 128, bf16, half layout, a turned part of 34: 93 us; of 128, in units, 37)
+        return launch_plain(rope_append_any_kernel<TI, TC, INTER>, a.n_tokens, 256, st, a, (int)wide);
     constexpr int UNITS = (INTER ? 24 : 12) / (int)sizeof(TI);
     const int per = INTER ? a.c.dh / 8 : a.rot / 16 + (a.c.dh - a.rot) / 8, rows = a.Hq + 2 * a.c.Hkv;
     // Few tokens: a CTA each, with all the threads that its rows keep busy.  Many: CTAs of 64 threads, which take turns at fetching, turning and
     // storing (8192 tokens of 48 heads of 128, us with 64, 128, 256 threads: from fp32 49, 54, 58; interleaved bf16 39, 40, 42; half 41, 42, 40).
     const bool few = a.n_tokens < 148 * 4;
     const int most = few ? 256 : 64, y = few ? std::min(most / per, rows) : std::min(most / per, (rows + UNITS - 1) / UNITS), z = few ? 1 : std::min(std::max(1, most / (per * y)), kRopeTokens);
-    rope_append_kernel<TI, TC, INTER, UNITS><<<(a.n_tokens + z - 1) / z, dim3(per, y, z), 0, st>>>(a);
+    return launch_plain(rope_append_kernel<TI, TC, INTER, UNITS>, (a.n_tokens + z - 1) / z, dim3(per, y, z), st, a);
 }
 template <class TI, class TC>
-void launch_rope(const RopeArgs &a, bool inter, cudaStream_t st) {
-    if (inter) launch_rope<TI, TC, true>(a, st);
-    else launch_rope<TI, TC, false>(a, st);
+int launch_rope(const RopeArgs &a, bool inter, cudaStream_t st) {
+    return inter ? launch_rope<TI, TC, true>(a, st) : launch_rope<TI, TC, false>(a, st);
 }
 
 }  // namespace
@@ -317,9 +314,6 @@ extern "C" int river_rope_append(const river_paged *c, int layer, int n_tokens, 
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const bool bf = c->dtype == RIVER_BF16, wide = in_dtype == RIVER_F32;
-    if (bf && wide) launch_rope<float, __nv_bfloat16>(a, interleaved != 0, st);
-    else if (bf) launch_rope<__nv_bfloat16, __nv_bfloat16>(a, interleaved != 0, st);
-    else if (wide) launch_rope<float, __half>(a, interleaved != 0, st);
-    else launch_rope<__half, __half>(a, interleaved != 0, st);
-    return launch_rc();
+    if (bf) return wide ? launch_rope<float, __nv_bfloat16>(a, interleaved != 0, st) : launch_rope<__nv_bfloat16, __nv_bfloat16>(a, interleaved != 0, st);
+    return wide ? launch_rope<float, __half>(a, interleaved != 0, st) : launch_rope<__half, __half>(a, interleaved != 0, st);
 }

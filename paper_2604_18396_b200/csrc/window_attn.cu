@@ -12,7 +12,7 @@ template <class T, int DH>
 int launch_step(const WindowArgs &a, int splits, cudaStream_t st) {
     const int64_t ctas = (int64_t)splits * a.c.Hkv * ((a.Hq / a.c.Hkv + 7) / 8) * a.max_q * a.c.n_seqs;
     if (ctas > INT32_MAX) return RIVER_E_SHAPE;
-    if (splits > 8 && cudaFuncSetAttribute(window_attn_step_kernel<T, DH>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return RIVER_E_DEVICE;
+    if (splits > 8 && cuda_rc(cudaFuncSetAttribute(window_attn_step_kernel<T, DH>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1))) return RIVER_E_DEVICE;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim = {(unsigned)splits, 1, 1};
@@ -22,14 +22,14 @@ int launch_step(const WindowArgs &a, int splits, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = splits > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, window_attn_step_kernel<T, DH>, a, splits) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
+    return cuda_rc(cudaLaunchKernelEx(&cfg, window_attn_step_kernel<T, DH>, a, splits));
 }
 
 template <class T, int DH, bool SPLIT>
 int launch_prompt(const PromptArgs &pa, const CUtensorMap &map, cudaStream_t st) {
     const WindowArgs &a = pa.w;
     const size_t smem = window_attn_prompt_smem();
-    if (cudaFuncSetAttribute(window_attn_prompt_kernel<T, DH, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return RIVER_E_DEVICE;
+    if (cuda_rc(cudaFuncSetAttribute(window_attn_prompt_kernel<T, DH, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem))) return RIVER_E_DEVICE;
     const int span = kWpRows / (a.Hq / a.c.Hkv) * pa.tiles;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
@@ -41,7 +41,7 @@ int launch_prompt(const PromptArgs &pa, const CUtensorMap &map, cudaStream_t st)
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = SPLIT ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, window_attn_prompt_kernel<T, DH, SPLIT>, map, pa) == cudaSuccess ? RIVER_OK : RIVER_E_DEVICE;
+    return cuda_rc(cudaLaunchKernelEx(&cfg, window_attn_prompt_kernel<T, DH, SPLIT>, map, pa));
 }
 template <class T, int DH>
 int launch_prompt(const PromptArgs &pa, cudaStream_t st) {
@@ -98,7 +98,6 @@ extern "C" int river_window_attention(const river_paged *c, int layer, int n_tok
     a.out = out;
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const int rc = c->dtype == RIVER_BF16 ? (c->dh == 64 ? launch<__nv_bfloat16, 64>(a, st) : launch<__nv_bfloat16, 128>(a, st))
-                                          : (c->dh == 64 ? launch<__half, 64>(a, st) : launch<__half, 128>(a, st));
-    return rc ? rc : launch_rc();
+    return c->dtype == RIVER_BF16 ? (c->dh == 64 ? launch<__nv_bfloat16, 64>(a, st) : launch<__nv_bfloat16, 128>(a, st))
+                                  : (c->dh == 64 ? launch<__half, 64>(a, st) : launch<__half, 128>(a, st));
 }

@@ -1,5 +1,6 @@
 """The operators on a caller's paged cache at their ends: calls without tokens, threads, errors left by others, small probabilities and infinities
 in f16, status words, lengths and starts that cannot be, and launches that only large or unaligned calls take (needs a B200)."""
+import ctypes as C
 import threading
 
 import pytest
@@ -59,3 +60,34 @@ def test_reorderings_of_several_threads():
     for t in threads:
         t.join()
     assert not failures, failures
+
+
+def test_a_launch_that_failed_is_not_the_next_calls_error():
+    """A launch into a capture that has been broken off is refused; calls on other streams know nothing of it."""
+    cu, lib = C.CDLL("libcuda.so.1"), binding.load()
+    st = torch.cuda.Stream()
+    handle, graph = C.c_void_p(st.cuda_stream), C.c_void_p()
+    a = [i32([[0, -1]]), i32([3]), i32([1, 0]), i32([1])]
+    outs = [torch.empty_like(x) for x in a[:3]] + [i32([77])]
+    k, q = torch.randn(1, 2, 64, device="cuda").to(BF), torch.randn(1, 2, 64, device="cuda").to(BF)
+    out, zero, f, start = torch.empty_like(q), i32([0]), freq(64), i32([0, 1])
+    par, reordered = i32([0]), [torch.empty_like(x) for x in a[:3]] + [i32([77])]
+    copies = torch.empty(4, dtype=torch.int32, device="cuda")
+    p2 = torch.zeros(1, 2, 2, 2, 16, 64, dtype=BF, device="cuda")
+    c_adv = cache_ops._PAGED.pack(0, a[0].data_ptr(), a[1].data_ptr(), 0, 1, 2, 1, 64, 16, 1, 2)
+    c_pool = cache_ops._PAGED.pack(p2.data_ptr(), a[0].data_ptr(), a[1].data_ptr(), 0, 1, 2, 2, 64, 16, 1, 2)
+    calls = {
+        "advance": lambda s: lib.river_pages_advance(c_adv, a[2].data_ptr(), a[3].data_ptr(), 0, 0, *(x.data_ptr() for x in outs), s),
+        "reorder": lambda s: lib.river_pages_reorder(c_pool, a[2].data_ptr(), par.data_ptr(), *(x.data_ptr() for x in reordered[:3]), copies.data_ptr(), reordered[3].data_ptr(), s),
+        "rope": lambda s: lib.river_rope_append(c_pool, 1, 1, 0, 0, None, cache_ops._rows(k, 0, "k"), cache_ops._rows(k, 0, "v"), zero.data_ptr(), zero.data_ptr(), f.data_ptr(), 64, 0, 1.0, 0, 0, s),
+        "attention": lambda s: lib.river_window_attention(c_pool, 1, 1, 1, start.data_ptr(), 2, cache_ops._rows(q, 0, "q"), 8, 0, 0.125, out.data_ptr(), 0, s),
+    }
+    torch.cuda.synchronize()
+    for name, call in calls.items():
+        assert cu.cuStreamBeginCapture_v2(handle, 2) == 0
+        assert cu.cuStreamSynchronize(handle) != 0  # (not allowed: the capture is invalid from here on)
+        assert call(st.cuda_stream) == -6, name
+        assert cu.cuStreamEndCapture(handle, C.byref(graph)) != 0
+        for other in calls.values():
+            assert other(0) == 0, name
+    torch.cuda.synchronize()
