@@ -360,12 +360,19 @@ int river_rope_append(const river_paged *c, int layer, int n_tokens, int Hq, int
  *   status        [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as
  *                 not visible), q_start descends, a length is more than a row of the
  *                 table holds (it counts as that), or a sequence has more than max_q queries (the rows of that sequence behind the
- *                 max_q-th may stay as they are); RIVER_E_TIMEOUT when a wait ran out.
+ *                 max_q-th may stay as they are); RIVER_E_TIMEOUT when a wait ran out (the rows that were waited for stay as they are).
  * Positions that a query does not see have no influence on its result, whatever the pool holds there.  Every result follows in a
  * fixed order of sums: the same inputs give the same bits. */
 int river_window_attention(const river_paged *c, int layer, int n_tokens, int max_q, const int32_t *q_start, int Hq,
                            const river_rows *q, int window, int sinks, float softmax_scale, void *out, int32_t *status,
                            void *cuda_stream);
+
+/* Self-test of the bounded waits in river_window_attention's kernel of prompts: the same call by that kernel, the keys of a row shared out
+ * over `splits` (1, 2, 4) CTAs, where the CTAs of KV head 0 that hold the first keys never ask for them.  Their waits give up after poll_limit
+ * (1 .. 2^20) polls: status receives RIVER_E_TIMEOUT, the rows of that KV head's query heads stay as they are, the others are as ever. */
+int river_selftest_window_timeout(const river_paged *c, int layer, int n_tokens, int max_q, const int32_t *q_start, int Hq,
+                                  const river_rows *q, int window, int sinks, float softmax_scale, void *out, int32_t *status, int splits,
+                                  int poll_limit, void *cuda_stream);
 
 /* The pages of a cache, kept on the device: refs[p] counts the table entries (and whatever else the caller counts) that hold page p, 0 =
  * free.  Every call reads a state (table, lens, refs) and writes the state behind it (table_out, lens_out, refs_out); n_seqs <= 8192.

@@ -60,7 +60,7 @@ EXPORTS = ("river_argmax_noalloc", "river_profile", "river_profile_read", "river
            "river_release", "river_stats", "river_destroy", "river_last_error", "river_clear_device_error",
            "river_selftest_wait_timeout", "river_attention", "river_project_kv", "river_quantize_w4", "river_generate", "river_offload", "river_exit_histogram",
            "river_suggest_offload", "river_rope_frequencies", "river_rope_append", "river_window_attention", "river_pages_advance",
-           "river_pages_reorder", "river_pages_compact")
+           "river_pages_reorder", "river_pages_compact", "river_selftest_window_timeout")
 
 _lib = None
 
@@ -106,6 +106,7 @@ def load():
     L.river_rope_frequencies.argtypes = [C.c_int, C.c_double, vp, vp, vp]
     L.river_rope_append.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp, vp, vp, vp, C.c_int, C.c_int, C.c_float, vp, vp, vp]
     L.river_window_attention.argtypes = [vp, C.c_int, C.c_int, C.c_int, vp, C.c_int, vp, C.c_int, C.c_int, C.c_float, vp, vp, vp]
+    L.river_selftest_window_timeout.argtypes = L.river_window_attention.argtypes[:-1] + [C.c_int, C.c_int, vp]
     L.river_pages_advance.argtypes = [vp, vp, vp, C.c_int, C.c_int, vp, vp, vp, vp, vp]
     L.river_pages_reorder.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.river_pages_compact.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]

@@ -62,7 +62,7 @@ template <> __device__ __forceinline__ __half from_f<__half>(float x) { return _
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 __device__ __forceinline__ void flag(int32_t *status, int code) {
-    if (status) atomicExch(status, code);
+    if (status) atomicMin(status, code);  // (a wait that ran out, RIVER_E_TIMEOUT, is not hidden by another CTA's RIVER_E_BADARG)
 }
 
 }  // namespace river

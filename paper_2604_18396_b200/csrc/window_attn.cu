@@ -67,6 +67,33 @@ int launch(const WindowArgs &a, cudaStream_t st) {
     return step_us <= prompt_us ? launch_step<T, DH>(a, splits, st) : launch_prompt<T, DH>(pa, st);
 }
 
+// The arguments of a call, checked.  RIVER_OK with a->n_tokens or a->max_q 0: nothing is to be done.
+int window_args(const river_paged *c, int layer, int n_tokens, int max_q, const int32_t *q_start, int Hq, const river_rows *q, int window, int sinks,
+                float softmax_scale, void *out, int32_t *status, WindowArgs *a) {
+    if (const int rc = paged_check(c, true, true, &a->c)) return rc;
+    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || max_q < 0 || !q_start || window < 1 || sinks < 0) return RIVER_E_BADARG;
+    if (Hq < 1 || Hq % c->Hkv || !std::isfinite(softmax_scale)) return RIVER_E_BADARG;
+    if (c->n_seqs > 65535 || Hq > 8192 || (int64_t)c->n_seqs * Hq > (1 << 26)) return RIVER_E_SHAPE;  // (the kernels' grids)
+    a->layer0 = layer - 1;
+    a->n_tokens = n_tokens;
+    a->max_q = std::min(max_q, n_tokens);
+    a->Hq = Hq;
+    a->window = window;
+    a->sinks = sinks;
+    a->q_start = q_start;
+    a->scale_log2 = softmax_scale * 1.4426950408889634f;
+    a->out = out;
+    a->status = status;
+    if (n_tokens == 0) return RIVER_OK;  // (rows that are none may have no address)
+    if (!q || !q->p || !out || !aligned_to(out, 16)) return RIVER_E_BADARG;
+    // heads are read 16 bytes at a time
+    if (!aligned_to(q->p, 16) || q->token % 8 || q->head % 8) return RIVER_E_BADARG;
+    a->q = q->p;
+    a->q_tok = q->token;
+    a->q_head = q->head;
+    return RIVER_OK;
+}
+
 }  // namespace
 }  // namespace river
 
@@ -75,29 +102,23 @@ extern "C" int river_window_attention(const river_paged *c, int layer, int n_tok
                                       void *cuda_stream) {
     using namespace river;
     WindowArgs a;
-    if (const int rc = paged_check(c, true, true, &a.c)) return rc;
-    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || max_q < 0 || !q_start || window < 1 || sinks < 0) return RIVER_E_BADARG;
-    if (Hq < 1 || Hq % c->Hkv || !std::isfinite(softmax_scale)) return RIVER_E_BADARG;
-    if (c->n_seqs > 65535 || Hq > 8192 || (int64_t)c->n_seqs * Hq > (1 << 26)) return RIVER_E_SHAPE;  // (the kernels' grids)
-    if (n_tokens == 0) return RIVER_OK;  // (rows that are none may have no address)
-    if (!q || !q->p || !out || !aligned_to(out, 16)) return RIVER_E_BADARG;
-    // heads are read 16 bytes at a time
-    if (!aligned_to(q->p, 16) || q->token % 8 || q->head % 8) return RIVER_E_BADARG;
-    if (max_q == 0) return RIVER_OK;
-    a.layer0 = layer - 1;
-    a.n_tokens = n_tokens;
-    a.max_q = max_q < n_tokens ? max_q : n_tokens;
-    a.Hq = Hq;
-    a.window = window;
-    a.sinks = sinks;
-    a.q_start = q_start;
-    a.q = q->p;
-    a.q_tok = q->token;
-    a.q_head = q->head;
-    a.scale_log2 = softmax_scale * 1.4426950408889634f;
-    a.out = out;
-    a.status = status;
+    if (const int rc = window_args(c, layer, n_tokens, max_q, q_start, Hq, q, window, sinks, softmax_scale, out, status, &a)) return rc;
+    if (a.n_tokens == 0 || a.max_q == 0) return RIVER_OK;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return c->dtype == RIVER_BF16 ? (c->dh == 64 ? launch<__nv_bfloat16, 64>(a, st) : launch<__nv_bfloat16, 128>(a, st))
                                   : (c->dh == 64 ? launch<__half, 64>(a, st) : launch<__half, 128>(a, st));
+}
+
+extern "C" int river_selftest_window_timeout(const river_paged *c, int layer, int n_tokens, int max_q, const int32_t *q_start, int Hq,
+                                             const river_rows *q, int window, int sinks, float softmax_scale, void *out, int32_t *status,
+                                             int splits, int poll_limit, void *cuda_stream) {
+    using namespace river;
+    WindowArgs a;
+    if (const int rc = window_args(c, layer, n_tokens, max_q, q_start, Hq, q, window, sinks, softmax_scale, out, status, &a)) return rc;
+    if (a.n_tokens == 0 || a.max_q == 0 || (splits != 1 && splits != 2 && splits != 4) || poll_limit < 1 || poll_limit > (1 << 20)) return RIVER_E_BADARG;
+    if (Hq / c->Hkv > kWpRows) return RIVER_E_SHAPE;
+    PromptArgs pa = {a, 2, splits, (uint32_t)poll_limit, 0};
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return c->dtype == RIVER_BF16 ? (c->dh == 64 ? launch_prompt<__nv_bfloat16, 64>(pa, st) : launch_prompt<__nv_bfloat16, 128>(pa, st))
+                                  : (c->dh == 64 ? launch_prompt<__half, 64>(pa, st) : launch_prompt<__half, 128>(pa, st));
 }

@@ -34,6 +34,8 @@ struct PromptArgs {
     WindowArgs w;
     int tiles;   // query tiles of a CTA: 1 or 2
     int splits;  // CTAs that share out the keys of a row, a cluster
+    uint32_t polls = kWaitLimit;  // of a wait, before it gives up
+    int mute = -1;                // self-test: the KV head whose first keys nobody asks for, so that waits run out
 };
 
 __device__ __forceinline__ void wp_ld32(uint32_t taddr, uint32_t (&r)[32]) {  // left under way (wp_ld_wait)
@@ -78,15 +80,14 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
     return r != 0;
 }
-// Bounded wait.  Where it runs out the kernel goes on with whatever is there, every later wait ends at once, and no result is stored:
-// nobody is left standing at a barrier.
-__device__ __forceinline__ void wp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *err) {
-    for (uint32_t it = 0; it < kWaitLimit; ++it) {
+// Bounded wait.  Where it runs out the kernel goes on with whatever is there, every later wait ends at once, nothing more is loaded and no
+// result of the CTA and its cluster is stored: nobody is left standing at a barrier.
+__device__ __forceinline__ void wp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t polls = kWaitLimit) {
+    for (uint32_t it = 0; it < polls; ++it) {
         if (mbar_try_wait(bar, parity & 1u)) return;
         if (*abort_flag) return;
     }
     *abort_flag = 1;
-    atomicExch(err, DEV_WAIT_TIMEOUT);
 }
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     // S done, P written (2), O done; Q there
     __shared__ uint64_t bars[16];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort, s_err, s_poison, s_missing;
+    __shared__ int s_abort, s_no_page, s_poison, s_missing;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int gq = a.Hq / a.c.Hkv, per = kWpRows / gq;  // tokens of a tile
     // heavy tiles, those behind a long history, first
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     const uint32_t b_first = smem_u32(&bars[0]), b_full = b_first + 8, b_free = b_full + 32, b_s = b_free + 16, b_p = b_s + 16, b_o = b_p + 32, b_q = b_o + 16;
     volatile int *abortp = &s_abort;
     if (tid == 0) {
-        s_abort = s_err = s_poison = s_missing = 0;
+        s_abort = s_no_page = s_poison = s_missing = 0;
         for (int i = 0; i < 16; ++i) mbar_init(smem_u32(&bars[i]), i >= 9 && i < 13 ? 4 : i == 15 ? 8 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -212,12 +213,13 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             // K of tile j + 1 comes together with V of tile j
             int page = -1;  // of tile j
             uint32_t bytes = 0;
-            for (int j = -1; j < n_kt; ++j) {
+            for (int j = pa.mute == kvh && t0 == 0 ? n_kt : -1; j < n_kt; ++j) {
                 const int next = ahead;  // of tile j + 1
                 ahead = blk < 8 ? page_of(8 * (t0 + j + 2) + blk) : -1;  // (under way while this tile waits for its place)
-                if (blk < 8 && 8 * (t0 + j + 1) + blk < nb && next < 0) s_err = DEV_BAD_PAGE;
+                if (blk < 8 && 8 * (t0 + j + 1) + blk < nb && next < 0) s_no_page = 1;
                 const uint32_t k_bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, next >= 0)) * 2048u, bar = j < 0 ? b_first : b_full + 8 * (j & 3);
-                if (j >= 2) wp_wait(b_free + 8 * (j & 1), (j >> 1) - 1, abortp, &s_err);
+                if (j >= 2) wp_wait(b_free + 8 * (j & 1), (j >> 1) - 1, abortp, pa.polls);
+                if (__any_sync(0xffffffffu, *abortp)) break;
                 if (lane == 0) mbar_expect_tx(bar, bytes + k_bytes);
                 __syncwarp();
                 load(sk + place * NB * KB, next, j + 1, 0, bar);
@@ -237,8 +239,8 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 tc_commit(b_s + 8 * q);
             };
             if (n_t > 0) {
-                wp_wait(b_q, 0, abortp, &s_err);
-                wp_wait(b_first, 0, abortp, &s_err);
+                wp_wait(b_q, 0, abortp, pa.polls);
+                wp_wait(b_first, 0, abortp, pa.polls);
                 tc_fence_after();
                 if (leader) {
                     scores(0, dk);
@@ -249,13 +251,13 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             for (int j = 0; j < n_t; ++j) {
                 place = place == 2 ? 0 : place + 1;  // of K of the next tile
                 const uint64_t v = dv + (j & 1) * (NB * KB >> 4), k_desc = dk + place * (NB * KB >> 4);
-                wp_wait(b_full + 8 * (j & 3), j >> 2, abortp, &s_err);
+                wp_wait(b_full + 8 * (j & 3), j >> 2, abortp, pa.polls);
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     if (q == 1 && n_q == 1) break;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {  // half of the keys
-                        wp_wait(b_p + 8 * (2 * q + h), j, abortp, &s_err);
+                        wp_wait(b_p + 8 * (2 * q + h), j, abortp, pa.polls);
                         tc_fence_after();
                         if (leader) {
 #pragma unroll
@@ -301,7 +303,6 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             asm volatile("bar.sync 1, 256;" ::: "memory");  // (s_missing)
         }
         const int q = (warp - 4) >> 2, r = 32 * (warp & 3) + lane, p = q * per + r / gq;
-        bool live = r < per * gq && p < n_tok;
         float m = -CUDART_INF_F, l = 0.f;
         if (q < nq) {
             const int pos = pos0 + min(p, n_tok - 1);
@@ -323,7 +324,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                     part = part || valid != 0xffu;
                 }
                 if (part && q == 0) {  // thread = V row: those that nobody sees become zero, the others are looked through
-                    wp_wait(b_full + 8 * (j & 3), j >> 2, abortp, &s_err);
+                    wp_wait(b_full + 8 * (j & 3), j >> 2, abortp, pa.polls);
                     const int cc = c0 + r;
                     uint8_t *row = sv + (j & 1) * NB * KB + r * 128;
                     if ((valid >> (r >> 4) & 1u) && (cc < all_sink || (cc >= all_lo && cc < all_hi))) {
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                wp_wait(b_s + 8 * q, j, abortp, &s_err);
+                wp_wait(b_s + 8 * q, j, abortp, pa.polls);
                 __syncwarp();
                 tc_fence_after();
                 uint32_t s[4][32];
@@ -423,12 +424,11 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 f2_unpack(sum, l0, l1);
                 l += l0 + l1;
             }
-            if (n_kt > 0) wp_wait(b_o + 8 * q, 0, abortp, &s_err);
+            if (n_kt > 0) wp_wait(b_o + 8 * q, 0, abortp, pa.polls);
             __syncwarp();
             tc_fence_after();
             if constexpr (!SPLIT) {
                 const bool none = m == -CUDART_INF_F;  // (no key seen: O may be 0 x whatever)
-                live = live && !*abortp;
                 const float inv = none ? 0.f : 1.f / l;
                 uint4 *const mine = reinterpret_cast<uint4 *>(sq + q * NB * QB);  // (rows through the place of this tile's Q: whole lines of them go out)
                 constexpr int C8 = DH / 8;
@@ -486,15 +486,17 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
         tc_fence_after();
         tc_dealloc(tmem, 512u);
     }
-    if (tid == 0 && s_err) flag(a.status, s_err == DEV_WAIT_TIMEOUT ? RIVER_E_TIMEOUT : RIVER_E_BADARG);
+    bool gave_up = *abortp != 0;
+    if (tid == 0 && (gave_up || s_no_page)) flag(a.status, gave_up ? RIVER_E_TIMEOUT : RIVER_E_BADARG);
     if constexpr (SPLIT) {
         // ---- the cluster's parts of a row, a row (dh 64: two) per warp: every CTA finishes its share of the rows.  (Not warps 0 .. 3, which have
         // few registers left.)
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
+        for (int k = 0; k < splits; ++k) gave_up = gave_up || *cluster.map_shared_rank(&s_abort, k) != 0;
         constexpr int L = DH / 4;  // lanes of a row
         const int rows = nq * kWpRows, mine = (rows + splits - 1) / splits;
-        for (int i = (warp - 4) * (32 / L) + lane / L; warp >= 4 && i < mine; i += 256 / L) {
+        for (int i = (warp - 4) * (32 / L) + lane / L; warp >= 4 && !gave_up && i < mine; i += 256 / L) {
             const int rr = split * mine + i, r = rr % kWpRows, t = rr / kWpRows * per + r / gq;
             if (rr >= rows || r >= per * gq || t >= n_tok) continue;
             const int chunk = lane % L;
@@ -525,7 +527,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
         }
         cluster.sync();  // (peers read this CTA's part; and no row is written any more)
     }
-    if (s_poison && warp >= 4)
+    if (s_poison && warp >= 4 && !gave_up)
 #pragma unroll 1
         for (int r = warp - 4; r < n_tok * gq; r += 8) window_attn_row<T, DH>(a, tok0 + r / gq, kvh * gq + r % gq, seq, pos0 + r / gq);
 }

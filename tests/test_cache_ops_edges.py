@@ -1,6 +1,9 @@
 """Calls of the operators on a paged cache at their ends, as far as the host alone decides (no GPU)."""
+import ctypes as C
+
 import pytest
 
+from paper_2604_18396_b200 import cache_ops
 from tests import test_cache_ops_checks as checks
 
 lib = checks.lib
@@ -17,3 +20,11 @@ def test_calls_without_tokens_are_checked_all_the_same(lib, kw):
     assert checks.rope(lib, n=0, q=NONE, k=NONE, v=NONE, pos=0, seqs=0, out=0, **kw) == -1
     if "layer" in kw:
         assert checks.attn(lib, n=0, q=NONE, out=0, **kw) == -1 and checks.attn(lib, n=0, q=NONE, out=0, window=0) == -1
+
+
+def test_the_self_test_of_waits_refuses_what_it_cannot_run(lib):
+    def call(splits=1, polls=1000, n=4, hq=4, c=None):
+        return lib.river_selftest_window_timeout(C.byref(c or checks.paged()), 1, n, 2, checks.P, hq, C.byref(cache_ops.river_rows(checks.P, 256, 64)),
+                                                 8, 0, 1.0, checks.P, 0, splits, polls, 0)
+    assert [call(splits=x) for x in (0, 3, 8)] == [-1] * 3 and [call(polls=x) for x in (0, -1, (1 << 20) + 1)] == [-1] * 3
+    assert call(n=0) == -1 and call(hq=3) == -1 and call(hq=258) == -2 and call(c=checks.paged(dh=96)) == -2

@@ -10,7 +10,8 @@ from paper_2604_18396_b200 import binding, cache_ops, rope_append, window_attent
 from tests import paged_reference as ref
 
 pytestmark = pytest.mark.gpu
-BF = torch.bfloat16
+BF, F16 = torch.bfloat16, torch.float16
+NAN = float("nan")
 
 
 def i32(v):
@@ -91,3 +92,26 @@ def test_a_launch_that_failed_is_not_the_next_calls_error():
         for other in calls.values():
             assert other(0) == 0, name
     torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------- a wait that runs out
+@pytest.mark.parametrize("splits", [1, 2, 4])
+@pytest.mark.parametrize("dtype,dh", [(BF, 128), (F16, 64)])
+def test_a_wait_that_runs_out_stores_no_row(splits, dtype, dh):
+    """CTAs that never ask for their keys: their waits end, the status says so, and no row of their clusters is stored."""
+    lib, hq, hkv = binding.load(), 4, 2
+    pool, table, lens = ref.cache([600, 300], 16, hkv, dh, dtype, 7)
+    q = torch.randn(300, hq, dh, generator=torch.Generator().manual_seed(8)).to(dtype).cuda()
+    starts = [0, 200, 300]
+    want, tol = ref.attention(q, starts, pool, 1, table, [600, 300], 400, 4, 0.125)
+    cache, q_start = cache_ops._PAGED.pack(pool.data_ptr(), table.data_ptr(), lens.data_ptr(), cache_ops._TYPES[dtype], 1, pool.shape[1], hkv, dh, 16, 2, table.shape[1]), i32(starts)
+    for status in (i32([0]), None):
+        out = torch.full_like(q, NAN)
+        rc = lib.river_selftest_window_timeout(cache, 1, 300, 200, q_start.data_ptr(), hq, cache_ops._rows(q, 0, "q"), 400, 4, 0.125, out.data_ptr(),
+                                               status.data_ptr() if status is not None else 0, splits, 2000, torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert rc == 0 and (status is None or status.item() == -7)
+        assert out[:, :2].isnan().all() and ((out.double() - want).abs() <= tol)[:, 2:].all()
+    out, status = torch.full_like(q, NAN), i32([0])  # and the kernel is none the worse for it
+    window_attention(q, out, q_start, pool, 1, table, lens, window=400, sinks=4, max_q=200, softmax_scale=0.125, status=status)
+    assert status.item() == 0 and ((out.double() - want).abs() <= tol).all()
