@@ -20,7 +20,7 @@
 //
 // Hidden positions: scores are replaced, not added to; V rows that no row of the CTA sees are set to zero in shared memory.  A row of V
 // that some rows see and others do not is harmless as long as it is finite (0 x v); tiles that have such rows are looked through,
-// and where one holds no number the CTA computes its rows again one by one (window_attn_row).
+// and where one holds no number the CTA computes its rows again one by one (window_attn_row).  So it does for scores beyond kWpHuge.
 #pragma once
 #include "attn_prefill_tc.cuh"
 #include "window_attn_step.cuh"
@@ -28,6 +28,9 @@
 namespace river {
 
 constexpr int kWpRows = 128, kWpKeys = 128, kWpThreads = 384, kWpMaxSplits = 4;
+// Scores (log2) from which on the distance between a product and its rounded maximum, half a unit in the last place, is more than an exponent of P has
+// room for: a CTA with such a row computes its rows one by one, which compares rounded scores with one another.
+template <class T> constexpr float kWpHuge = std::is_same<T, __half>::value ? 8388608.f : 536870912.f;  // 2^23, 2^29
 constexpr float kWpLazy = 8.f;  // growth of a row's maximum (log2) that O waits for before it is rescaled
 
 struct PromptArgs {
@@ -313,6 +316,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + 128u * q + quarter, t_o = tmem + kO + (uint32_t)DH * q + quarter;
             const float c = fmaxf(fabsf(a.scale_log2), 1e-30f);  // (a scale of 0: every score 0, hidden ones -inf still)
             const bool missing = s_missing != 0;
+            auto huge = [&] { if (fabsf(m) > kWpHuge<T> && m != -CUDART_INF_F) s_poison = 1; };
             for (int j = 0; j < n_kt; ++j) {
                 const int c0 = 128 * (t0 + j);
                 uint32_t valid = 0xffu;  // blocks that are there
@@ -377,6 +381,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                         for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
                     const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
                     m = mx < CUDART_INF_F ? mx : CUDART_NAN_F;
+                    huge();
                 }
                 while (true) {
                     sum = 0ull;
@@ -389,9 +394,10 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                     const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
                     wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), sum, w);
                     const bool grow = !(mx <= m + kWpLazy) && !(m != m);  // (a maximum that is no number stays)
-                    if (!__any_sync(0xffffffffu, grow)) break;
                     const float corr = grow ? ex2(m - mx) : 1.f;
+                    if (!__any_sync(0xffffffffu, grow)) break;
                     if (grow) m = mx < CUDART_INF_F ? mx : CUDART_NAN_F;  // (inf - inf, as the formula has it)
+                    huge();
                     l *= corr;
                     if (j > 0) {  // (the MMAs that wrote O are complete: S of these keys was issued behind them)
 #pragma unroll 1

@@ -115,3 +115,22 @@ def test_a_wait_that_runs_out_stores_no_row(splits, dtype, dh):
     out, status = torch.full_like(q, NAN), i32([0])  # and the kernel is none the worse for it
     window_attention(q, out, q_start, pool, 1, table, lens, window=400, sinks=4, max_q=200, softmax_scale=0.125, status=status)
     assert status.item() == 0 and ((out.double() - want).abs() <= tol).all()
+
+
+# ---------------------------------------------------------------- f16
+@pytest.mark.parametrize("dtype", [F16, BF])
+@pytest.mark.parametrize("new", [1, 64, 300])
+def test_scores_of_many_millions(new, dtype):
+    """However coarse a float is at the scores' size, every probability is a number."""
+    n, dh, page = 700, 128, 16
+    pool, table, lens = ref.cache([n], page, 1, dh, dtype, 3, fill=0.0)
+    q = torch.ones(new, 2, dh, dtype=dtype, device="cuda")
+    q[:, 1] *= -1
+    for x in (500.0, 1000.0, 1901.0, 3001.0, 7777.0, 20000.0, 65000.0) + ((1e6, 1e9, 1e12) if dtype is BF else ()):
+        pool[:, :, 0] = -x
+        pool[0, table[0, 0].long(), 0, 0, 5] = x
+        pool[0, table[0, 20].long(), 0, 0, 3] = x
+        out = torch.full_like(q, NAN)
+        window_attention(q * x, out, i32([0, new]), pool, 1, table, lens, window=n, max_q=new)
+        want, tol = ref.attention(q * x, [0, new], pool, 1, table, [n], n, 0, dh ** -0.5)
+        assert ((out.double() - want).abs() <= tol).all(), x
