@@ -16,7 +16,8 @@
 // start and end.  8192 positions of the 8B class, window 4096: 407 us, 1.01 PFLOP/s of visible products (346 in a graph).
 //
 // P in 16 bits: its rounding weighs as much as the rounding of the result (2^-9 of sum p |v| against 2^-9 of the result in bf16, both
-// random), and one product instead of two is half of the tensor pipe's work.
+// random), and one product instead of two is half of the tensor pipe's work.  In f16 a probability below 2^-21 of the row's largest loses bits, and below
+// 2^-31 counts as 2^-31 or nothing (kWpBelow).
 //
 // Hidden positions: scores are replaced, not added to; V rows that no row of the CTA sees are set to zero in shared memory.  A row of V
 // that some rows see and others do not is harmless as long as it is finite (0 x v); tiles that have such rows are looked through,
@@ -32,6 +33,9 @@ constexpr int kWpRows = 128, kWpKeys = 128, kWpThreads = 384, kWpMaxSplits = 4;
 // room for: a CTA with such a row computes its rows one by one, which compares rounded scores with one another.
 template <class T> constexpr float kWpHuge = std::is_same<T, __half>::value ? 8388608.f : 536870912.f;  // 2^23, 2^29
 constexpr float kWpLazy = 8.f;  // growth of a row's maximum (log2) that O waits for before it is rescaled
+// f16 ends at 2^-24 below and 2^16 above: there a row's m, which its probabilities 2^(s - m), their sum and O refer to, lies this far below its
+// maximum, so that probabilities are as large as the type has room for beside the growth.
+constexpr float kWpBelow = 7.f;
 
 struct PromptArgs {
     WindowArgs w;
@@ -144,6 +148,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     namespace cg = cooperative_groups;
     const WindowArgs &a = pa.w;
     constexpr int NB = DH / 64;                                          // blocks of 64 dims
+    constexpr bool kHalf = std::is_same<T, __half>::value;
     constexpr uint32_t QB = kWpRows * 128, KB = kWpKeys * 128;           // bytes of one block of Q / of K or V
     constexpr uint32_t kO = 256;                                         // TMEM: tile q has S / P in columns 128 q .., O in 256 + DH q ..
     constexpr uint32_t kIdS = (1u << 4) | (sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) |
@@ -380,7 +385,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
                     const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
-                    m = mx < CUDART_INF_F ? mx : CUDART_NAN_F;
+                    m = mx < CUDART_INF_F ? (kHalf ? mx - kWpBelow : mx) : CUDART_NAN_F;
                     huge();
                 }
                 while (true) {
@@ -393,10 +398,17 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                         for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
                     const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
                     wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), sum, w);
-                    const bool grow = !(mx <= m + kWpLazy) && !(m != m);  // (a maximum that is no number stays)
-                    const float corr = grow ? ex2(m - mx) : 1.f;
+                    bool grow;
+                    float corr;
+                    if constexpr (kHalf) {  // (by the difference, which is exact where the two are near: no rounding of a large m makes P infinite)
+                        grow = !(mx - fmaxf(m, -3e38f) <= kWpLazy + kWpBelow) && !(m != m);
+                        corr = grow ? ex2(m - (mx - kWpBelow)) : 1.f;
+                    } else {
+                        grow = !(mx <= m + kWpLazy) && !(m != m);  // (a maximum that is no number stays)
+                        corr = grow ? ex2(m - mx) : 1.f;
+                    }
                     if (!__any_sync(0xffffffffu, grow)) break;
-                    if (grow) m = mx < CUDART_INF_F ? mx : CUDART_NAN_F;  // (inf - inf, as the formula has it)
+                    if (grow) m = mx < CUDART_INF_F ? (kHalf ? mx - kWpBelow : mx) : CUDART_NAN_F;  // (inf - inf, as the formula has it)
                     huge();
                     l *= corr;
                     if (j > 0) {  // (the MMAs that wrote O are complete: S of these keys was issued behind them)

@@ -7,7 +7,8 @@
 //                                      Q is loaded in the same order: no shared memory, no transposition.
 //   softmax                            online, fp32, base 2: a row lies with four lanes.
 //   O^T [dh x 8 heads] += V^T P^T      S in its accumulator layout is the B operand; the A operand pairs the values of two keys, which a
-//                                      byte permutation makes of two loaded rows.  P = hi + lo, so that it keeps 16 bits and more.
+//                                      byte permutation makes of two loaded rows.  P = hi + lo, so that it keeps 16 bits and more (f16:
+//                                      kStepScale; down to 2^-23 of the row's largest, and something of it down to 2^-39).
 // K of the next block is requested when S has been computed, V when O has: 8 KB (dh 128) per warp are under way all the time.
 //
 // Bound by HBM where rows are many: 128 rows of the 8B class, window 8192, 680 us with the host, 655 without (6.57 TB/s, the copy rate); one row by its chain
@@ -19,6 +20,8 @@
 #pragma once
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "window_attn_rows.cuh"
 
 namespace river {
@@ -26,6 +29,9 @@ namespace river {
 constexpr int kStepWarps = 4;
 constexpr int kStepCtas = 3;         // resident per SM (168 registers)
 constexpr int kStepMaxSplits = 16;   // CTAs of a cluster
+// P and its sum are held times kStepScale: f16 ends at 2^-24 below and 2^16 above, and p at most 1 would leave the upper part unused (32768 positions
+// of 2^-25 each counted in the sum but not in O).  bf16 has fp32's exponents.
+template <class T> constexpr float kStepScale = std::is_same<T, __half>::value ? 32768.f : 1.f;
 
 template <class T> __device__ __forceinline__ void mma_16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
 template <> __device__ __forceinline__ void mma_16<__nv_bfloat16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -174,7 +180,7 @@ __global__ void __launch_bounds__(32 * kStepWarps, kStepCtas) window_attn_step_k
         }
         const float base = m == -CUDART_INF_F ? 0.f : m;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) p[x] = ex2(p[x] - base);
+        for (int x = 0; x < 4; ++x) p[x] = ex2(p[x] - base) * kStepScale<T>;
         l += (p[0] + p[1]) + (p[2] + p[3]);
         uint32_t hi0, lo0, hi1, lo1;
         split_pair<T>(p[0], p[1], hi0, lo0);

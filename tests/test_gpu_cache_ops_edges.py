@@ -118,6 +118,25 @@ def test_a_wait_that_runs_out_stores_no_row(splits, dtype, dh):
 
 
 # ---------------------------------------------------------------- f16
+@pytest.mark.parametrize("new", [1, 64])
+def test_f16_many_weak_positions_beside_a_strong_one(new):
+    """32768 positions of 2^-25 each of the strongest weigh 2^-10 together.  A probability is kept to 2^-24 of the largest that the type
+    has room for: 2^-24 / 2^15 (single tokens), 2^-24 / 2^7 (prompts)."""
+    n, dh, page = 32768 + new, 64, 64
+    pool, table, lens = ref.cache([n], page, 1, dh, F16, 3, fill=0.0)
+    pool[:, :, 0], pool[:, :, 1] = 0.0, 1.0
+    first = table[0, 0].long()
+    pool[0, first, 0, 0, 0], pool[0, first, 1, 0, 0] = 2.175, 0.0
+    q = torch.ones(new, 2, dh, dtype=F16, device="cuda")
+    out, status = torch.full_like(q, NAN), i32([0])
+    window_attention(q, out, i32([0, new]), pool, 1, table, lens, window=n, max_q=new, status=status)
+    want, _ = ref.attention(q, [0, new], pool, 1, table, [n], n, 0, dh ** -0.5)
+    assert status.item() == 0 and 5e-4 < want.min().item() and want.max().item() < 2e-3
+    fp32 = 2 * (dh + 8) * 2.0 ** -24 * 64 * 2.175 / 8 + (n + 8) * 2.0 ** -23
+    tol = ref.U[F16] * want + fp32 * want + n * 2.0 ** -24 * 2.0 ** (-15 if new == 1 else -7) + ref.TINY[F16]
+    assert ((out.double() - want).abs() <= tol).all(), ((out.double() - want).abs() / tol).max().item()
+
+
 @pytest.mark.parametrize("dtype", [F16, BF])
 @pytest.mark.parametrize("new", [1, 64, 300])
 def test_scores_of_many_millions(new, dtype):
