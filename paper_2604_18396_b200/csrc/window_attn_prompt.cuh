@@ -17,7 +17,7 @@
 //
 // P in 16 bits: its rounding weighs as much as the rounding of the result (2^-9 of sum p |v| against 2^-9 of the result in bf16, both
 // random), and one product instead of two is half of the tensor pipe's work.  In f16 a probability below 2^-21 of the row's largest loses bits, and below
-// 2^-31 counts as 2^-31 or nothing (kWpBelow).
+// 2^-31 it counts as 2^-31 (kWpBelow).
 //
 // Hidden positions: scores are replaced, not added to; V rows that no row of the CTA sees are set to zero in shared memory.  A row of V
 // that some rows see and others do not is harmless as long as it is finite (0 x v); tiles that have such rows are looked through,
@@ -114,17 +114,23 @@ __device__ __forceinline__ int prompt_seq(const int32_t *q_start, int n_seqs, in
     return lo;
 }
 
+// max of two pairs of f16, what is no number handed on
+__device__ __forceinline__ uint32_t max2_f16_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 // max of three that hands on what is no number
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// Probabilities of 64 keys, w = 2^(s c - m) in pairs, and their sum on top of `sum`.  (The special-function units give 4 of them a cycle
+// Probabilities of 64 keys, w = 2^(s c - m) in pairs, and their sum on top of `sum`; in f16 each is at least that of `least`.  (The special-function units give 4 of them a cycle
 // and quarter of an SM: 1024 of a tile's 1900 cycles.  A quarter, an eighth of them by a polynomial instead cost more than they saved,
 // 160 -> 171, 167 us: with one warp of a query tile per quarter it is the length of its program that counts, not a unit's rate.)
 template <class T>
-__device__ __forceinline__ void wp_exps(const uint32_t (&a)[32], const uint32_t (&b)[32], uint64_t c2, uint64_t m2, uint64_t &sum, uint32_t (&w)[32]) {
+__device__ __forceinline__ void wp_exps(const uint32_t (&a)[32], const uint32_t (&b)[32], uint64_t c2, uint64_t m2, uint32_t least, uint64_t &sum, uint32_t (&w)[32]) {
     uint64_t part[2] = {sum, 0ull};
     float p[32][2];
 #pragma unroll
@@ -138,6 +144,7 @@ __device__ __forceinline__ void wp_exps(const uint32_t (&a)[32], const uint32_t 
     for (int e = 0; e < 32; ++e) {
         part[e & 1] = f2_add(part[e & 1], f2_pack(p[e][0], p[e][1]));
         w[e] = pack_pair<T>(p[e][0], p[e][1]);
+        if constexpr (std::is_same<T, __half>::value) w[e] = max2_f16_nan(w[e], least);
     }
     sum = f2_add(part[0], part[1]);
 }
@@ -336,7 +343,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                     wp_wait(b_full + 8 * (j & 3), j >> 2, abortp, pa.polls);
                     const int cc = c0 + r;
                     uint8_t *row = sv + (j & 1) * NB * KB + r * 128;
-                    if ((valid >> (r >> 4) & 1u) && (cc < all_sink || (cc >= all_lo && cc < all_hi))) {
+                    if (!kHalf && (valid >> (r >> 4) & 1u) && (cc < all_sink || (cc >= all_lo && cc < all_hi))) {
                         // (seen by every row: whatever it is, it belongs in every result)
                     } else if ((valid >> (r >> 4) & 1u) && (cc < any_sink || (cc >= any_lo && cc < any_hi))) {
                         // an exponent of ones (what is no number) and one more carries into the sign's place
@@ -377,6 +384,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 // far past it (a first tile, a rare later one) it is made again.
                 uint64_t sum;
                 uint32_t w[32];
+                // A probability that f16 has no number for would make 0 x inf of an infinite value: where every row sees every key it counts as 2^-24
+                // (2^-31 of the row's largest); tiles in parts are looked through.
+                const uint32_t least = part ? 0u : 0x00010001u;
                 const uint64_t c2 = f2_pack(c, c);
                 if (j == 0) {
                     float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
@@ -397,7 +407,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
                     const float mx = max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
-                    wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), sum, w);
+                    wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), least, sum, w);
                     bool grow;
                     float corr;
                     if constexpr (kHalf) {  // (by the difference, which is exact where the two are near: no rounding of a large m makes P infinite)
@@ -435,7 +445,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
                 wp_pin(s[3]);
                 {
                     const float base = m == -CUDART_INF_F ? 0.f : m;
-                    wp_exps<T>(s[2], s[3], c2, f2_pack(-base, -base), sum, w);
+                    wp_exps<T>(s[2], s[3], c2, f2_pack(-base, -base), least, sum, w);
                 }
                 hand_over(1);
                 float l0, l1;

@@ -15,8 +15,8 @@
 // (1B class, window 1024: 5.3 us): lengths, page ids, K, then the warps' and the CTAs' parts joined.
 //
 // Hidden positions: their scores are -inf and their values are zero in the operand (never loaded), so what the pool holds there
-// does not matter.  hi is rounded downwards from a little below p, so that lo is positive too: an infinite value that is seen
-// gives infinity and not 0 x inf.
+// does not matter.  hi is rounded downwards from a little below p, and both are at least the type's smallest number where p is not 0: an
+// infinite value that is seen gives infinity and not 0 x inf.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -42,7 +42,7 @@ template <> __device__ __forceinline__ void mma_16<__half>(float (&d)[4], uint32
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// p -> hi (rounded towards zero from p (1 - 2^-9)) and lo = p - hi > 0, two values to a word
+// p -> hi (rounded towards zero from p (1 - 2^-9)) and lo = p - hi > 0, two values to a word; f16: both at least 2^-24 where p is not 0
 template <class T> __device__ __forceinline__ void split_pair(float p0, float p1, uint32_t &hi, uint32_t &lo);
 template <> __device__ __forceinline__ void split_pair<__nv_bfloat16>(float p0, float p1, uint32_t &hi, uint32_t &lo) {
     const uint32_t h0 = __float_as_uint(p0 * 0.998046875f) & 0xffff0000u, h1 = __float_as_uint(p1 * 0.998046875f) & 0xffff0000u;
@@ -51,8 +51,9 @@ template <> __device__ __forceinline__ void split_pair<__nv_bfloat16>(float p0, 
     lo = *reinterpret_cast<const uint32_t *>(&l);
 }
 template <> __device__ __forceinline__ void split_pair<__half>(float p0, float p1, uint32_t &hi, uint32_t &lo) {
-    const __half h0 = __float2half_rz(p0 * 0.998046875f), h1 = __float2half_rz(p1 * 0.998046875f);
-    const __half2 h = __halves2half2(h0, h1), l = __floats2half2_rn(p0 - __half2float(h0), p1 - __half2float(h1));
+    const float least0 = p0 > 0.f ? 1.f / 16777216.f : 0.f, least1 = p1 > 0.f ? 1.f / 16777216.f : 0.f;  // 2^-24
+    const __half2 h = __halves2half2(__float2half_rz(fmaxf(p0 * 0.998046875f, least0)), __float2half_rz(fmaxf(p1 * 0.998046875f, least1)));
+    const __half2 l = __floats2half2_rn(fmaxf(p0 - __low2float(h), least0), fmaxf(p1 - __high2float(h), least1));
     hi = *reinterpret_cast<const uint32_t *>(&h);
     lo = *reinterpret_cast<const uint32_t *>(&l);
 }

@@ -11,7 +11,7 @@ from tests import paged_reference as ref
 
 pytestmark = pytest.mark.gpu
 BF, F16 = torch.bfloat16, torch.float16
-NAN = float("nan")
+NAN, INF = float("nan"), float("inf")
 
 
 def i32(v):
@@ -153,3 +153,42 @@ def test_scores_of_many_millions(new, dtype):
         window_attention(q * x, out, i32([0, new]), pool, 1, table, lens, window=n, max_q=new)
         want, tol = ref.attention(q * x, [0, new], pool, 1, table, [n], n, 0, dh ** -0.5)
         assert ((out.double() - want).abs() <= tol).all(), x
+
+
+@pytest.mark.parametrize("dtype", [F16, BF])
+@pytest.mark.parametrize("n,new,j", [(1000, 1, 5), (1000, 3, 13), (1000, 1, 200), (1000, 64, 200), (1000, 64, 990), (1000, 200, 3), (1000, 200, 850), (400, 380, 15), (400, 380, 90)])
+@pytest.mark.parametrize("value", [INF, -INF])
+def test_an_infinite_value_behind_a_small_probability(n, new, j, value, dtype):
+    """Far below the smallest number of 16 bits, but a number in 32: the result is infinite where the position is seen, and only there."""
+    dh, page, dim = 128, 16, 7
+    pool, table, lens = ref.cache([n], page, 2, dh, dtype, 3, fill=0.0)
+    pool[:, :, 0] = 0.0
+    pool[0, table[0, 0].long(), 0, :, 0] = 2.65  # q k / sqrt(dh) = 30: the others have 2^-43 of its weight
+    q = torch.ones(new, 4, dh, dtype=dtype, device="cuda")
+    want, tol = ref.attention(q, [0, new], pool, 1, table, [n], n, 0, dh ** -0.5)
+    pool[0, table[0, j // page].long(), 1, 1, j % page, dim] = value
+    out, status = torch.full_like(q, NAN), i32([0])
+    window_attention(q, out, i32([0, new]), pool, 1, table, lens, window=n, max_q=new, status=status)
+    sees = torch.arange(n - new, n, device="cuda") >= j
+    assert status.item() == 0
+    assert (out[sees][:, 2:, dim] == value).all()
+    same = (out.double() - want).abs() <= tol
+    same[sees, 2:, dim] = True
+    assert same.all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF])
+@pytest.mark.parametrize("new,j", [(1, 5), (3, 199), (100, 20), (300, 350)])
+def test_a_key_that_is_no_number_is_none_in_the_result(new, j, dtype):
+    n, dh = 400, 64
+    pool, table, lens = ref.cache([n], 16, 2, dh, dtype, 3, fill=0.0)
+    q = torch.randn(new, 4, dh, generator=torch.Generator().manual_seed(8)).to(dtype).cuda()
+    want, tol = ref.attention(q, [0, new], pool, 1, table, [n], n, 0, dh ** -0.5)
+    pool[0, table[0, j // 16].long(), 0, 1, j % 16, 7] = NAN
+    out = torch.full_like(q, 0.0)
+    window_attention(q, out, i32([0, new]), pool, 1, table, lens, window=n, max_q=new)
+    sees = torch.arange(n - new, n, device="cuda") >= j
+    assert out[sees][:, 2:].isnan().all()
+    same = (out.double() - want).abs() <= tol
+    same[sees, 2:] = True
+    assert same.all()
