@@ -31,12 +31,13 @@ __device__ __forceinline__ float2 rope_turn(int pos, float inv_freq, float scale
     sincospif((float)rest, &s, &c);
     return make_float2(c * scale, s * scale);
 }
+constexpr int kRopePadding = -1;  // the sequence of a token that is none
 // The page of a token's place; -1: it has none (a padding token, or something is out of range, which `bad` tells).
 __device__ __forceinline__ int rope_page(const RopeArgs &a, int pos, int seq, bool &bad) {
     bad = false;
-    if (seq < 0) return -1;
+    if (seq == kRopePadding) return -1;
     int page = -1;
-    if (pos >= 0 && seq < a.c.n_seqs && (pos >> a.c.ps_log2) < a.c.max_pages) page = a.c.table[(size_t)seq * a.c.max_pages + (pos >> a.c.ps_log2)];
+    if (pos >= 0 && seq >= 0 && seq < a.c.n_seqs && (pos >> a.c.ps_log2) < a.c.max_pages) page = a.c.table[(size_t)seq * a.c.max_pages + (pos >> a.c.ps_log2)];
     bad = page < 0 || page >= a.c.n_pages;
     return bad ? -1 : page;
 }
@@ -112,10 +113,10 @@ __global__ void __launch_bounds__(256) rope_append_any_kernel(const RopeArgs a, 
             const int d0 = INTER ? 2 * i : i, d1 = INTER ? 2 * i + 1 : i + half;
             const float x = to_f(row.src[d0]), y = to_f(row.src[d1]);
             const float2 w = row.turn ? cs[i] : make_float2(1.f, 0.f);
-            row.dst[d0] = from_f<TC>(seq < 0 ? 0.f : row.turn ? x * w.x - y * w.y : x);
-            row.dst[d1] = from_f<TC>(seq < 0 ? 0.f : row.turn ? y * w.x + x * w.y : y);
+            row.dst[d0] = from_f<TC>(seq == kRopePadding ? 0.f : row.turn ? x * w.x - y * w.y : x);
+            row.dst[d1] = from_f<TC>(seq == kRopePadding ? 0.f : row.turn ? y * w.x + x * w.y : y);
         } else if (i < single) {
-            row.dst[i + half] = from_f<TC>(seq < 0 ? 0.f : to_f(row.src[i + half]));
+            row.dst[i + half] = from_f<TC>(seq == kRopePadding ? 0.f : to_f(row.src[i + half]));
         } else {
             const int d = eights + 8 * (i - single);
             Eight<TI> e;
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(256) rope_append_any_kernel(const RopeArgs a, 
             e.load(row.src + d);
             e.get(p);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) p[k] = seq < 0 ? 0.f : p[k];
+            for (int k = 0; k < 8; ++k) p[k] = seq == kRopePadding ? 0.f : p[k];
             store_eight(row.dst + d, p);
         }
     }
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
     // dims of this unit: d0 .. d0 + 7, and in the half layout d0 + half ..
     const bool pairs = x < (a.rot + 7) / (INTER ? 8 : 16);
     const int d0 = INTER || pairs ? 8 * x : 8 * x + half;
-    const int pos = live ? a.positions[t] : 0, seq = live ? a.seqs[t] : -1;
+    const int pos = live ? a.positions[t] : 0, seq = live ? a.seqs[t] : kRopePadding;
     // this thread's units of the token's first heads, in bytes; heads are a 32-bit step apart (the launch has looked)
     const char *const q_at = static_cast<const char *>(a.q) + (t * a.q_tok + d0) * (int64_t)sizeof(TI);
     const char *const k_at = static_cast<const char *>(a.k) + (t * a.k_tok + d0) * (int64_t)sizeof(TI);
@@ -206,7 +207,7 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {
                     }
                 }
             }
-            if (seq < 0) {
+            if (seq == kRopePadding) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) p[e] = q[e] = 0.f;
             }

@@ -192,3 +192,20 @@ def test_a_key_that_is_no_number_is_none_in_the_result(new, j, dtype):
     same = (out.double() - want).abs() <= tol
     same[sees, 2:] = True
     assert same.all()
+
+
+# ---------------------------------------------------------------- what is told
+@pytest.mark.parametrize("aligned", [True, False])
+@pytest.mark.parametrize("inter", [True, False])
+def test_rope_append_tells_sequences_below_padding(aligned, inter):
+    pool, table, _ = ref.cache([40, 20], 16, 2, 64, BF, 3, fill=0.0)
+    before = pool.clone()
+    x = torch.randn(1 + 2 * 8 * 64, device="cuda").to(BF)
+    x = (x[:-1] if aligned else x[1:]).view(2, 8, 64)
+    q, k, v = x.split([4, 2, 2], 1)
+    for bad in (-2, -2 ** 31):
+        q_out, status = torch.full((2, 4, 64), NAN, dtype=BF, device="cuda"), i32([0])
+        rope_append(q, k, v, i32([5, 6]), i32([-1, bad]), freq(64), pool, 1, table, q_out, interleaved=inter, status=status)
+        assert status.item() == -1 and torch.equal(pool, before)
+        want = ref.rope(q[1:], i32([6]), freq(64), inter, 1.0)
+        assert (q_out[0] == 0).all() and ((q_out[1:].double() - want).abs() <= ref.U[BF] * want.abs() + 2.0 ** -19 * q.abs().max()).all()
