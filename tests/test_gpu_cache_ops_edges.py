@@ -209,3 +209,15 @@ def test_rope_append_tells_sequences_below_padding(aligned, inter):
         assert status.item() == -1 and torch.equal(pool, before)
         want = ref.rope(q[1:], i32([6]), freq(64), inter, 1.0)
         assert (q_out[0] == 0).all() and ((q_out[1:].double() - want).abs() <= ref.U[BF] * want.abs() + 2.0 ** -19 * q.abs().max()).all()
+
+
+def test_window_attention_answers_the_first_max_q_queries():
+    """A sequence with more queries than max_q is told, and its first max_q rows are right."""
+    pool, table, lens = ref.cache([50, 40], 16, 1, 64, BF, 4)
+    q = torch.randn(5, 2, 64, device="cuda").to(BF)
+    for max_q in (1, 2, 3):
+        out, status = torch.zeros_like(q), i32([0])
+        window_attention(q, out, i32([0, 4, 5]), pool, 1, table, lens, window=10, sinks=2, max_q=max_q, status=status)
+        want, tol = ref.attention(q, [0, 4, 5], pool, 1, table, [50, 40], 10, 2, 0.125)
+        rows = list(range(max_q)) + [4]
+        assert status.item() == -1 and ((out.double() - want).abs() <= tol)[rows].all(), max_q
