@@ -33,22 +33,27 @@ class Model:
 
 
 class Cache:
-    """Pool, page table, lengths and reference counts of `seqs` sequences; `grow` and `become` keep the state before in a second set."""
+    """Pool, page table, lengths and reference counts of `seqs` sequences; `grow` and `become` keep the state before in a second set.
+
+    What goes wrong on the device stays in `failed` until somebody looks: rotary positions and attention write it only when something is wrong,
+    but the pages' calls answer every time, so they have a word of their own that is taken over behind each."""
 
     def __init__(self, seqs, pages, positions, device="cuda"):
         i32 = lambda *s, v=0: torch.full(s, v, dtype=torch.int32, device=device)  # noqa: E731
         self.pool = torch.full((LAYERS, pages, 2, HKV, PAGE, DH), float("nan"), dtype=torch.bfloat16, device=device)
         self.state = [i32(seqs, -(-positions // PAGE), v=-1), i32(seqs), i32(pages)]
         self.other = [torch.empty_like(t) for t in self.state]
-        self.status = i32(1)
+        self.status, self.failed = i32(1), i32(1)
 
     table, lens, refs = (property(lambda self, k=k: self.state[k]) for k in range(3))
 
     def grow(self, n_new, window, sinks):
         pages_advance(*self.state, n_new, *self.state, self.status, page_size=PAGE, window=window, sinks=sinks)
+        torch.minimum(self.failed, self.status, out=self.failed)
 
     def become(self, parents):
         pages_reorder(self.pool, *self.state, parents, *self.other, self.status)
+        torch.minimum(self.failed, self.status, out=self.failed)
         self.state, self.other = self.other, self.state
 
 
@@ -60,8 +65,8 @@ def forward(model, cache, tokens, positions, seqs, q_start, max_q, window, sinks
     for layer in range(LAYERS):
         q, k, v = ((x @ model.qkv[layer]).split([HQ * DH, HKV * DH, HKV * DH], -1))
         q, k, v = (t.unflatten(-1, (-1, DH)) for t in (q, k, v))
-        rope_append(q, k, v, positions, seqs, model.inv_freq, cache.pool, layer + 1, cache.table, q_out, scale=model.scale, status=cache.status)
-        window_attention(q_out, o, q_start, cache.pool, layer + 1, cache.table, cache.lens, window=window, sinks=sinks, max_q=max_q, status=cache.status)
+        rope_append(q, k, v, positions, seqs, model.inv_freq, cache.pool, layer + 1, cache.table, q_out, scale=model.scale, status=cache.failed)
+        window_attention(q_out, o, q_start, cache.pool, layer + 1, cache.table, cache.lens, window=window, sinks=sinks, max_q=max_q, status=cache.failed)
         x = x + o.flatten(1) @ model.out[layer]
     return x
 
@@ -93,8 +98,8 @@ def run(model, prompt, *, beams, steps, chunk=256, window=300, sinks=4, pages=No
         parent = flat // VOCAB
         cache.become(parent.int())
         said, x = torch.cat((said[parent], (flat % VOCAB)[:, None]), 1), x[parent]
-    if cache.status.item():
-        raise RuntimeError(f"the cache's status is {cache.status.item()}")
+    if cache.failed.item():
+        raise RuntimeError(f"a call on the cache failed: {cache.failed.item()}")
     return said, score, x, cache
 
 

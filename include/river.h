@@ -297,7 +297,8 @@ int river_quantize_w4(const void *w, int out, int in, int group, int refine_iter
  * take a context's pool; they are asynchronous on cuda_stream, allocate nothing, read nothing back and can be captured in a graph.
  * What the host can see is refused before anything is queued: RIVER_E_BADARG (null or misaligned pointers, values out of range),
  * RIVER_E_SHAPE (a shape, type or combination that has no kernel).  A call with n_tokens 0 does nothing; addresses of its rows may be NULL.
- * What only the device can see goes to `status` ([dev] int32). */
+ * What only the device can see goes to `status` ([dev] int32): river_rope_append and river_window_attention lower it where something is wrong and
+ * leave it otherwise (the caller clears it), river_pages_advance and river_pages_reorder write it every time, so they need a word of their own. */
 enum { RIVER_BF16 = 0, RIVER_F16 = 1, RIVER_F32 = 2 };
 
 typedef struct river_paged {

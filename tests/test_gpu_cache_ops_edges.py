@@ -1,6 +1,8 @@
 """The operators on a caller's paged cache at their ends: calls without tokens, threads, errors left by others, small probabilities and infinities
 in f16, status words, lengths and starts that cannot be, and launches that only large or unaligned calls take (needs a B200)."""
 import ctypes as C
+import importlib.util
+import os
 import threading
 
 import pytest
@@ -8,6 +10,7 @@ import torch
 
 from paper_2604_18396_b200 import binding, cache_ops, rope_append, window_attention
 from tests import paged_reference as ref
+from tests import test_gpu_cache_ops as base
 
 pytestmark = pytest.mark.gpu
 BF, F16 = torch.bfloat16, torch.float16
@@ -221,3 +224,14 @@ def test_window_attention_answers_the_first_max_q_queries():
         want, tol = ref.attention(q, [0, 4, 5], pool, 1, table, [50, 40], 10, 2, 0.125)
         rows = list(range(max_q)) + [4]
         assert status.item() == -1 and ((out.double() - want).abs() <= tol)[rows].all(), max_q
+
+
+@pytest.mark.parametrize("tokens,beams,steps,pages", [(90, 1, 20, 6), (300, 2, 6, 5), (64, 4, 30, 9)])
+def test_the_example_ends_with_an_error_where_pages_do_not_suffice(tokens, beams, steps, pages):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(base.__file__)))
+    spec = importlib.util.spec_from_file_location("windowed_beams", os.path.join(root, "examples", "windowed_beams.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    prompt = torch.randint(0, ex.VOCAB, (tokens,), generator=torch.Generator().manual_seed(2)).cuda()
+    with pytest.raises(RuntimeError):
+        ex.run(ex.Model(), prompt, beams=beams, steps=steps, window=1000, sinks=0, pages=pages)
