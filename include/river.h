@@ -293,8 +293,9 @@ int river_quantize_w4(const void *w, int out, int in, int group, int refine_iter
 /* ---------------------------------------------------------------- long contexts on a paged cache
  * (The paper has no counterpart: these serve models and conversations whose positions are scaled, whose attention sees a window and a
  * few first positions, and whose sequences share, drop and move pages.)
- * The calls below need no context.  They work on caller-owned device buffers, in the layout of river_kv_pool_bytes, so that they also
- * take a context's pool; they are asynchronous on cuda_stream, allocate nothing, read nothing back and can be captured in a graph.
+ * The calls below need no context.  They work on caller-owned device buffers: a pool in the layout of river_kv_pool_bytes, and the page table,
+ * lengths and counts that go with it.  A context's own pool is not for them, since only the context knows which of its pages holds what.
+ * They are asynchronous on cuda_stream, allocate nothing, read nothing back and can be captured in a graph.
  * What the host can see is refused before anything is queued: RIVER_E_BADARG (null or misaligned pointers, values out of range),
  * RIVER_E_SHAPE (a shape, type or combination that has no kernel).  A call with n_tokens 0 does nothing; addresses of its rows may be NULL.
  * What only the device can see goes to `status` ([dev] int32): river_rope_append and river_window_attention lower it where something is wrong and

@@ -9,7 +9,8 @@ Argument marshalling and checks only, like binding.py: every operator is one cal
     refs   int32 [n_pages]                                                 table entries that hold a page; 0: free
 
 all contiguous CUDA tensors of one device.  status (int32 [1]) takes what only the device can see: rope_append and window_attention write it only
-where something is wrong (the lowest code stays), pages_advance and pages_reorder every time - so not one word for both.  A context's pool (River.kv_pool) has the same layout.
+where something is wrong (the lowest code stays), pages_advance and pages_reorder every time - so not one word for both.  A context's pool (River.kv_pool) is not for them: its page table
+stays with the context.
 """
 from __future__ import annotations
 
