@@ -360,8 +360,8 @@ int river_rope_append(const river_paged *c, int layer, int n_tokens, int Hq, int
  *   window        >= 1 (one that reaches over the whole context is ordinary causal attention);  sinks >= 0
  *   out           [dev] [n_tokens][Hq][dh] of the pool's type, 16-byte aligned
  *   status        [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as
- *                 not visible), q_start descends, a length is more than a row of the
- *                 table holds (it counts as that), or a sequence has more than max_q queries (the rows of that sequence behind the
+ *                 not visible), q_start descends, a length is negative (it counts as 0) or
+ *                 more than a row of the table holds (it counts as that), or a sequence has more than max_q queries (the rows of that sequence behind the
  *                 max_q-th may stay as they are); RIVER_E_TIMEOUT when a wait ran out (the rows that were waited for stay as they are).
  * Positions that a query does not see have no influence on its result, whatever the pool holds there.  Every result follows in a
  * fixed order of sums: the same inputs give the same bits. */

@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
             if (x < 0 || y < x || y > a.n_tokens || y - x > a.max_q) flag(a.status, RIVER_E_BADARG);
         }
     if (first < 0 || n < 0 || first + n > a.n_tokens || at < 0 || at >= n) return;
-    const int n_tok = min(n - at, per * pa.tiles), tok0 = first + at, pos0 = window_len(a, seq) - n + at, last_pos = pos0 + n_tok - 1;
+    const int n_tok = min(n - at, per * pa.tiles), tok0 = first + at, pos0 = window_len(a, a.c.lens[seq]) - n + at, last_pos = pos0 + n_tok - 1;
     const int nq = n_tok > per ? 2 : 1;
 
     const uint32_t b_first = smem_u32(&bars[0]), b_full = b_first + 8, b_free = b_full + 32, b_s = b_free + 16, b_p = b_s + 16, b_o = b_p + 32, b_q = b_o + 16;

@@ -19,11 +19,11 @@ struct WindowArgs {
     int32_t *status;
 };
 
-// Positions that sequence s holds; a length that its row of the table cannot have is told and counts as the row's.
-__device__ __forceinline__ int window_len(const WindowArgs &a, int s) {
-    const int len = a.c.lens[s], cap = a.c.max_pages << a.c.ps_log2;
-    if (len > cap && threadIdx.x == 0) flag(a.status, RIVER_E_BADARG);
-    return min(len, cap);
+// Positions that a sequence with queries holds; a length that its row of the table cannot have is told and counts as the row's, a negative one as 0.
+__device__ __forceinline__ int window_len(const WindowArgs &a, int len) {
+    const int cap = a.c.max_pages << a.c.ps_log2;
+    if ((len < 0 || len > cap) && threadIdx.x == 0) flag(a.status, RIVER_E_BADARG);
+    return max(0, min(len, cap));
 }
 // the first position of the window of the query at p
 __device__ __forceinline__ int window_low(int p, int window) { return p >= window ? p - window + 1 : 0; }

@@ -81,11 +81,11 @@ __global__ void __launch_bounds__(32 * kStepWarps, kStepCtas) window_attn_step_k
     const int unit = blockIdx.x / splits, tile = unit % (a.c.Hkv * rt), row = unit / (a.c.Hkv * rt);
     const int kvh = tile / rt, head0 = kvh * gq + tile % rt * 8, heads = min(8, gq - tile % rt * 8);
     const int seq = row / a.max_q, i = row % a.max_q;
-    const int tok0 = a.q_start[seq], end = a.q_start[seq + 1], len = window_len(a, seq);
+    const int tok0 = a.q_start[seq], end = a.q_start[seq + 1], held = a.c.lens[seq];
     const bool odd = tok0 < 0 || end < tok0 || end > a.n_tokens;
     if (threadIdx.x == 0 && (odd || end - tok0 > a.max_q)) flag(a.status, RIVER_E_BADARG);
     if (odd || i >= end - tok0) return;
-    const int n = end - tok0;
+    const int n = end - tok0, len = window_len(a, held);
     const int token = tok0 + i, pos = len - n + i;
     T *out = static_cast<T *>(a.out) + ((size_t)token * a.Hq + head0) * DH;
     // blocks of 16 positions: n_sb of the sinks, then wb0 .. pos / 16

@@ -235,3 +235,19 @@ def test_the_example_ends_with_an_error_where_pages_do_not_suffice(tokens, beams
     prompt = torch.randint(0, ex.VOCAB, (tokens,), generator=torch.Generator().manual_seed(2)).cuda()
     with pytest.raises(RuntimeError):
         ex.run(ex.Model(), prompt, beams=beams, steps=steps, window=1000, sinks=0, pages=pages)
+
+
+@pytest.mark.parametrize("bad", [-5, -1, -2 ** 31, -2 ** 31 + 1])
+@pytest.mark.parametrize("new", [1, 40])
+def test_window_attention_tells_negative_lengths(new, bad):
+    """Such a sequence holds nothing; the others are as ever."""
+    pool, table, lens = ref.cache([60, 70], 16, 1, 64, BF, 4)
+    q = torch.randn(2 * new, 2, 64, device="cuda").to(BF)
+    out, status = torch.full_like(q, NAN), i32([0])
+    window_attention(q, out, i32([0, new, 2 * new]), pool, 1, table, i32([bad, 70]), window=20, sinks=2, max_q=new, status=status)
+    want, tol = ref.attention(q, [0, new, 2 * new], pool, 1, table, [0, 70], 20, 2, 0.125)
+    assert status.item() == -1 and (out[:new] == 0).all() and ((out.double() - want).abs() <= tol).all()
+    status.zero_()  # (a sequence without queries may have any)
+    window_attention(q[:new], out[:new], i32([0, 0, new]), pool, 1, table, i32([bad, 70]), window=20, sinks=2, max_q=new, status=status)
+    want, tol = ref.attention(q[:new], [0, 0, new], pool, 1, table, [0, 70], 20, 2, 0.125)
+    assert status.item() == 0 and ((out[:new].double() - want).abs() <= tol).all()
