@@ -109,7 +109,7 @@ __device__ __forceinline__ int prompt_seq(const int32_t *q_start, int n_seqs, in
     int lo = 0, hi = n_seqs;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (q_start[mid] / per + mid <= x) lo = mid; else hi = mid;
+        if (q_start[mid] / per <= x - mid) lo = mid; else hi = mid;
     }
     return lo;
 }
@@ -175,13 +175,14 @@ __global__ void __launch_bounds__(kWpThreads, 1) window_attn_prompt_kernel(const
     // heavy tiles, those behind a long history, first
     const int splits = SPLIT ? pa.splits : 1, unit = blockIdx.x / splits, kvh = unit % a.c.Hkv, slot = gridDim.x / splits / a.c.Hkv - 1 - unit / a.c.Hkv;
     const int seq = prompt_seq(a.q_start, a.c.n_seqs, per * pa.tiles, slot);
-    const int first = a.q_start[seq], n = a.q_start[seq + 1] - first, at = (slot - (first / (per * pa.tiles) + seq)) * per * pa.tiles;
+    const int first = a.q_start[seq], end = a.q_start[seq + 1];  // (compared before they are subtracted: any ints may stand there)
+    const int n = first < 0 || end < first || end > a.n_tokens ? 0 : end - first, at = n == 0 ? 0 : (slot - (first / (per * pa.tiles) + seq)) * per * pa.tiles;
     if (blockIdx.x == 0)
         for (int s = tid; s < a.c.n_seqs; s += kWpThreads) {
             const int x = a.q_start[s], y = a.q_start[s + 1];
             if (x < 0 || y < x || y > a.n_tokens || y - x > a.max_q) flag(a.status, RIVER_E_BADARG);
         }
-    if (first < 0 || n < 0 || first + n > a.n_tokens || at < 0 || at >= n) return;
+    if (at < 0 || at >= n) return;
     const int n_tok = min(n - at, per * pa.tiles), tok0 = first + at, pos0 = window_len(a, a.c.lens[seq]) - n + at, last_pos = pos0 + n_tok - 1;
     const int nq = n_tok > per ? 2 : 1;
 

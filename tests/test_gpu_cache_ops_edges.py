@@ -251,3 +251,25 @@ def test_window_attention_tells_negative_lengths(new, bad):
     window_attention(q[:new], out[:new], i32([0, 0, new]), pool, 1, table, i32([bad, 70]), window=20, sinks=2, max_q=new, status=status)
     want, tol = ref.attention(q[:new], [0, 0, new], pool, 1, table, [0, 70], 20, 2, 0.125)
     assert status.item() == 0 and ((out[:new].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("hq", [4, 256])  # (256 heads to two: a tile for every query)
+@pytest.mark.parametrize("starts", [[0, 5, -2 ** 31], [0, 2 ** 31 - 1, 80], [2 ** 31 - 1, 3, 80], [-2 ** 31, 3, 80], [0, 81, 80], [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1],
+                                    [-1, -2 ** 31, 80], [7, 2 ** 31 - 2, -2 ** 31 + 5]])
+def test_window_attention_tells_starts_that_cannot_be(starts, hq):
+    """Whatever stands there: it is told, and no row but those of sound sequences is written."""
+    pool, table, lens = ref.cache([90, 100], 16, 2, 64, BF, 4)
+    q = torch.randn(80, hq, 64, device="cuda").to(BF)
+    for max_q in (1, 80):
+        around, status = torch.full((3 * 80, hq, 64), NAN, dtype=BF, device="cuda"), i32([0])
+        out = around[80:160]
+        window_attention(q, out, i32(starts), pool, 1, table, lens, window=20, sinks=2, max_q=max_q, status=status)
+        assert status.item() == -1 and around[:80].isnan().all() and around[160:].isnan().all()
+        for s, n in enumerate((90, 100)):
+            a, b = starts[s], starts[s + 1]
+            if 0 <= a <= b <= 80:
+                b = min(b, a + max_q)
+                want, tol = ref.attention(q[a:b], [0, b - a], pool, 1, table[s:s + 1], [n - (starts[s + 1] - b)], 20, 2, 0.125)
+                assert ((out[a:b].double() - want).abs() <= tol).all()
+                around[80 + a:80 + starts[s + 1]] = NAN
+        assert around.isnan().all()
