@@ -34,6 +34,7 @@ struct PagesScan {
     int part[33], count[2];
     int bad, full;  // what every CTA finds for itself: a sequence or length out of range, a row too long
     int odd;        // a page out of range: the first CTA's tells, behind a barrier of the cluster
+    unsigned long long wanted;  // of all sequences, where 32 bits may not hold it
 };
 struct PagesShared : PagesScan {
     int prefix[kPgSeqs];
@@ -191,7 +192,8 @@ __global__ void __launch_bounds__(kPgThreads) pages_advance_kernel(const PagesAr
     cg::cluster_group cluster = cg::this_cluster();
     const int S = a.c.n_seqs, P = a.c.max_pages, N = a.c.n_pages, lg = a.c.ps_log2, up = (1 << lg) - 1, lane = threadIdx.x & 31;
     const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
-    if (threadIdx.x == 0) s.bad = s.full = s.odd = 0;
+    const bool wide = (int64_t)S * P > INT32_MAX;
+    if (threadIdx.x == 0) s.bad = s.full = s.odd = 0, s.wanted = 0;
     if (a.table_out != a.c.table) copy_ints(a.table_out, a.c.table, (size_t)S * P, thread, threads);
     if (a.refs_out != a.refs) copy_ints(a.refs_out, a.refs, N, thread, threads);
     __syncthreads();
@@ -203,8 +205,10 @@ __global__ void __launch_bounds__(kPgThreads) pages_advance_kernel(const PagesAr
         else if (n > cap - len) s.full = 1;
         else want = ((len + n + up) >> lg) - ((len + up) >> lg);
         s.prefix[i] = want;
+        if (wide) atomicAdd(&s.wanted, (unsigned long long)want);
     }
     __syncthreads();
+    if (wide && threadIdx.x == 0 && s.wanted > N) s.full = 1;  // (else the sums below fit 32 bits)
     const int want = scan_shared(s.prefix, S, s.part);
     cluster.sync();  // (the copies)
     // pages that no query needs any longer: a warp per sequence, from the window's first page backwards to the first that is gone

@@ -8,7 +8,7 @@ import threading
 import pytest
 import torch
 
-from paper_2604_18396_b200 import binding, cache_ops, rope_append, window_attention
+from paper_2604_18396_b200 import binding, cache_ops, pages_advance, rope_append, window_attention
 from tests import paged_reference as ref
 from tests import test_gpu_cache_ops as base
 
@@ -273,3 +273,17 @@ def test_window_attention_tells_starts_that_cannot_be(starts, hq):
                 assert ((out[a:b].double() - want).abs() <= tol).all()
                 around[80 + a:80 + starts[s + 1]] = NAN
         assert around.isnan().all()
+
+
+def test_pages_advance_wants_more_pages_than_32_bits_count():
+    """8192 sequences that want 262145 pages each, and 524288: 2^31 and 2^32 and a few more."""
+    seqs, page = 8192, 16
+    for width in (262145, 524289):
+        table = torch.full((seqs, width), -1, dtype=torch.int32, device="cuda")
+        lens, refs, status = torch.zeros(seqs, dtype=torch.int32, device="cuda"), torch.zeros(50000, dtype=torch.int32, device="cuda"), i32([77])
+        pages_advance(table, lens, refs, torch.full_like(lens, width * page), table, lens, refs, status, page_size=page)
+        assert status.item() == -4 and not lens.any() and not refs.any() and table[0, 0].item() == -1 and table.max().item() == -1
+        pages_advance(table, lens, refs, torch.full_like(lens, 96), table, lens, refs, status, page_size=page)  # 49152 pages
+        assert status.item() == 0 and (lens == 96).all() and (refs[:49152] == 1).all() and not refs[49152:].any()
+        assert torch.equal(table[:, :6].flatten(), torch.arange(49152, dtype=torch.int32, device="cuda")) and table[:, 6:].max().item() == -1
+        del table
