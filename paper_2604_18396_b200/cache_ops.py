@@ -67,10 +67,10 @@ def _cache(pool: torch.Tensor, table: torch.Tensor, lens: Optional[torch.Tensor]
 
 
 def _rows(x: torch.Tensor, device: int, what: str) -> bytes:
-    t, h, d = x.stride()
+    (t, h, d), (n, heads, _) = x.stride(), x.shape
     if x.get_device() != device or (d != 1 and x.shape[2] != 1):
         _refuse(f"{what}: a tensor [tokens, heads, dh] with consecutive dims on CUDA device {device}")
-    return _ROWS.pack(x.data_ptr(), t, h)
+    return _ROWS.pack(x.data_ptr(), t if n > 1 else 0, h if heads > 1 else 0)  # (the step of a dim with one place may be anything)
 
 
 def _run(fn, device: int, stream, used: Sequence[Optional[torch.Tensor]], *args):

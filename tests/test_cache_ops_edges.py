@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2604_18396_b200 import cache_ops
 from tests import test_cache_ops_checks as checks
@@ -28,3 +29,11 @@ def test_the_self_test_of_waits_refuses_what_it_cannot_run(lib):
                                                  8, 0, 1.0, checks.P, 0, splits, polls, 0)
     assert [call(splits=x) for x in (0, 3, 8)] == [-1] * 3 and [call(polls=x) for x in (0, -1, (1 << 20) + 1)] == [-1] * 3
     assert call(n=0) == -1 and call(hq=3) == -1 and call(hq=258) == -2 and call(c=checks.paged(dh=96)) == -2
+
+
+def test_steps_of_dims_with_one_place_are_none():
+    x = torch.zeros(1000, dtype=torch.bfloat16)
+    rows = lambda *a: cache_ops._ROWS.unpack(cache_ops._rows(x.as_strided(*a), -1, "q"))[1:]  # noqa: E731
+    assert rows((1, 4, 64), (259, 64, 1)) == (0, 64) and rows((3, 1, 64), (64, 7, 1)) == (64, 0) and rows((2, 3, 64), (259, 65, 1)) == (259, 65)
+    with pytest.raises(ValueError):
+        rows((2, 3, 64), (256, 1, 2))

@@ -287,3 +287,16 @@ def test_pages_advance_wants_more_pages_than_32_bits_count():
         assert status.item() == 0 and (lens == 96).all() and (refs[:49152] == 1).all() and not refs[49152:].any()
         assert torch.equal(table[:, :6].flatten(), torch.arange(49152, dtype=torch.int32, device="cuda")) and table[:, 6:].max().item() == -1
         del table
+
+
+def test_steps_of_one_token_and_one_head_may_be_anything():
+    """A view of one row that is 3 longer than its heads, and one head of rows of any length."""
+    pool, table, lens = ref.cache([50], 16, 1, 64, BF, 4)
+    row = torch.randn(1, 4 * 64 + 3, device="cuda").to(BF)
+    q = row.as_strided((1, 4, 64), (259, 64, 1))
+    heads = torch.randn(64 * 9, device="cuda").to(BF).as_strided((9, 1, 64), (64, 7, 1))
+    for x in (q, heads):
+        out, status, n = torch.full(x.shape, NAN, dtype=BF, device="cuda"), i32([0]), x.shape[0]
+        window_attention(x, out, i32([0, n]), pool, 1, table, lens, window=20, sinks=2, max_q=n, status=status)
+        want, tol = ref.attention(x, [0, n], pool, 1, table, [50], 20, 2, 0.125)
+        assert status.item() == 0 and ((out.double() - want).abs() <= tol).all()
