@@ -3,17 +3,18 @@ in f16, status words, lengths and starts that cannot be, and launches that only 
 import ctypes as C
 import importlib.util
 import os
+import random
 import threading
 
 import pytest
 import torch
 
-from paper_2604_18396_b200 import binding, cache_ops, pages_advance, rope_append, window_attention
+from paper_2604_18396_b200 import binding, cache_ops, pages_advance, pages_compact, pages_reorder, rope_append, window_attention
 from tests import paged_reference as ref
 from tests import test_gpu_cache_ops as base
 
 pytestmark = pytest.mark.gpu
-BF, F16 = torch.bfloat16, torch.float16
+BF, F16, F32 = torch.bfloat16, torch.float16, torch.float32
 NAN, INF = float("nan"), float("inf")
 
 
@@ -300,3 +301,68 @@ def test_steps_of_one_token_and_one_head_may_be_anything():
         window_attention(x, out, i32([0, n]), pool, 1, table, lens, window=20, sinks=2, max_q=n, status=status)
         want, tol = ref.attention(x, [0, n], pool, 1, table, [50], 20, 2, 0.125)
         assert status.item() == 0 and ((out.double() - want).abs() <= tol).all()
+
+
+# ---------------------------------------------------------------- launches of large and unaligned calls
+@pytest.mark.parametrize("t,hq,hkv,dh,rot,inter,tin,tc,page,packed", [
+    (592, 32, 8, 128, 128, False, BF, BF, 16, True), (701, 8, 2, 64, 64, False, F32, F16, 32, True), (1999, 4, 1, 64, 48, True, BF, BF, 16, True),
+    (593, 1, 1, 64, 16, True, F16, F16, 64, True), (799, 24, 8, 128, 98, True, F32, BF, 16, True), (1030, 3, 1, 128, 32, False, F16, F16, 64, True),
+    # rows of 16 bytes with a turned part that is none: the dims behind it go by eights
+    (5, 3, 1, 128, 34, False, F16, F16, 16, True), (650, 6, 2, 128, 18, False, BF, BF, 32, True), (9, 4, 4, 128, 62, False, F32, BF, 16, True),
+    (700, 2, 2, 64, 6, False, F32, F16, 64, True), (650, 5, 1, 64, 34, True, BF, BF, 16, False)])
+def test_rope_append_of_prompts(t, hq, hkv, dh, rot, inter, tin, tc, page, packed):
+    base.test_rope_append(t, hq, hkv, dh, rot, inter, tin, tc, page, packed)
+
+
+def test_pages_reorder_of_wide_tables():
+    base.test_pages_reorder(300, 900, 16, 9000, 1, 1, 64, BF)
+
+
+def test_pages_compact_of_many_pages():
+    base.test_pages_compact(262200, 1, 1, 64, 16, BF)
+
+
+def off16(v):
+    """The same ints, four bytes behind a 16-byte boundary."""
+    x = i32(v)
+    y = torch.empty(x.numel() + 1, dtype=torch.int32, device="cuda")[1:].view(x.shape)
+    return y.copy_(x)
+
+
+@pytest.mark.parametrize("seqs,width,n_pages", [(3, 7, 60), (70, 33, 3001)])
+def test_pages_off_16_bytes(seqs, width, n_pages):
+    rng, page = random.Random(seqs), 16
+    table, lens, refs = base.state(rng, seqs, width, page, n_pages)
+    new = [min(rng.choice([0, 1, page, 40]), width * page - m) for m in lens]
+    want = ref.advance(table, lens, refs, new, page, 50, 3)
+    a = [off16(x) for x in (table, lens, refs, new)]
+    outs = [off16(x) for x in (table, lens, refs)] + [i32([77])]
+    pages_advance(*a, *outs, page_size=page, window=50, sinks=3)
+    assert [x.tolist() for x in outs] == [want[0], want[1], want[2], [want[3]]]
+    parents = [rng.randrange(-1, seqs) for _ in range(seqs)]
+    want = ref.reorder(table, lens, refs, parents, page)
+    pool = torch.randn(2, n_pages, 2, 1, page, 64, device="cuda").to(BF)
+    want_pool = pool.clone()
+    for src, dst, fill in want[3]:
+        want_pool[:, dst, :, :, :fill] = want_pool[:, src, :, :, :fill]
+    pages_reorder(pool, *a[:3], off16(parents), *outs)
+    assert [x.tolist() for x in outs] == [want[0], want[1], want[2], [want[4]]] and torch.equal(pool, want_pool)
+    want = ref.compact(table, refs)
+    for src, dst in want[4]:
+        want_pool[:, dst] = want_pool[:, src].clone()
+    outs, n = [off16(table), off16(refs), off16(refs)], off16([77])
+    pages_compact(pool, a[0], a[2], *outs, n)
+    assert [x.tolist() for x in outs] + [n.item()] == [want[0], want[1], want[2], want[3]] and torch.equal(pool, want_pool)
+
+
+@pytest.mark.parametrize("seqs,hq,hkv,dh,width,dtype", [(128, 32, 8, 128, 32768, BF), (48, 32, 8, 128, 131072, F16), (32, 8, 8, 128, 32768, BF), (200, 8, 1, 64, 65536, BF)])
+def test_single_tokens_under_long_windows(seqs, hq, hkv, dh, width, dtype):
+    """Ordinary attention of short conversations whose table has room for long ones."""
+    rng = random.Random(seqs)
+    lens = [rng.choice([1, 17, 300, rng.randint(1, 900)]) for _ in range(seqs)]
+    pool, table, lens_t = ref.cache(lens, 16, hkv, dh, dtype, 7, width=width // 16)
+    q = (torch.randn(seqs, hq, dh, generator=torch.Generator().manual_seed(8)) * 2).to(dtype).cuda()
+    out, status, starts = torch.full_like(q, NAN), i32([0]), list(range(seqs + 1))
+    window_attention(q, out, i32(starts), pool, 1, table, lens_t, window=width, max_q=1, status=status)
+    want, tol = ref.attention(q, starts, pool, 1, table, lens, width, 0, dh ** -0.5)
+    assert status.item() == 0 and ((out.double() - want).abs() <= tol).all()
