@@ -20,6 +20,11 @@ struct Paged {
 };
 
 inline bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// int32 and float arrays (NULL is aligned)
+template <class... P>
+bool words(const P *...p) {
+    return ((reinterpret_cast<uintptr_t>(p) | ... | 0) & 3) == 0;
+}
 
 // The description of a cache, checked (need_pool: the call touches the pool's values).  Every offset in elements fits 63 bits; page
 // ids, table columns and positions fit 31.

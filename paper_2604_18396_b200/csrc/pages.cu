@@ -453,6 +453,7 @@ extern "C" int river_pages_advance(const river_paged *c, const int32_t *refs, co
     PagesArgs a = {};
     if (const int rc = paged_check(c, false, true, &a.c)) return rc;
     if (!refs || !n_new || !table_out || !lens_out || !refs_out || !status || window < 0 || sinks < 0) return RIVER_E_BADARG;
+    if (!words(refs, n_new, table_out, lens_out, refs_out, status)) return RIVER_E_BADARG;
     if (c->n_seqs > kPgSeqs) return RIVER_E_SHAPE;
     a.refs = refs;
     a.n_new = n_new;
@@ -470,6 +471,7 @@ extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, co
     PagesArgs a = {};
     if (const int rc = paged_check(c, true, true, &a.c)) return rc;
     if (!refs || !parents || !table_out || !lens_out || !refs_out || !copies || !status) return RIVER_E_BADARG;
+    if (!words(refs, parents, table_out, lens_out, refs_out, copies, status)) return RIVER_E_BADARG;
     if (table_out == c->table || lens_out == c->lens || refs_out == refs) return RIVER_E_BADARG;
     if (c->n_seqs > kPgSeqs) return RIVER_E_SHAPE;
     a.refs = refs;
@@ -493,6 +495,7 @@ extern "C" int river_pages_compact(const river_paged *c, const int32_t *refs, in
     PagesArgs a = {};
     if (const int rc = paged_check(c, true, false, &a.c)) return rc;
     if (!refs || !table_out || !refs_out || !remap || !n_used || !moves) return RIVER_E_BADARG;
+    if (!words(refs, table_out, refs_out, remap, n_used, moves)) return RIVER_E_BADARG;
     a.refs = refs;
     a.table_out = table_out;
     a.refs_out = refs_out;

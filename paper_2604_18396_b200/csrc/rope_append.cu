@@ -291,12 +291,12 @@ extern "C" int river_rope_append(const river_paged *c, int layer, int n_tokens, 
     using namespace river;
     RopeArgs a;
     if (const int rc = paged_check(c, true, false, &a.c)) return rc;
-    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || Hq < 0 || Hq > (1 << 16) || !inv_freq || !std::isfinite(scale)) return RIVER_E_BADARG;
+    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || Hq < 0 || Hq > (1 << 16) || !inv_freq || !words(inv_freq, status) || !std::isfinite(scale)) return RIVER_E_BADARG;
     if (rotary_dim < 2 || rotary_dim % 2 || rotary_dim > c->dh) return RIVER_E_BADARG;
     if (in_dtype != c->dtype && in_dtype != RIVER_F32) return RIVER_E_SHAPE;
     if (n_tokens == 0) return RIVER_OK;  // (rows that are none may have no address)
     const size_t es = in_dtype == RIVER_F32 ? 4 : 2;
-    if (!positions || !seqs) return RIVER_E_BADARG;
+    if (!positions || !seqs || !words(positions, seqs)) return RIVER_E_BADARG;
     if (!k || !k->p || !v || !v->p || (Hq > 0 && (!q || !q->p || !q_out)) || !aligned_to(q_out, 16)) return RIVER_E_BADARG;
     if (!aligned_to(k->p, es) || !aligned_to(v->p, es) || (Hq > 0 && !aligned_to(q->p, es))) return RIVER_E_BADARG;
     a.layer0 = layer - 1;

@@ -71,7 +71,7 @@ int launch(const WindowArgs &a, cudaStream_t st) {
 int window_args(const river_paged *c, int layer, int n_tokens, int max_q, const int32_t *q_start, int Hq, const river_rows *q, int window, int sinks,
                 float softmax_scale, void *out, int32_t *status, WindowArgs *a) {
     if (const int rc = paged_check(c, true, true, &a->c)) return rc;
-    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || max_q < 0 || !q_start || window < 1 || sinks < 0) return RIVER_E_BADARG;
+    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || max_q < 0 || !q_start || !words(q_start, status) || window < 1 || sinks < 0) return RIVER_E_BADARG;
     if (Hq < 1 || Hq % c->Hkv || !std::isfinite(softmax_scale)) return RIVER_E_BADARG;
     if (c->n_seqs > 65535 || Hq > 8192 || (int64_t)c->n_seqs * Hq > (1 << 26)) return RIVER_E_SHAPE;  // (the kernels' grids)
     a->layer0 = layer - 1;

@@ -37,3 +37,19 @@ def test_steps_of_dims_with_one_place_are_none():
     assert rows((1, 4, 64), (259, 64, 1)) == (0, 64) and rows((3, 1, 64), (64, 7, 1)) == (64, 0) and rows((2, 3, 64), (259, 65, 1)) == (259, 65)
     with pytest.raises(ValueError):
         rows((2, 3, 64), (256, 1, 2))
+
+
+ODD = checks.P + 2  # no address of an int or a float
+
+
+@pytest.mark.parametrize("call,names", [(checks.rope, ("pos", "seqs", "f")), (checks.attn, ("qs",)), (checks.advance, ("refs", "new", "t", "ln", "r", "st")),
+                                        (checks.reorder, ("refs", "par", "t", "ln", "r", "copies", "st")), (checks.compact, ("refs", "t", "r", "remap", "n", "moves"))])
+def test_arrays_off_their_words_are_refused(lib, call, names):
+    for name in names:
+        assert call(lib, **{name: ODD}) == -1, name
+
+
+def test_a_status_off_its_word_is_refused(lib):
+    c, rows = C.byref(checks.paged()), C.byref(cache_ops.river_rows(checks.P, 256, 64))
+    assert lib.river_rope_append(c, 1, 4, 4, 0, rows, rows, rows, checks.P, checks.P, checks.P, 64, 0, 1.0, checks.P, ODD, 0) == -1
+    assert lib.river_window_attention(c, 1, 4, 2, checks.P, 4, rows, 8, 0, 1.0, checks.P, ODD, 0) == -1
