@@ -67,10 +67,12 @@ def _cache(pool: torch.Tensor, table: torch.Tensor, lens: Optional[torch.Tensor]
 
 
 def _rows(x: torch.Tensor, device: int, what: str) -> bytes:
-    (t, h, d), (n, heads, _) = x.stride(), x.shape
+    t, h, d = x.stride()
     if x.get_device() != device or (d != 1 and x.shape[2] != 1):
         _refuse(f"{what}: a tensor [tokens, heads, dh] with consecutive dims on CUDA device {device}")
-    return _ROWS.pack(x.data_ptr(), t if n > 1 else 0, h if heads > 1 else 0)  # (the step of a dim with one place may be anything)
+    if (t | h) & 7:  # (the step of a dim with one place may be anything, and only an odd one would be in the way)
+        t, h = t if x.shape[0] > 1 else 0, h if x.shape[1] > 1 else 0
+    return _ROWS.pack(x.data_ptr(), t, h)
 
 
 def _run(fn, device: int, stream, used: Sequence[Optional[torch.Tensor]], *args):
