@@ -345,7 +345,7 @@ int river_rope_frequencies(int rotary_dim, double theta, const river_rope_scalin
  *   interleaved   0: pair i = dims (i, i + rotary_dim / 2); 1: dims (2 i, 2 i + 1)
  *   q_out         [dev] [n_tokens][Hq][dh] of the pool's type, 16-byte aligned; must not overlap the inputs
  *   status        [dev] int32 or NULL: RIVER_E_BADARG is stored there when a position is negative, a sequence or a page out of
- *                 range; such a token stores no key and value (its query is turned all the same, by 0 for a negative position).
+ *                 range (a sequence below -1 too); such a token stores no key and value (its query is turned all the same, by 0 for a negative position).
  * Distinct tokens of a call have distinct places. */
 int river_rope_append(const river_paged *c, int layer, int n_tokens, int Hq, int in_dtype, const river_rows *q, const river_rows *k,
                       const river_rows *v, const int32_t *positions, const int32_t *seqs, const float *inv_freq, int rotary_dim,
@@ -358,7 +358,7 @@ int river_rope_append(const river_paged *c, int layer, int n_tokens, int Hq, int
  *   max_q         at least the largest number of queries of a sequence (1: a decode step)
  *   q_start       [dev] int32 [n_seqs + 1], ascending from 0 to n_tokens
  *   window        >= 1 (one that reaches over the whole context is ordinary causal attention);  sinks >= 0
- *   out           [dev] [n_tokens][Hq][dh] of the pool's type, 16-byte aligned
+ *   out           [dev] [n_tokens][Hq][dh] of the pool's type, 16-byte aligned; must not overlap the inputs
  *   status        [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as
  *                 not visible), q_start descends, a length is negative (it counts as 0) or
  *                 more than a row of the table holds (it counts as that), or a sequence has more than max_q queries (the rows of that sequence behind the

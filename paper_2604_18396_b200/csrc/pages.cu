@@ -482,7 +482,9 @@ extern "C" int river_pages_reorder(const river_paged *c, const int32_t *refs, co
     a.list = copies;
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    // A few sequences' last pages (up to 4 MB) are copied by the deciding cluster itself: four beams of the 1B class 14.2 us in two launches, 12.3 in one.
+    // A few sequences' last pages (up to 4 MB) are copied by the deciding cluster itself, which saves the host a launch: four beams of the 1B class 14.2 us
+    // in two launches, 12.3 in one.  The GPU alone takes longer that way (in a graph, us in one / two: 0.25 MB 10.7 / 7.6, 2 MB 13.5 / 7.6, 4 MB 19.1 /
+    // 8.4, 8 MB 30.5 / 9.7), and at 4 MB the host's launch costs less than that (20.6 / 16 in a loop).
     const int64_t most = (int64_t)std::min(c->n_seqs, c->n_pages) * c->n_layers * 2 * c->Hkv;
     a.copy_here = most * c->page_size * c->dh * 2 <= (4 << 20);
     const size_t work = std::max((size_t)c->n_seqs * c->max_pages + c->n_pages, a.copy_here && most > 32 ? (size_t)4 * kPgThreads + 1 : (size_t)0);

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(256) rope_append_any_kernel(const RopeArgs a, 
 // 16-byte rows.  A CTA takes blockDim.z tokens; thread (x, y, z) unit x of the rows y, y + blockDim.y, .. of token z.  A unit is eight dims
 // (interleaved: four pairs, or dims that stay), or eight pairs and their partners half a turned part further (half layout).  UNITS rows of
 // a thread, 192 bytes, are under way before place and angles are known; a thread's sines and cosines are the same for all its rows.
-// Prompts are bound by HBM and by the instructions beside it: 8192 tokens of 48 heads of 128, three quarters turned, bf16: 39 us, 5.1 TB/s (44 with
+// Prompts are bound by HBM and by the instructions beside it: 8192 tokens of 48 heads of 128, three quarters turned, bf16: 40 us without the host (41.5 with), 5.0 TB/s (44 with
 // 64-bit products for every unit's address).
 template <class TI, class TC, bool INTER, int UNITS>
 __global__ void __launch_bounds__(256) rope_append_kernel(const RopeArgs a) {

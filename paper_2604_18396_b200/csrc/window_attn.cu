@@ -58,6 +58,10 @@ int launch_prompt(const PromptArgs &pa, cudaStream_t st) {
 // 128 rows.  (us, single tokens / query tiles, heads of 128; 32 query and 8 KV heads, one sequence, window 4096: 2 tokens 12 / 21, 6 22
 // / 22, 16 37 / 23; 64 sequences of 2: 283 / 219; window 1024, one sequence, 8 tokens 11 / 14, 16 15 / 15; 12 and 1 heads, 4 sequences of 8:
 // 12 / 16.)
+// Measured for windows up to 4096 and heads of 128.  Both estimates take the table's width for a sequence's length, which the host does not know, and
+// that of query tiles has no bound by HBM: from windows of 32 K on, batches of single tokens of many query heads go to query tiles where they lose
+// (128 rows of 1000 positions, window and table 32768: 137 us, with a table of 1024 single tokens' 103; 64 rows, 131072: 201 / 63; 128 rows of 16000,
+// 32768: 1427 / 1284).  A table no wider than its sequences are long avoids that.
 template <class T, int DH>
 int launch(const WindowArgs &a, cudaStream_t st) {
     double step_us, prompt_us = 1e300;

@@ -13,15 +13,17 @@
 //
 // What bounds it: a tile's chain - S, softmax, P V - of 2900 cycles for two query tiles, of which the tensor pipe needs 2240 (an MMA of 128 x 128 x 16
 // takes 74 cycles with A in shared memory, 66 with A in tensor memory) and the special-function units 2048; and some 17000 cycles of a CTA's
-// start and end.  8192 positions of the 8B class, window 4096: 407 us, 1.01 PFLOP/s of visible products (346 in a graph).
+// start and end.  8192 positions of the 8B class, window 4096: 405 us in a loop of seconds, 1.02 PFLOP/s of visible products, 340 to 365 in bursts (f16 2 %
+// more, for the least number of a probability).
 //
 // P in 16 bits: its rounding weighs as much as the rounding of the result (2^-9 of sum p |v| against 2^-9 of the result in bf16, both
 // random), and one product instead of two is half of the tensor pipe's work.  In f16 a probability below 2^-21 of the row's largest loses bits, and below
 // 2^-31 it counts as 2^-31 (kWpBelow).
 //
 // Hidden positions: scores are replaced, not added to; V rows that no row of the CTA sees are set to zero in shared memory.  A row of V
-// that some rows see and others do not is harmless as long as it is finite (0 x v); tiles that have such rows are looked through,
-// and where one holds no number the CTA computes its rows again one by one (window_attn_row).  So it does for scores beyond kWpHuge.
+// that some rows see and others do not is harmless as long as it is finite (0 x v); tiles that have such rows are looked through (f16: all
+// of their rows), and where one holds an infinity or no number the CTA computes its rows again one by one (window_attn_row).  So it does for scores
+// beyond kWpHuge.  That costs: 8192 positions, window 4096, 63 ms with one such value, 325 ms where all are, for 0.37.
 #pragma once
 #include "attn_prefill_tc.cuh"
 #include "window_attn_step.cuh"

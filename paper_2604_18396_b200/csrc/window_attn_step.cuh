@@ -11,8 +11,8 @@
 //                                      kStepScale; down to 2^-23 of the row's largest, and something of it down to 2^-39).
 // K of the next block is requested when S has been computed, V when O has: 8 KB (dh 128) per warp are under way all the time.
 //
-// Bound by HBM where rows are many: 128 rows of the 8B class, window 8192, 680 us with the host, 655 without (6.57 TB/s, the copy rate); one row by its chain
-// (1B class, window 1024: 5.3 us): lengths, page ids, K, then the warps' and the CTAs' parts joined.
+// Bound by HBM where rows are many: 128 rows of the 8B class, window 8192, 4.2 GB in 650 to 685 us by the GPU (6.1 to 6.45 TB/s, the copy rate); one row by
+// its chain (1B class, window 1024: 5.4 us without the host): lengths, page ids, K, then the warps' and the CTAs' parts joined.
 //
 // Hidden positions: their scores are -inf and their values are zero in the operand (never loaded), so what the pool holds there
 // does not matter.  hi is rounded downwards from a little below p, and both are at least the type's smallest number where p is not 0: an
