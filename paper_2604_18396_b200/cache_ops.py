@@ -50,6 +50,12 @@ def _refuse(what: str):
     raise ValueError(what)
 
 
+def _ints(bits: int, what: str):
+    """`bits`: numbers or'ed together; ctypes would cut off what 32 bits do not hold (a negative one among them is refused by the library)."""
+    if not -0x80000000 <= bits <= 0x7fffffff:
+        _refuse(f"{what}: numbers of 32 bits")
+
+
 def _i32(t: torch.Tensor, shape, device: int, what: str) -> int:
     if t.dtype is not _I32 or t.get_device() != device or t.shape != shape or not t.is_contiguous():
         _refuse(f"{what}: a contiguous int32 tensor of shape {tuple(shape)} on CUDA device {device}")
@@ -106,6 +112,7 @@ def rope_frequencies(rotary_dim: int, theta: float, kind: str = "none", *, facto
     """river_rope_frequencies -> (CPU float32 [rotary_dim / 2] radians per position, factor on the turned values).
 
     kind: none, linear, by_parts, ramp, per_pair (see include/river.h); attn_scale 0 = the kind's own."""
+    _ints(rotary_dim | original_context, "rotary_dim, original_context")
     n = max(0, rotary_dim // 2)
     if kind not in ROPE_KINDS:
         _refuse(f"kind: one of {', '.join(ROPE_KINDS)}")
@@ -127,6 +134,7 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos
 
     q, k, v: [tokens, heads, dh] of the pool's type or float32, any strides over tokens and heads (q and q_out may be None); positions,
     seqs: int32 [tokens] (sequence -1: padding); inv_freq: float32 [rotary_dim / 2]; status: int32 [1], set where a token has no place."""
+    _ints(layer, "layer")
     dev = pool.get_device()
     c = _cache(pool, table, None, dev)
     n, hkv, dh = k.shape
@@ -155,6 +163,7 @@ def window_attention(q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, 
 
     q: [tokens, Hq, dh] of the pool's type (any strides over tokens and heads that are multiples of 8); sequence s has the rows q_start[s] ..
     q_start[s + 1] - 1 (int32 [n_seqs + 1]), its last positions, at most max_q of them; softmax_scale: default 1 / sqrt(dh)."""
+    _ints(layer | window | sinks | max_q, "layer, window, sinks, max_q")
     dev, qs = pool.get_device(), q.shape
     c = _cache(pool, table, lens, dev)
     if q.dtype is not pool.dtype or len(qs) != 3 or qs[2] != pool.shape[5]:
@@ -172,6 +181,7 @@ def pages_advance(table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, n
     """river_pages_advance: gives back the pages that window and sinks no longer need, hands out those of n_new[s] more positions.
 
     The outputs may be the inputs.  status (int32 [1]): 0, -4 (not enough pages: nothing was handed out) or -1."""
+    _ints(page_size | window | sinks, "page_size, window, sinks")
     dev, s, r = table.get_device(), table.shape, refs.shape
     if len(s) != 2 or len(r) != 1 or dev < 0:
         _refuse("table: [n_seqs, max_pages], refs: [n_pages], CUDA tensors")

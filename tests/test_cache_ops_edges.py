@@ -53,3 +53,25 @@ def test_a_status_off_its_word_is_refused(lib):
     c, rows = C.byref(checks.paged()), C.byref(cache_ops.river_rows(checks.P, 256, 64))
     assert lib.river_rope_append(c, 1, 4, 4, 0, rows, rows, rows, checks.P, checks.P, checks.P, 64, 0, 1.0, checks.P, ODD, 0) == -1
     assert lib.river_window_attention(c, 1, 4, 2, checks.P, 4, rows, 8, 0, 1.0, checks.P, ODD, 0) == -1
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """ctypes would hand on the lower half: a window of 2^32 + 5 as one of 5."""
+    pool, table, lens = torch.zeros(1, 2, 2, 1, 16, 64, dtype=torch.bfloat16), torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    q, big = torch.zeros(1, 1, 64, dtype=torch.bfloat16), 2 ** 32 + 5
+    args = dict(window=4, sinks=1, max_q=1)
+    for name in args:
+        for x in (big, 2 ** 31, -2 ** 31 - 1):
+            with pytest.raises(ValueError, match="32 bits"):
+                cache_ops.window_attention(q, q, lens, pool, 1, table, lens, **{**args, name: x})
+    with pytest.raises(ValueError, match="32 bits"):
+        cache_ops.window_attention(q, q, lens, pool, big, table, lens, **args)
+    with pytest.raises(ValueError, match="32 bits"):
+        cache_ops.rope_append(q, q, q, lens, lens, torch.zeros(32), pool, big, table, q)
+    for kw in (dict(page_size=big), dict(page_size=16, window=big), dict(page_size=16, sinks=big)):
+        with pytest.raises(ValueError, match="32 bits"):
+            cache_ops.pages_advance(table, lens, lens, lens, table, lens, lens, lens, **kw)
+    with pytest.raises(ValueError, match="32 bits"):
+        cache_ops.rope_frequencies(64, 1e4, "ramp", factor=4.0, original_context=2 ** 32 + 4096)
+    with pytest.raises(ValueError, match="32 bits"):
+        cache_ops.rope_frequencies(2 ** 32 + 64, 1e4)
