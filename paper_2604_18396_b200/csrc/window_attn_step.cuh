@@ -8,7 +8,7 @@
 //   softmax                            online, fp32, base 2: a row lies with four lanes.
 //   O^T [dh x 8 heads] += V^T P^T      S in its accumulator layout is the B operand; the A operand pairs the values of two keys, which a
 //                                      byte permutation makes of two loaded rows.  P = hi + lo, so that it keeps 16 bits and more (f16:
-//                                      kStepScale; down to 2^-23 of the row's largest, and something of it down to 2^-39).
+//                                      kStepScale; down to 2^-23 of the row's largest; what is not 0 counts as 2^-38 at least).
 // K of the next block is requested when S has been computed, V when O has: 8 KB (dh 128) per warp are under way all the time.
 //
 // Bound by HBM where rows are many: 128 rows of the 8B class, window 8192, 4.2 GB in 650 to 685 us by the GPU (6.1 to 6.45 TB/s, the copy rate); one row by
