@@ -403,6 +403,67 @@ int river_pages_reorder(const river_paged *c, const int32_t *refs, const int32_t
 int river_pages_compact(const river_paged *c, const int32_t *refs, int32_t *table_out, int32_t *refs_out, int32_t *remap,
                         int32_t *n_used, int32_t *moves, void *cuda_stream);
 
+/* ---------------------------------------------------------------- requests that share prefixes, on a paged cache
+ * What holds for the calls above holds for these: caller-owned buffers, asynchronous on cuda_stream, nothing allocated or read back, open to graphs.
+ *
+ * The page tables of a batch of requests from their lengths.  Sequence i becomes a request of total[i] positions that begins with the first
+ * begin[i] positions of what sequence like[i] was (-1: with none; its own number: it goes on).  Of those k = min(begin[i], lens[like[i]], total[i])
+ * positions it takes over whole pages, shared by reference (k is rounded down; a sequence that goes on with all it had keeps its last page too); the others'
+ * pages are the lowest free ids, in order of (sequence, position).  What a sequence held and nobody takes over is given back.
+ *   refs [dev] int32 [n_pages]; like, begin, total [dev] int32 [n_seqs]; n_seqs <= 8192; c->pool may be NULL
+ *   table_out, lens_out (= total), refs_out: the state behind the call; the outputs overlap no input
+ *   n_new     [dev] int32 [n_seqs]: positions of request i that are still to be computed, its last ones (total[i] less what it took over)
+ *   status    [dev] int32, always written: RIVER_OK; RIVER_E_NOPAGE (free pages or a table row do not suffice); RIVER_E_BADARG (a sequence, page
+ *             or length out of range).  Where it is not RIVER_OK the state behind the call is the state before it, and n_new is 0. */
+int river_pages_admit(const river_paged *c, const int32_t *refs, const int32_t *like, const int32_t *begin, const int32_t *total,
+                      int32_t *table_out, int32_t *lens_out, int32_t *refs_out, int32_t *n_new, int32_t *status, void *cuda_stream);
+
+/* Where the new tokens of a batch stand: sequence s has the rows q_start[s] .. q_start[s + 1] - 1 (the sums of n_new), its last n_new[s] of
+ * lens[s] positions.  Row t: positions[t] and seqs[t], as river_rope_append takes them, and slots[t] = page * page_size + place in the page, for
+ * kernels of the caller's own.  Rows behind the last sequence's (n_tokens is the number of rows, the sum of n_new may be less) are padding: -1 in all three.
+ *   q_start   [dev] int32 [n_seqs + 1];  positions, seqs [dev] int32 [n_tokens];  slots [dev] int64 [n_tokens];  n_seqs <= 8192
+ *   status    [dev] int32 or NULL: RIVER_E_BADARG where a position is negative or has no page (slots[t] is -1), n_new[s] is negative (it counts as
+ *             0), or there are more new tokens than rows (then every row is padding and q_start is 0). */
+int river_pages_slots(const river_paged *c, const int32_t *n_new, int n_tokens, int32_t *q_start, int32_t *positions, int32_t *seqs, int64_t *slots,
+                      int32_t *status, void *cuda_stream);
+
+/* Which neighbours share their first pages: c[s] is the number of equal first entries of the table's rows s - 1 and s, among the whole pages of positions
+ * that both held before their new tokens (lens[s] - (q_start[s + 1] - q_start[s])).  Sequence s goes on with the group of s - 1 where c[s] *
+ * page_size >= max(least, page_size); lead[s] is the first sequence of its group, shared[s] page_size times the least c of the group's others (0 for a
+ * sequence by itself).
+ *   least >= 1;  lead, shared [dev] int32 [n_seqs];  n_seqs <= 8192;  c->pool may be NULL */
+int river_prefix_groups(const river_paged *c, const int32_t *q_start, int least, int32_t *lead, int32_t *shared, void *cuda_stream);
+
+/* Causal attention over all positions of each sequence, where neighbours share their first ones: query i of n of sequence s stands at p = lens[s] -
+ * n + i and sees the positions j <= p;  out = softmax(softmax_scale q K^T) V over those, zero where there are none.  The sequences lead[s], .. of a
+ * group follow one another, and positions j < shared[s] are read once for all of them, from the row of lead[s] in the table; the others from the
+ * sequence's own row.  Every query of a group stands behind its shared positions.
+ *   q, q_start, max_q, softmax_scale, out   as river_window_attention has them;  Hq / Hkv at most 128;  n_tokens * Hq at most 2^30
+ *   lead      [dev] int32 [n_seqs]: the group's first sequence (s itself where s is that, or by itself)
+ *   shared    [dev] int32 [n_seqs]: a multiple of page_size, the same for a group's sequences, at most lens[s] - n; 0: none
+ *   max_own   about the most positions behind the shared ones that a sequence has, new ones included, by which the way of computing is chosen
+ *             (0: as many as a row of the table holds); the result does not depend on it but for rounding
+ *   workspace [dev] river_prefix_attention_bytes(n_seqs, n_tokens, Hq, Hkv, dh) bytes, 128-byte aligned; what it holds before does not matter, and calls
+ *             that may run at the same time have one each
+ *   status    [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as not visible);
+ *             lead or shared is not as described (rows of sequences that it concerns may hold anything); q_start descends, a length is negative (it
+ *             counts as 0), less than the sequence's queries or more than a row of the table holds (it counts as that), or a sequence has more than max_q
+ *             queries (the rows behind the max_q-th may stay as they are); RIVER_E_TIMEOUT when a wait ran out (any row may then hold anything).
+ * Positions that a query does not see have no influence on its result, whatever the pool holds there.  Every result follows in a fixed order of
+ * sums: the same inputs give the same bits. */
+int river_prefix_attention(const river_paged *c, int layer, int n_tokens, int max_q, int max_own, const int32_t *q_start, const int32_t *lead,
+                           const int32_t *shared, int Hq, const river_rows *q, float softmax_scale, void *out, void *workspace,
+                           size_t workspace_bytes, int32_t *status, void *cuda_stream);
+/* Self-test of river_prefix_attention: the same call by way 0 (single tokens), 1 (groups' keys in query tiles, then single tokens), 2 (both kinds of keys in
+ * query tiles), 3 (query tiles over all of a sequence's keys); 1 and 2 where
+ * sequences have less than two query tiles of rows on average, else RIVER_E_SHAPE.  A CTA of query
+ * tiles whose first keys are KV head `mute`'s (-1: none) never asks for them: its waits give up after poll_limit (1 .. 2^20) polls and status
+ * receives RIVER_E_TIMEOUT. */
+int river_selftest_prefix_attention(const river_paged *c, int layer, int n_tokens, int max_q, const int32_t *q_start, const int32_t *lead,
+                                    const int32_t *shared, int Hq, const river_rows *q, float softmax_scale, void *out, void *workspace,
+                                    size_t workspace_bytes, int32_t *status, int way, int mute, int poll_limit, void *cuda_stream);
+size_t river_prefix_attention_bytes(int n_seqs, int n_tokens, int Hq, int Hkv, int dh); /* 0: a shape that has no kernel */
+
 int river_seq_len(const river_ctx *ctx, int slot);       /* tokens cached in the slot, or RIVER_E_BADSLOT */
 int river_release(river_ctx *ctx, int slot);             /* free the slot's pages, behind the work queued so far; does not wait */
 int river_stats(river_ctx *ctx, river_stats_t *host_out); /* synchronises the stream; fills host_out even when it

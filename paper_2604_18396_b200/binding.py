@@ -60,7 +60,8 @@ EXPORTS = ("river_argmax_noalloc", "river_profile", "river_profile_read", "river
            "river_release", "river_stats", "river_destroy", "river_last_error", "river_clear_device_error",
            "river_selftest_wait_timeout", "river_attention", "river_project_kv", "river_quantize_w4", "river_generate", "river_offload", "river_exit_histogram",
            "river_suggest_offload", "river_rope_frequencies", "river_rope_append", "river_window_attention", "river_pages_advance",
-           "river_pages_reorder", "river_pages_compact", "river_selftest_window_timeout")
+           "river_pages_reorder", "river_pages_compact", "river_selftest_window_timeout", "river_pages_admit", "river_pages_slots", "river_prefix_groups",
+           "river_prefix_attention", "river_prefix_attention_bytes", "river_selftest_prefix_attention")
 
 _lib = None
 
@@ -110,6 +111,13 @@ def load():
     L.river_pages_advance.argtypes = [vp, vp, vp, C.c_int, C.c_int, vp, vp, vp, vp, vp]
     L.river_pages_reorder.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.river_pages_compact.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    L.river_pages_admit.argtypes = [vp] * 11
+    L.river_pages_slots.argtypes = [vp, vp, C.c_int, vp, vp, vp, vp, vp, vp]
+    L.river_prefix_groups.argtypes = [vp, vp, C.c_int, vp, vp, vp]
+    L.river_prefix_attention.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_int, vp, C.c_float, vp, vp, C.c_size_t, vp, vp]
+    L.river_selftest_prefix_attention.argtypes = L.river_prefix_attention.argtypes[:4] + L.river_prefix_attention.argtypes[5:-1] + [C.c_int, C.c_int, C.c_int, vp]
+    L.river_prefix_attention_bytes.argtypes = [C.c_int] * 5
+    L.river_prefix_attention_bytes.restype = C.c_size_t
     L.river_clear_device_error.argtypes = [vp]
     L.river_selftest_wait_timeout.argtypes = [vp, C.c_int]
     L.river_destroy.argtypes = [vp]

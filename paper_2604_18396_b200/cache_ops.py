@@ -1,4 +1,5 @@
-"""Operators for long contexts on a paged cache (river_rope_append, river_window_attention, river_pages_*), over torch tensors.
+"""Operators on a paged cache, for long contexts and for requests that share prefixes (river_rope_append, river_window_attention, river_prefix_*,
+river_pages_*), over torch tensors.
 
 Argument marshalling and checks only, like binding.py: every operator is one call into the CUDA library, asynchronous on `stream`
 (default: torch's current stream; another one has been ordered behind the inputs' by the caller); there is no fallback.  A cache is
@@ -221,3 +222,93 @@ def pages_compact(pool: torch.Tensor, table: torch.Tensor, refs: torch.Tensor, t
     _run(load().river_pages_compact, dev, stream, (pool, table, refs, table_out, refs_out, remap, n_used, moves), c, _i32(refs, r, dev, "refs"),
          _i32(table_out, s, dev, "table_out"), _i32(refs_out, r, dev, "refs_out"), _i32(remap, r, dev, "remap"), _i32(n_used, (1,), dev, "n_used"),
          _i32(moves, (1 + r[0],), dev, "moves"))
+
+
+def _table(table: torch.Tensor, lens: torch.Tensor, n_pages: int, page_size: int, device: int) -> bytes:
+    """A cache of which a call touches the page table only."""
+    s = table.shape
+    if len(s) != 2 or device < 0:
+        _refuse("table: [n_seqs, max_pages], a CUDA tensor")
+    return _PAGED.pack(0, _i32(table, s, device, "table"), _i32(lens, s[:1], device, "lens"), RIVER_BF16, 1, n_pages, 1, 64, page_size, s[0], s[1])
+
+
+def pages_admit(table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, like: torch.Tensor, begin: torch.Tensor, total: torch.Tensor,
+                table_out: torch.Tensor, lens_out: torch.Tensor, refs_out: torch.Tensor, n_new: torch.Tensor, status: torch.Tensor, *,
+                page_size: int, stream=None) -> None:
+    """river_pages_admit: sequence i becomes a request of total[i] positions that begins with the first begin[i] of what sequence like[i] was (-1:
+    none; i: it goes on); whole pages are shared, the others the lowest free ones.
+
+    The outputs overlap no input.  n_new (int32 [n_seqs]): positions that are still to be computed; status (int32 [1]): 0, -4 (not enough pages: the
+    state as it was) or -1."""
+    _ints(page_size, "page_size")
+    dev, s, r = table.get_device(), table.shape, refs.shape
+    if len(r) != 1:
+        _refuse("refs: [n_pages]")
+    c = _table(table, lens, r[0], page_size, dev)
+    n = s[:1]
+    _run(load().river_pages_admit, dev, stream, (table, lens, refs, like, begin, total, table_out, lens_out, refs_out, n_new, status), c,
+         _i32(refs, r, dev, "refs"), _i32(like, n, dev, "like"), _i32(begin, n, dev, "begin"), _i32(total, n, dev, "total"),
+         _i32(table_out, s, dev, "table_out"), _i32(lens_out, n, dev, "lens_out"), _i32(refs_out, r, dev, "refs_out"), _i32(n_new, n, dev, "n_new"),
+         _i32(status, (1,), dev, "status"))
+
+
+def pages_slots(table: torch.Tensor, lens: torch.Tensor, n_new: torch.Tensor, q_start: torch.Tensor, positions: torch.Tensor, seqs: torch.Tensor,
+                slots: torch.Tensor, *, page_size: int, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """river_pages_slots: where the last n_new[s] positions of each sequence stand, row by row.
+
+    q_start: int32 [n_seqs + 1]; positions, seqs: int32 [tokens]; slots: int64 [tokens], page * page_size + place in the page.  Rows behind the
+    last sequence's are -1 (padding, as rope_append has it)."""
+    _ints(page_size, "page_size")
+    dev = table.get_device()
+    c = _table(table, lens, 1, page_size, dev)
+    t = positions.shape
+    if len(t) != 1:
+        _refuse("positions: [tokens]")
+    if slots.dtype is not torch.int64 or slots.get_device() != dev or slots.shape != t or not slots.is_contiguous():
+        _refuse(f"slots: a contiguous int64 tensor of shape {tuple(t)} on CUDA device {dev}")
+    _run(load().river_pages_slots, dev, stream, (table, lens, n_new, q_start, positions, seqs, slots, status), c, _i32(n_new, lens.shape, dev, "n_new"), t[0],
+         _i32(q_start, (table.shape[0] + 1,), dev, "q_start"), _i32(positions, t, dev, "positions"), _i32(seqs, t, dev, "seqs"), slots.data_ptr(),
+         0 if status is None else _i32(status, (1,), dev, "status"))
+
+
+def prefix_groups(table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor, lead: torch.Tensor, shared: torch.Tensor, *, page_size: int,
+                  least: int = 1, stream=None) -> None:
+    """river_prefix_groups: lead[s] = the first sequence of the group that s shares its first pages with, shared[s] = how many positions.
+
+    Groups are neighbours that share `least` positions or more before their new tokens, of which sequence s has q_start[s + 1] - q_start[s]."""
+    _ints(page_size | least, "page_size, least")
+    dev = table.get_device()
+    c = _table(table, lens, 1, page_size, dev)
+    _run(load().river_prefix_groups, dev, stream, (table, lens, q_start, lead, shared), c, _i32(q_start, (table.shape[0] + 1,), dev, "q_start"), least,
+         _i32(lead, lens.shape, dev, "lead"), _i32(shared, lens.shape, dev, "shared"))
+
+
+def prefix_attention(q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, pool: torch.Tensor, layer: int, table: torch.Tensor, lens: torch.Tensor,
+                     lead: torch.Tensor, shared: torch.Tensor, *, max_q: int, max_own: int = 0, softmax_scale: Optional[float] = None,
+                     workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """river_prefix_attention: out[t] = causal attention of q[t] over its sequence, the first shared[s] positions read once for the group of lead[s].
+
+    q: [tokens, Hq, dh] of the pool's type (any strides over tokens and heads that are multiples of 8); sequence s has the rows q_start[s] ..
+    q_start[s + 1] - 1 (int32 [n_seqs + 1]), its last positions, at most max_q of them; max_own: about the most positions behind the shared ones (0: not
+    known); softmax_scale: default 1 / sqrt(dh); workspace (uint8): prefix_attention_bytes of them, for callers who keep one."""
+    _ints(layer | max_q | max_own, "layer, max_q, max_own")
+    dev, qs, n = pool.get_device(), q.shape, lens.shape
+    c = _cache(pool, table, lens, dev)
+    if q.dtype is not pool.dtype or len(qs) != 3 or qs[2] != pool.shape[5]:
+        _refuse("q: [tokens, Hq, dh] of the pool's type")
+    if out.dtype is not q.dtype or out.shape != qs or out.get_device() != dev or not out.is_contiguous():
+        _refuse("out: contiguous, q's shape and type")
+    if workspace is None:
+        workspace = _scratch(-(-prefix_attention_bytes(table.shape[0], qs[0], qs[1], pool.shape[3], qs[2]) // 4), pool.device, stream)
+    elif workspace.dtype is not torch.uint8 or workspace.dim() != 1 or workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse("workspace: contiguous CUDA uint8 [bytes]")
+    _run(load().river_prefix_attention, dev, stream, (q, out, q_start, pool, table, lens, lead, shared, workspace, status), c, layer, qs[0], max_q, max_own,
+         _i32(q_start, (table.shape[0] + 1,), dev, "q_start"), _i32(lead, n, dev, "lead"), _i32(shared, n, dev, "shared"), qs[1], _rows(q, dev, "q"),
+         qs[2] ** -0.5 if softmax_scale is None else softmax_scale, out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+         0 if status is None else _i32(status, (1,), dev, "status"))
+
+
+def prefix_attention_bytes(n_seqs: int, tokens: int, hq: int, hkv: int, dh: int) -> int:
+    """river_prefix_attention_bytes: of the workspace of prefix_attention."""
+    _ints(n_seqs | tokens | hq | hkv | dh, "n_seqs, tokens, heads, dh")
+    return load().river_prefix_attention_bytes(n_seqs, tokens, hq, hkv, dh)

@@ -1,0 +1,642 @@
+// Attention over shared prefixes on tcgen05 (sm_100a, internal): the units of prefix_units.cuh.
+//
+// One CTA per SM walks its part of the row of units, 128 keys at a time, without a stop between units: the loads of the next one are under way
+// while a unit ends.
+//   S [128 x 128] = Q K^T     Q and K in shared memory, S in tensor memory
+//   O [128 x DH] += P V       P (rounded to the inputs' type) in tensor memory over the place of S, V as it lies in the cache
+//   warp 0        TMA: K and V pages, one 16 x 64 box per lane, three places for K, two for V
+//   warp 1        tensor memory; one lane issues the MMAs: P V of a stream, S of its next keys, then the other stream's, so that the softmax of
+//                 one runs under the MMAs of the other
+//   warp 2        the parts of units, one ahead
+//   warps 4..11   softmax, four per stream: thread = query row = TMEM lane; online, base 2, fp32; all 128 scores of a row in registers; O is
+//                 rescaled only when a row's maximum has grown by more than 2^8 since it last was.  P goes out in two halves.
+// Two streams: the two query tiles of a unit, over the same K and V; or, where a unit has one query tile, its even and its odd key tiles, joined
+// through shared memory when the keys are through (dual).
+//
+// P in 16 bits: its rounding weighs as much as the rounding of the result (2^-9 of sum p |v| against 2^-9 of the result in bf16, both
+// random).  In f16 a probability below 2^-21 of the row's largest loses bits, and below 2^-31 it counts as 2^-31 (kWpBelow).
+//
+// Hidden positions: scores are replaced, not added to; V rows that no row of the unit sees are set to zero in shared memory.  A row of V
+// that some rows see and others do not is harmless as long as it is finite (0 x v); tiles that have such rows are looked through (f16: all
+// of their rows), and where one holds an infinity or no number the part is computed again row by row (pf_row).  So it is for scores beyond
+// kWpHuge.
+#pragma once
+#include "prefix_units.cuh"
+#include "window_attn_prompt.cuh"
+
+namespace river {
+
+// A part of a unit, as the warps of a CTA hand it on
+struct PfSeg {
+    int n_kt, t0;          // key tiles (0: that was the last part), the first one
+    int tok0, n_tok, kvh;  // rows
+    int seq, base, keys;   // whose row of the table, from which position on, how many
+    int causal, pos0;      // a sequence's unit: position of the first token
+    int64_t row;           // first row in the scratch; -1: the result's
+};
+
+// Exclusive prefix sum over the CTA's threads (`part`: one per warp); `total` gets the sum.  Ends with a barrier behind every read.
+__device__ __forceinline__ int64_t pf_scan(int64_t x, int64_t *part, int64_t &total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t inc = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    if (lane == 31) part[warp] = inc;
+    __syncthreads();
+    int64_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kWpThreads / 32; ++w) {
+        const int64_t y = part[w];
+        if (w < warp) before += y;
+        total += y;
+    }
+    __syncthreads();
+    return before + inc - x;
+}
+
+// One row over the positions [lo, hi) of a row of the table, by one warp in their order: O (not divided), maximum and sum.
+template <class T, int DH>
+__device__ void pf_row(const PrefixArgs &a, int token, int head, int seq, int lo, int hi, float (&o)[DH / 32], float &m, float &l) {
+    constexpr int E = DH / 32;
+    const int lane = threadIdx.x & 31, kvh = head / a.p.gq, pmask = (1 << a.c.ps_log2) - 1;
+    const T *q = static_cast<const T *>(a.q) + token * a.q_tok + head * a.q_head + E * lane, *pool = reinterpret_cast<const T *>(a.c.pool);
+    float x[E];
+    m = -CUDART_INF_F;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) { x[e] = to_f(q[e]) * a.scale_log2; o[e] = 0.f; }
+    for (int j = lo; j < hi; ++j) {
+        const int col = j >> a.c.ps_log2, page = col < a.c.max_pages ? a.c.table[(size_t)seq * a.c.max_pages + col] : -1;
+        if (page < 0 || page >= a.c.n_pages) continue;
+        const T *k = pool + a.c.row(a.layer0, page, 0, kvh, j & pmask) + E * lane, *v = pool + a.c.row(a.layer0, page, 1, kvh, j & pmask) + E * lane;
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += x[e] * to_f(k[e]);
+        s = warp_sum(s);
+        const float mx = fmaxf(m, s), base = mx == -CUDART_INF_F ? 0.f : mx, corr = exp2f(m - base), p = exp2f(s - base);
+        m = mx;
+        l = l * corr + p;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = o[e] * corr + p * to_f(v[e]);
+    }
+}
+
+template <class T, int DH>
+__global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __grid_constant__ CUtensorMap tmap, const PrefixArgs a) {
+    constexpr int NB = DH / 64;                                          // blocks of 64 dims
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    constexpr uint32_t QB = kWpRows * 128, KB = kWpKeys * 128;           // bytes of one block of Q / of K or V
+    constexpr uint32_t kO = 256;                                         // TMEM: stream q has S / P in columns 128 q .., O in 256 + DH q ..
+    constexpr uint32_t kIdS = (1u << 4) | (kHalf ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(kWpRows >> 4) << 24) | ((uint32_t)(kWpKeys >> 3) << 17);
+    constexpr uint32_t kIdO = (kIdS & ~(0x3Fu << 17)) | ((uint32_t)(DH >> 3) << 17) | (1u << 16);  // (B of the second product: N-major)
+    extern __shared__ uint8_t wp_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(wp_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *const sq = smem, *const sv = sq + 2 * NB * QB, *const sk = sv + 2 * NB * KB;  // [tile], [2 places of V], [3 of K] [NB][128 rows][128 bytes]
+    // K of the first tile there; V of tile i and K of tile i + 1 there (4, in turn; tiles are counted over all units); V and K of tile i before
+    // free (2); per stream: S done (2), P written (2 x 2), O done (2); Q there; a part there (2), no longer needed (2)
+    __shared__ uint64_t bars[20];
+    __shared__ int64_t s_part[kWpThreads / 32], s_at;
+    __shared__ PfSeg s_seg[2];
+    __shared__ float2 s_ml[kWpRows];  // dual: the second stream's maxima and sums
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_first, s_abort, s_no_page, s_poison[2], s_missing[2];
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+    const int gq = a.p.gq, per = pf_per(gq), span = 2 * per, S = a.c.n_seqs, D = pf_entries(a);
+    const uint32_t b_first = smem_u32(&bars[0]), b_full = b_first + 8, b_free = b_full + 32, b_s = b_free + 16, b_p = b_s + 16, b_o = b_p + 32, b_q = b_o + 16,
+                   b_seg = b_q + 8, b_used = b_seg + 16;
+    volatile int *abortp = &s_abort;
+    if (tid == 0) {
+        s_abort = s_no_page = s_poison[0] = s_poison[1] = s_missing[0] = s_missing[1] = 0;
+        s_first = -1;
+        for (int i = 0; i < 20; ++i) mbar_init(smem_u32(&bars[i]), i >= 9 && i < 13 ? 4 : i == 15 ? 8 : i >= 18 ? 10 : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+
+    // ---- this CTA's part of the row of units
+    int64_t all = 0, at = 0, mine = 0, total;
+    for (int i0 = 0; i0 < D; i0 += kWpThreads) {
+        const int64_t w = i0 + tid < D ? pf_entry(a, i0 + tid, span).w : 0, before = pf_scan(w, s_part, total);
+        if (i0 == 0) at = before, mine = w;
+        all += total;
+    }
+    const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.p.ctas);
+    const int64_t x0 = blockIdx.x * share, x1 = min(x0 + share, everything);
+    if (x0 < everything || blockIdx.x == 0) {
+        const int64_t xl = all ? x0 % all : 0;
+        int64_t base = 0;
+        for (int i0 = 0; i0 < D; i0 += kWpThreads) {
+            const int i = i0 + tid;
+            if (D > kWpThreads) {  // (else they are known)
+                mine = i < D ? pf_entry(a, i, span).w : 0;
+                at = base + pf_scan(mine, s_part, total);
+                base += total;
+            }
+            if (mine && at <= xl && xl < at + mine) s_first = i, s_at = at;
+            if (blockIdx.x == 0 && i < D) {  // for who joins the parts
+                if (!a.p.groups || i >= S) a.own_at[a.p.groups ? i - S : i] = at;
+                else if (mine) {
+                    const PfEntry e = pf_entry(a, i, span);
+                    a.group[e.seq] = PfGroup{at, e.tok0, e.keys};
+                }
+            }
+        }
+        if (blockIdx.x == 0) {
+            if (tid == 0) *a.head = PfHead{all, share};
+            for (int s = tid; s < S; s += kWpThreads)
+                if (!pf_sound(a, s)) flag(a.status, RIVER_E_BADARG);
+        }
+    }
+    if (x0 >= everything) {
+        pdl_launch();
+        return;
+    }
+    if (warp == 1) {
+        tc_alloc(smem_u32(&s_tmem), 512u);
+        pdl_launch();
+        tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = uniform(s_tmem);
+    // the next part; whether there is one.  `used`: told at once that it has been read
+    auto take = [&](int n, PfSeg &g) {
+        wp_wait(b_seg + 8 * (n & 1), n >> 1, abortp, a.polls);
+        g = s_seg[n & 1];
+        return g.n_kt > 0 && !__any_sync(0xffffffffu, *abortp);
+    };
+    auto used = [&](int n) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_used + 8 * (n & 1));
+    };
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 2) {  // ---- the parts
+            int64_t x = x0, ent = s_at;  // (ent: the weight before the entry, of this KV head)
+            int i = s_first, kvh = (int)(x0 / all), n = 0;
+            while (true) {
+                const PfEntry e = pf_entry(a, i, span);
+                int64_t y = x - kvh * all - ent;  // within the entry
+                for (int t = pf_unit_at(e, y, span); x < x1 && y < e.w; ++t) {
+                    const PfUnit u = pf_unit(e, t, span);
+                    const PfPart p = pf_part(a.p, share, x - y + u.at, u, blockIdx.x, kvh, e.group);
+                    if (p.k1 > p.k0) {
+                        if (n >= 2) wp_wait(b_used + 8 * (n & 1), (n >> 1) - 1, abortp, a.polls);
+                        if (lane == 0) {
+                            s_seg[n & 1] = PfSeg{p.k1 - p.k0, p.k0, u.tok, u.n, kvh, e.seq, e.base, u.keys, !e.group, e.pos0 + u.tok - e.tok0, p.row};
+                            mbar_arrive(b_seg + 8 * (n & 1));
+                        }
+                        ++n;
+                    }
+                    x += u.at + u.w - y;
+                    y = u.at + u.w;
+                }
+                if (x >= x1 || __any_sync(0xffffffffu, *abortp)) break;
+                // the next entry that has units: from behind this one, or the next KV head's first
+                ent += e.w;
+                int i0 = i + 1;
+                while (true) {
+                    if (i0 >= D) i0 = 0, ++kvh, ent = 0;
+                    const unsigned there = __ballot_sync(0xffffffffu, i0 + lane < D && pf_entry(a, i0 + lane, span).w > 0);
+                    if (there) {
+                        i = i0 + __ffs(there) - 1;
+                        break;
+                    }
+                    i0 += 32;
+                }
+            }
+            if (n >= 2) wp_wait(b_used + 8 * (n & 1), (n >> 1) - 1, abortp, a.polls);
+            if (lane == 0) {
+                s_seg[n & 1].n_kt = 0;
+                mbar_arrive(b_seg + 8 * (n & 1));
+            }
+        } else if (warp == 0) {  // ---- K and V
+            const int blk = lane / NB, half = lane % NB, bpp = a.c.ps_log2 - 4;
+            PfSeg g, f;  // of the tile whose V is loaded, of the one whose K is
+            int n = 0, j = -1, place = 0;
+            auto page_of = [&](const PfSeg &s, int t) {  // of this lane's block of tile t; -1: none
+                const int u = 8 * (s.t0 + t) + blk, col = ((s.base >> 4) + u) >> bpp;
+                const int page = blk < 8 && t < s.n_kt && 16 * u < s.keys && col < a.c.max_pages ? a.c.table[(size_t)s.seq * a.c.max_pages + col] : -1;
+                return page < a.c.n_pages ? max(page, -1) : -1;
+            };
+            auto load = [&](const PfSeg &s, int t, uint8_t *dst, int page, int v, uint32_t bar) {
+                const int row = ((page * 2 * a.c.Hkv + s.kvh + v * a.c.Hkv) << a.c.ps_log2) + ((s.base + 16 * (8 * (s.t0 + t) + blk)) & ((1 << a.c.ps_log2) - 1));
+                if (page >= 0) tma_load_2d(smem_u32(dst) + half * KB + blk * 2048, &tmap, 64 * half, row, bar);
+            };
+            bool more = take(n, f);
+            used(n++);
+            if (more && f.kvh == a.mute) more = false;
+            int jf = 0, page = -1, ahead = more ? page_of(f, 0) : -1;
+            uint32_t bytes = 0;
+            for (int i = -1; more || i >= 0; ++i) {
+                // V of tile i (g, j), K of tile i + 1 (f, jf)
+                const int next = more ? ahead : -1;
+                if (more) {
+                    if (blk < 8 && 16 * (8 * (f.t0 + jf) + blk) < f.keys && next < 0) s_no_page = 1;
+                    ahead = page_of(f, jf + 1);  // (under way while this tile waits for its place)
+                }
+                const uint32_t k_bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, next >= 0)) * 2048u, bar = i < 0 ? b_first : b_full + 8 * (i & 3);
+                if (i >= 2) wp_wait(b_free + 8 * (i & 1), (i >> 1) - 1, abortp, a.polls);
+                if (__any_sync(0xffffffffu, *abortp)) break;
+                if (lane == 0) mbar_expect_tx(bar, bytes + k_bytes);
+                __syncwarp();
+                if (more) load(f, jf, sk + place * NB * KB, next, 0, bar);
+                if (i >= 0) load(g, j, sv + (i & 1) * NB * KB, page, 1, bar);
+                if (!more) break;
+                page = next;
+                bytes = k_bytes;
+                place = place == 2 ? 0 : place + 1;
+                g = f;
+                j = jf;
+                if (++jf == f.n_kt) {
+                    more = take(n, f);
+                    used(n++);
+                    jf = 0;
+                    ahead = more ? page_of(f, 0) : -1;
+                }
+            }
+        } else if (warp == 1) {  // ---- the products
+            const uint64_t dq = tc_smem_desc(smem_u32(sq)), dk = tc_smem_desc(smem_u32(sk)), dv = pt_desc_n(smem_u32(sv), KB);
+            const bool leader = elect_one();
+            PfSeg g;
+            int i0 = 0, cp0 = 0, cp1 = 0;  // tiles of the parts before; of each stream
+            int k_i = 0, place = 0;        // K of tile k_i is next, at `place`
+            auto scores = [&](int q, int tile) {  // S of stream q: query tile `tile` and the next K
+                wp_wait(k_i == 0 ? b_first : b_full + 8 * ((k_i - 1) & 3), k_i == 0 ? 0 : (k_i - 1) >> 2, abortp, a.polls);
+                tc_fence_after();
+                const uint64_t k_desc = dk + place * (NB * KB >> 4);
+                if (leader) {
+#pragma unroll
+                    for (int k = 0; k < DH / 16; ++k)
+                        tc_mma(tmem + 128u * q, dq + (tile * NB + (k >> 2)) * (QB >> 4) + 2 * (k & 3), k_desc + (k >> 2) * (KB >> 4) + 2 * (k & 3), kIdS, k ? 1u : 0u);
+                    tc_commit(b_s + 8 * q);
+                }
+                __syncwarp();
+            };
+            auto next_k = [&] { ++k_i; place = place == 2 ? 0 : place + 1; };
+            auto values = [&](int q, int i, int count, bool fresh, bool frees) {  // O of stream q += P V of tile i
+                const uint64_t v = dv + (i & 1) * (NB * KB >> 4);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {  // half of the keys
+                    wp_wait(b_p + 8 * (2 * q + h), count, abortp, a.polls);
+                    tc_fence_after();
+                    if (leader) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)  // 16 keys: 8 columns of P, 2048 bytes of V
+                            tc_mma_ts(tmem + kO + (uint32_t)DH * q, tmem + 128u * q + 32 * h + 8 * k, v + (4 * h + k) * (2048 >> 4), kIdO, !fresh || h || k ? 1u : 0u);
+                        if (h == 1 && frees) tc_commit(b_free + 8 * (i & 1));
+                    }
+                    __syncwarp();
+                }
+            };
+            for (int n = 0;; ++n) {
+                const bool more = take(n, g);
+                used(n);
+                if (!more) break;
+                const int n_t = uniform(g.n_kt), nq = g.n_tok > per ? 2 : 1;
+                const bool dual = nq == 1 && n_t > 1;
+                wp_wait(b_q, n, abortp, a.polls);
+                scores(0, 0);
+                if (dual) {
+                    next_k();
+                    scores(1, 0);
+                } else if (nq == 2) scores(1, 1);
+                next_k();
+                for (int j = 0; j < n_t; ++j) {
+                    const int i = i0 + j;
+                    wp_wait(b_full + 8 * (i & 3), i >> 2, abortp, a.polls);
+                    if (dual) {
+                        const int q = j & 1;
+                        values(q, i, q ? cp1++ : cp0++, j < 2, true);
+                        if (j + 2 < n_t) {
+                            scores(q, 0);
+                            next_k();
+                        } else if (leader) tc_commit(b_o + 8 * q);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            if (q == nq) break;
+                            values(q, i, q ? cp1++ : cp0++, j == 0, q == nq - 1);
+                            if (j + 1 < n_t) scores(q, q);
+                            else if (leader) tc_commit(b_o + 8 * q);
+                        }
+                        if (j + 1 < n_t) next_k();
+                    }
+                    __syncwarp();
+                    if (*abortp) break;
+                }
+                i0 += n_t;
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int q = (warp - 4) >> 2, r = 32 * (warp & 3) + lane, u0 = tid - 128, inv_gq = 65536 / gq + 1;  // (r * inv_gq >> 16 = r / gq for r < 128)
+        const uint32_t turn = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+        const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + 128u * q + quarter, t_o = tmem + kO + (uint32_t)DH * q + quarter;
+        const float c = fmaxf(fabsf(a.scale_log2), 1e-30f);  // (a scale of 0: every score 0, hidden ones -inf still)
+        const int bpp = a.c.ps_log2 - 4;
+        PfSeg g;
+        int i0 = 0, count = 0, ended = 0;  // tiles of the parts before; tiles, and parts, of this stream
+        for (int n = 0;; ++n) {
+            // the part before: where something in it was no number, its rows again
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (n > 0 && s_poison[(n - 1) & 1] && !*abortp)
+#pragma unroll 1
+                for (int x = warp - 4; x < g.n_tok * gq; x += 8) {
+                    const int token = g.tok0 + x / gq, lo = g.base + kPfKeys * g.t0;
+                    const int hi = g.base + min(min(g.keys, kPfKeys * (g.t0 + g.n_kt)), g.causal ? g.pos0 + x / gq + 1 - g.base : g.keys);
+                    float o[DH / 32], m, l;
+                    pf_row<T, DH>(a, token, g.kvh * gq + x % gq, g.seq, lo, hi, o, m, l);
+                    if (g.row < 0) {
+                        T *out = static_cast<T *>(a.out) + ((size_t)token * a.p.Hq + g.kvh * gq + x % gq) * DH + DH / 32 * lane;
+#pragma unroll
+                        for (int e = 0; e < DH / 32; ++e) out[e] = from_f<T>(l == 0.f ? 0.f : o[e] / l);
+                    } else {
+                        if (lane == 0) a.ml[g.row + x] = make_float2(m, l);
+#pragma unroll
+                        for (int e = 0; e < DH / 32; ++e) a.o[(g.row + x) * DH + DH / 32 * lane + e] = o[e];
+                    }
+                }
+            if (n > 0) used(n - 1);
+            {  // one answer for all eight warps: nobody leaves while others wait at a barrier
+                const bool more = take(n, g);
+                uint32_t none = more ? 0u : 1u;
+                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %0, 0;\n\tbarrier.cta.red.or.pred p, 1, 256, q;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "+r"(none)::"memory");
+                if (none) break;
+            }
+            const int nq = g.n_tok > per ? 2 : 1;
+            const bool dual = nq == 1 && g.n_kt > 1;
+            {  // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
+                constexpr int C8 = DH / 8, U = C8;  // 16-byte chunks of a row; all of a thread's are under way together
+                const int c8 = u0 % C8;
+                const T *src = static_cast<const T *>(a.q) + g.tok0 * a.q_tok + g.kvh * gq * a.q_head + 8 * c8;
+                uint4 x[U];
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int rr = u0 / C8 + i * (256 / C8), rx = rr % kWpRows, pp = rx * inv_gq >> 16, p = rr / kWpRows * per + pp, h = rx - pp * gq;
+                    x[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (pp < per && p < g.n_tok) x[i] = *reinterpret_cast<const uint4 *>(src + p * a.q_tok + h * a.q_head);
+                }
+                bool missing = false;
+                for (int u = 8 * g.t0 + u0; u < 8 * (g.t0 + g.n_kt) && 16 * u < g.keys; u += 256) {
+                    const int col = ((g.base >> 4) + u) >> bpp, page = col < a.c.max_pages ? a.c.table[(size_t)g.seq * a.c.max_pages + col] : -1;
+                    missing = missing || page < 0 || page >= a.c.n_pages;
+                }
+                if (missing) s_missing[n & 1] = 1;
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int rr = u0 / C8 + i * (256 / C8), rx = rr % kWpRows;
+                    x[i].x ^= turn; x[i].y ^= turn; x[i].z ^= turn; x[i].w ^= turn;
+                    *reinterpret_cast<uint4 *>(sq + rr / kWpRows * NB * QB + (c8 >> 3) * QB + rx * 128 + (((c8 & 7) ^ (rx & 7)) * 16)) = x[i];
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_q);
+                asm volatile("bar.sync 1, 256;" ::: "memory");  // (s_missing; the part before is through with its s_poison)
+                if (tid == 128) s_missing[(n + 1) & 1] = s_poison[(n + 1) & 1] = 0;
+            }
+            float m = -CUDART_INF_F, l = 0.f;
+            const int row_q = dual ? 0 : q, p = row_q * per + r / gq;
+            if (dual || q < nq) {
+                const int pos = g.pos0 + min(p, g.n_tok - 1);
+                // columns (positions from g.base on) that this row sees, that all rows of the unit see, that some row sees
+                const int hi = g.causal ? pos + 1 - g.base : g.keys, all_hi = g.causal ? g.pos0 + 1 - g.base : g.keys;
+                const bool missing = s_missing[n & 1] != 0;
+                auto huge = [&] { if (fabsf(m) > kWpHuge<T> && m != -CUDART_INF_F) s_poison[n & 1] = 1; };
+                for (int j = dual ? q : 0; j < g.n_kt; j += dual ? 2 : 1) {
+                    const int i = i0 + j, c0 = kPfKeys * (g.t0 + j);
+                    const bool fresh = j == (dual ? q : 0);
+                    uint32_t valid = 0xffu;  // blocks that are there
+                    bool part = c0 + kPfKeys > all_hi;
+                    if (missing) {
+#pragma unroll 1
+                        for (int b = 0; b < 8; ++b) {
+                            const int u = 8 * (g.t0 + j) + b, col = ((g.base >> 4) + u) >> bpp;
+                            const int page = col < a.c.max_pages ? a.c.table[(size_t)g.seq * a.c.max_pages + col] : -1;
+                            if (page < 0 || page >= a.c.n_pages) valid &= ~(1u << b);
+                        }
+                        part = part || valid != 0xffu;
+                    }
+                    if (part && (dual || q == 0)) {  // thread = V row: those that nobody sees become zero, the others are looked through
+                        wp_wait(b_full + 8 * (i & 3), i >> 2, abortp, a.polls);
+                        const int cc = c0 + r;
+                        uint8_t *row = sv + (i & 1) * NB * KB + r * 128;
+                        if (!kHalf && (valid >> (r >> 4) & 1u) && cc < all_hi) {
+                            // (seen by every row: whatever it is, it belongs in every result)
+                        } else if ((valid >> (r >> 4) & 1u) && cc < g.keys) {
+                            // an exponent of ones (what is no number) and one more carries into the sign's place
+                            constexpr uint32_t E = kHalf ? 0x7c007c00u : 0x7f807f80u, ONE = E & ~(E << 1);
+                            uint32_t odd = 0u;
+#pragma unroll
+                            for (int d = 0; d < DH / 8; ++d) {
+                                const uint4 y = *reinterpret_cast<const uint4 *>(row + (d >> 3) * KB + (((d & 7) ^ (r & 7)) * 16));
+                                odd |= ((y.x & E) + ONE) | ((y.y & E) + ONE) | ((y.z & E) + ONE) | ((y.w & E) + ONE);
+                            }
+                            if (odd & 0x80008000u) s_poison[n & 1] = 1;
+                        } else {
+#pragma unroll
+                            for (int d = 0; d < DH / 8; ++d) *reinterpret_cast<uint4 *>(row + (d >> 3) * KB + (((d & 7) ^ (r & 7)) * 16)) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    wp_wait(b_s + 8 * q, count++, abortp, a.polls);
+                    __syncwarp();
+                    tc_fence_after();
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) wp_ld32(t_s + 32 * x, s[x]);
+                    wp_ld_wait();
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) wp_pin(s[x]);
+                    if (part) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const uint32_t there = (valid >> (2 * x) & 1u ? 0xffffu : 0u) | (valid >> (2 * x + 1) & 1u ? 0xffff0000u : 0u);
+                            const uint32_t see = bits_between(0, hi - c0 - 32 * x) & there;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) s[x][e] = see >> e & 1u ? s[x][e] : 0xff800000u;  // -inf
+                        }
+                    }
+                    // The first half is made with the maximum as it stood; only where the tile's own maximum, found meanwhile, has grown too
+                    // far past it (a first tile, a rare later one) it is made again.
+                    uint64_t sum;
+                    uint32_t w[32];
+                    // A probability that f16 has no number for would make 0 x inf of an infinite value: where every row sees every key it counts as 2^-24
+                    // (2^-31 of the row's largest); tiles in parts are looked through.
+                    const uint32_t least = part ? 0u : 0x00010001u;
+                    const uint64_t c2 = f2_pack(c, c);
+                    auto top = [&] {
+                        float x[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                        for (int y = 0; y < 4; ++y)
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[y][e]), __uint_as_float(s[y][e + 1]));
+                        return max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
+                    };
+                    if (fresh) {
+                        const float mx = top();
+                        m = mx < CUDART_INF_F ? (kHalf ? mx - kWpBelow : mx) : CUDART_NAN_F;
+                        huge();
+                    }
+                    while (true) {
+                        sum = 0ull;
+                        const float base = m == -CUDART_INF_F ? 0.f : m, mx = top();
+                        wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), least, sum, w);
+                        bool grow;
+                        float corr;
+                        if constexpr (kHalf) {  // (by the difference, which is exact where the two are near: no rounding of a large m makes P infinite)
+                            grow = !(mx - fmaxf(m, -3e38f) <= kWpLazy + kWpBelow) && !(m != m);
+                            corr = grow ? ex2(m - (mx - kWpBelow)) : 1.f;
+                        } else {
+                            grow = !(mx <= m + kWpLazy) && !(m != m);  // (a maximum that is no number stays)
+                            corr = grow ? ex2(m - mx) : 1.f;
+                        }
+                        if (!__any_sync(0xffffffffu, grow)) break;
+                        if (grow) m = mx < CUDART_INF_F ? (kHalf ? mx - kWpBelow : mx) : CUDART_NAN_F;  // (inf - inf, as the formula has it)
+                        huge();
+                        l *= corr;
+                        if (!fresh) {  // (the MMAs that wrote O are complete: S of these keys was issued behind them)
+#pragma unroll 1
+                            for (int d = 0; d < DH; d += 32) {
+                                uint32_t o[32];
+                                wp_ld32(t_o + d, o);
+                                wp_ld_wait();
+                                wp_pin(o);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr);
+                                tc_st32(t_o + d, o);
+                            }
+                        }
+                    }
+                    auto hand_over = [&](int h) {
+                        tc_st32(t_s + 32 * h, w);
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(b_p + 8 * (2 * q + h));
+                    };
+                    hand_over(0);
+                    wp_pin(s[2]);  // (no probability of the second half before the first is handed over)
+                    wp_pin(s[3]);
+                    {
+                        const float base = m == -CUDART_INF_F ? 0.f : m;
+                        wp_exps<T>(s[2], s[3], c2, f2_pack(-base, -base), least, sum, w);
+                    }
+                    hand_over(1);
+                    float l0, l1;
+                    f2_unpack(sum, l0, l1);
+                    l += l0 + l1;
+                }
+                wp_wait(b_o + 8 * q, ended++, abortp, a.polls);
+                __syncwarp();
+                tc_fence_after();
+            }
+            i0 += g.n_kt;
+            // ---- the rows go out through the place of Q, whole lines at a time
+            constexpr int CH = DH / 8;  // 16-byte chunks of half a row in fp32, of a row in T
+            auto chunk = [&](int tile, int row, int x) { return reinterpret_cast<uint4 *>(sq + tile * NB * QB) + row * CH + (x ^ (row & (CH - 1))); };
+            auto load_o = [&](int d, uint32_t (&o)[32]) {
+                wp_ld32(t_o + d, o);
+                wp_ld_wait();
+                wp_pin(o);
+            };
+            if (dual) {
+                asm volatile("bar.sync 1, 256;" ::: "memory");  // (both streams' MMAs are complete: Q is no longer read)
+                if (q == 1) {
+                    s_ml[r] = make_float2(m, l);
+#pragma unroll 1
+                    for (int d = 0; d < DH; d += 32) {
+                        uint32_t o[32];
+                        load_o(d, o);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) *chunk(d / (DH / 2), r, d % (DH / 2) / 4 + e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    }
+                }
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            }
+            if (q < nq) {
+                float f0 = 1.f, f1 = 0.f;
+                bool none1 = true;
+                const bool none0 = m == -CUDART_INF_F;  // (no key seen: O may be 0 x whatever)
+                if (dual) {
+                    const float2 other = s_ml[r];
+                    none1 = other.x == -CUDART_INF_F;
+                    const float t = none0 ? other.x : none1 ? m : m > other.x ? m : other.x, base = t == -CUDART_INF_F ? 0.f : t;
+                    f0 = none0 ? 0.f : ex2(m - base);
+                    f1 = none1 ? 0.f : ex2(other.x - base);
+                    l = l * f0 + other.y * f1;
+                    if (m != m || other.x != other.x) f0 = f1 = l = CUDART_NAN_F;
+                    m = t;
+                }
+                const bool none = none0 && none1, direct = g.row < 0;
+                const float inv = direct ? (none ? 0.f : 1.f / l) : 1.f;
+                const int rows = min(per, g.n_tok - row_q * per) * gq;  // of this tile
+                if (!direct && r < rows) a.ml[g.row + row_q * per * gq + r] = make_float2(m, l);
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+                    for (int d = h * (DH / 2); d < (h + 1) * (DH / 2); d += 32) {
+                        uint32_t o[32];
+                        load_o(d, o);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float y[4];
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) y[z] = none0 ? 0.f : __uint_as_float(o[4 * e + z]) * f0;
+                            if (dual && !none1) {
+                                const uint4 x = *chunk(h, r, d % (DH / 2) / 4 + e);
+                                y[0] += __uint_as_float(x.x) * f1; y[1] += __uint_as_float(x.y) * f1; y[2] += __uint_as_float(x.z) * f1; y[3] += __uint_as_float(x.w) * f1;
+                            }
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) o[4 * e + z] = __float_as_uint(y[z] * inv);
+                        }
+                        if (direct) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                *chunk(q, r, d / 8 + e) = make_uint4(pack_pair<T>(__uint_as_float(o[8 * e]), __uint_as_float(o[8 * e + 1])), pack_pair<T>(__uint_as_float(o[8 * e + 2]), __uint_as_float(o[8 * e + 3])),
+                                                                     pack_pair<T>(__uint_as_float(o[8 * e + 4]), __uint_as_float(o[8 * e + 5])), pack_pair<T>(__uint_as_float(o[8 * e + 6]), __uint_as_float(o[8 * e + 7])));
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) *chunk(dual ? h : q, r, d % (DH / 2) / 4 + e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        }
+                    }
+                    if (direct && h == 0) continue;
+                    __syncwarp();
+                    const int lr = lane / CH, lc = lane % CH;
+                    if (!*abortp)
+#pragma unroll 4
+                        for (int x = 0; x < 32; x += 32 / CH) {
+                            const int rr = 32 * (warp & 3) + x + lr, pp = rr * inv_gq >> 16;
+                            if (rr >= rows) continue;
+                            const uint4 y = *chunk(!direct && dual ? h : q, rr, lc);
+                            if (direct) *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + ((size_t)(g.tok0 + row_q * per + pp) * a.p.Hq + g.kvh * gq + rr - pp * gq) * DH + 8 * lc) = y;
+                            else *reinterpret_cast<uint4 *>(a.o + (g.row + row_q * per * gq + rr) * DH + h * (DH / 2) + 4 * lc) = y;
+                        }
+                    __syncwarp();  // (the place is written again)
+                }
+                tc_fence_before();
+            }
+        }
+    }
+    __syncwarp();
+    if (*abortp) {  // a wait ran out: what this CTA has asked for lands within microseconds; do not leave before
+        for (int i = 0; i < 64; ++i) __nanosleep(4000);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tc_dealloc(tmem, 512u);
+    }
+    const bool gave_up = *abortp != 0;
+    if (tid == 0 && (gave_up || s_no_page)) flag(a.status, gave_up ? RIVER_E_TIMEOUT : RIVER_E_BADARG);
+}
+
+// (the head dim of 64 asks for as much as 128 does: no CTA that wants tensor memory shares an SM with one that holds all of it)
+inline size_t prefix_tiles_smem() { return 1024 + 7 * 2 * 128 * 128; }
+
+}  // namespace river

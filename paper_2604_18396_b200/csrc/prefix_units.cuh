@@ -1,0 +1,59 @@
+// The units of prefix_plan.h as kernels find them: from a batch's arrays on the device (internal).
+#pragma once
+#include "prefix_plan.h"
+#include "window_attn_rows.cuh"
+
+namespace river {
+
+struct PfHead {
+    int64_t all, share;  // weight of one KV head's units; of a CTA's part
+};
+struct PfGroup {  // at a group's first sequence
+    int64_t at;  // the weight before it
+    int32_t tok0, keys;
+};
+
+struct PrefixArgs {
+    Paged c;
+    PfPlan p;
+    int layer0, max_q;
+    const int32_t *q_start, *lead, *shared;
+    const void *q;
+    int64_t q_tok, q_head;
+    float scale_log2;
+    void *out;
+    int32_t *status;
+    // scratch
+    PfHead *head;
+    PfGroup *group;   // [n_seqs]
+    int64_t *own_at;  // [n_seqs] the weight before a sequence's units
+    float2 *ml;       // [rows]: maximum (log2), sum
+    float *o;         // [rows][dh]
+    uint32_t polls;   // of a wait, before it gives up
+    int mute;         // self-test: the KV head whose keys nobody asks for, so that waits run out
+};
+
+// positions that a group shares: whole pages that its row of the table can hold
+__device__ __forceinline__ int pf_shared(const Paged &c, int v) { return max(0, min(v, c.max_pages << c.ps_log2)) & ~((1 << c.ps_log2) - 1); }
+__device__ __forceinline__ int pf_len(const Paged &c, int len) { return max(0, min(len, c.max_pages << c.ps_log2)); }
+// whether sequence s goes on with the group of the one before it
+__device__ __forceinline__ bool pf_linked(const PrefixArgs &a, int s) { return s > 0 && a.lead[s] != s && a.lead[s] == a.lead[s - 1] && a.shared[s] == a.shared[s - 1]; }
+// whether what the batch's arrays say of sequence s is as it should be
+__device__ __forceinline__ bool pf_sound(const PrefixArgs &a, int s) {
+    const int x = a.q_start[s], y = a.q_start[s + 1], len = a.c.lens[s], sh = a.shared[s];
+    return x >= 0 && y >= x && y <= a.p.n_tokens && y - x <= a.max_q && len >= 0 && len <= (a.c.max_pages << a.c.ps_log2) && sh == pf_shared(a.c, sh) && len - (y - x) >= sh &&
+           (a.lead[s] == s || pf_linked(a, s));
+}
+// entries of a KV head: groups, each where its last sequence stands, then sequences
+__device__ __forceinline__ int pf_entries(const PrefixArgs &a) { return a.c.n_seqs * (a.p.groups + a.p.own); }
+__device__ __forceinline__ PfEntry pf_entry(const PrefixArgs &a, int i, int span) {
+    const int S = a.c.n_seqs;
+    const bool group = a.p.groups && i < S;
+    const int s = a.p.groups && !group ? i - S : i, l = group ? a.lead[s] : s, shared = a.p.groups ? pf_shared(a.c, a.shared[s]) : 0;
+    if (group && (shared == 0 || l < 0 || l > s || (s + 1 < S && pf_linked(a, s + 1)))) return PfEntry{};
+    const int t0 = a.q_start[l], t1 = a.q_start[s + 1];
+    if (t0 < 0 || t1 <= t0 || t1 > a.p.n_tokens) return PfEntry{};
+    return group ? pf_group_entry(t0, t1 - t0, l, shared, span) : pf_own_entry(t0, t1 - t0, s, shared, pf_len(a.c, a.c.lens[s]), span);
+}
+
+}  // namespace river
