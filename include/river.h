@@ -438,7 +438,7 @@ int river_prefix_groups(const river_paged *c, const int32_t *q_start, int least,
  * n + i and sees the positions j <= p;  out = softmax(softmax_scale q K^T) V over those, zero where there are none.  The sequences lead[s], .. of a
  * group follow one another, and positions j < shared[s] are read once for all of them, from the row of lead[s] in the table; the others from the
  * sequence's own row.  Every query of a group stands behind its shared positions.
- *   q, q_start, max_q, softmax_scale, out   as river_window_attention has them;  Hq / Hkv at most 128;  n_tokens * Hq at most 2^30
+ *   q, q_start, max_q, softmax_scale, out   as river_window_attention has them;  Hq / Hkv at most 128;  n_tokens * Hq at most 2^30;  n_seqs <= 8192
  *   lead      [dev] int32 [n_seqs]: the group's first sequence (s itself where s is that, or by itself)
  *   shared    [dev] int32 [n_seqs]: a multiple of page_size, the same for a group's sequences, at most lens[s] - n; 0: none
  *   max_own   about the most positions behind the shared ones that a sequence has, new ones included, by which the way of computing is chosen
@@ -446,8 +446,8 @@ int river_prefix_groups(const river_paged *c, const int32_t *q_start, int least,
  *   workspace [dev] river_prefix_attention_bytes(n_seqs, n_tokens, Hq, Hkv, dh) bytes, 128-byte aligned; what it holds before does not matter, and calls
  *             that may run at the same time have one each
  *   status    [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as not visible);
- *             lead or shared is not as described (rows of sequences that it concerns may hold anything); q_start descends, a length is negative (it
- *             counts as 0), less than the sequence's queries or more than a row of the table holds (it counts as that), or a sequence has more than max_q
+ *             lead or shared is not as described, where the way of computing reads them (rows of sequences that it concerns may hold anything); q_start
+ *             descends, a length is negative (it counts as 0) or more than a row of the table holds (it counts as that), or a sequence has more than max_q
  *             queries (the rows behind the max_q-th may stay as they are); RIVER_E_TIMEOUT when a wait ran out (any row may then hold anything).
  * Positions that a query does not see have no influence on its result, whatever the pool holds there.  Every result follows in a fixed order of
  * sums: the same inputs give the same bits. */

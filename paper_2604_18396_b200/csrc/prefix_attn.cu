@@ -2,21 +2,36 @@
 #include <algorithm>
 #include <cmath>
 
-#include "prefix_attn_step.cuh"
+#include "prefix_attn_own.cuh"
 #include "prefix_attn_tiles.cuh"
 #include "tensor_maps.h"
 
 namespace river {
 namespace {
 
-constexpr int kPfCtas = 148;  // one per SM
-
 enum PrefixMode {
     kPfStep,    // single tokens by themselves: what is shared is read once per sequence
-    kPfGroups,  // the groups' keys in query tiles, then single tokens with their own keys
+    kPfGroups,  // the groups' keys in query tiles, beside them single tokens with their own keys
     kPfBoth,    // the groups' and the sequences' keys in query tiles, joined row by row
     kPfWhole    // the sequences' rows in query tiles over all of their keys
 };
+// CTAs of a cluster of single tokens, by an estimate of the time in us: a round of CTAs takes what memory needs for its blocks at `rate` bytes per us, or 0.5
+// for each block that a warp has one after the other, and 4 + s / 4 for its start and the joining.  Clusters of more than four leave places free: a GPC,
+// of about 16 SMs, takes whole ones.
+int own_splits(const PrefixArgs &a, int64_t positions, double rate, double &best_t) {
+    const int per_sm = a.c.dh == 128 ? kPfOwnCtas<128> : kPfOwnCtas<64>;
+    const double units = (double)a.p.n_tokens * a.c.Hkv * ((a.p.gq + 7) / 8), blocks = positions / 16 + 1.0, block_us = 64.0 * a.c.dh / rate;
+    int best = 1;
+    best_t = 1e300;
+    for (int s = 1; s <= kStepMaxSplits; ++s) {
+        const double places = s <= 4 ? kPfCtas * per_sm : kPfCtas / 18 * (16 * per_sm / s) * s;
+        const double turns = 0.5 * std::ceil(blocks / (s * kStepWarps)), stream = places * blocks / s * block_us, fixed = 4.0 + 0.25 * s;
+        const double rounds = units * s / places, full = std::floor(rounds), rest = rounds - full;
+        const double t = full * (std::max(stream, turns) + fixed) + (rest > 0 ? std::max(stream * rest, turns) + fixed : 0.0);
+        if (t < 0.99 * best_t) { best_t = t; best = s; }
+    }
+    return best;
+}
 struct PrefixShape {
     PrefixMode mode;
     int splits;  // of single tokens
@@ -26,63 +41,66 @@ struct PrefixShape {
 bool prefix_both(int n_seqs, int n_tokens, int gq) { return n_tokens < (int64_t)n_seqs * 2 * pf_per(gq); }
 
 // What a call costs in us by each way, and the one that costs least.  `cap`: positions that a row of the table holds, `own`: the most that are a
-// sequence's own, as the caller says; how many groups there are the host does not know: one is assumed.
+// sequence's own, as the caller says; how many groups there are the host does not know: one is assumed, and that it has the rest of the row.
+//   single tokens     what is shared comes out of L2, at 13 TB/s, but once
+//   query tiles       a CTA takes 0.9 us for each of its tiles of up to 128 rows, 1.8 for two of them, and 4 to 8 for a unit's start and end
+//   beside them       SMs' shares of HBM (pf_split); 30 us until everything is under way and joined
+// (us, single tokens / groups / both / whole; 8B-class heads: 64 rows behind 8200 positions, 20 to 600 of their own 200 / 51 / 77 / 370; 200 rows in groups of
+// five, 24 query heads, 100 to 2100 shared, f16 97 / 111 / 173 / 260; four beams behind 1500 of the 1B class 16 / 27 / 30 / 30; questions of 17 to 333
+// tokens in groups of four behind 700 to 2300 1120 / - / - / 90.)
 PrefixShape prefix_shape(const PrefixArgs &a, int own) {
     const int gq = a.p.gq, span = 2 * pf_per(gq);
     const int64_t cap = (int64_t)a.c.max_pages << a.c.ps_log2;
-    WindowArgs w = {};
-    w.c = a.c;
-    w.n_tokens = a.p.n_tokens;
-    w.max_q = a.max_q;
-    w.Hq = a.p.Hq;
-    w.window = (int)cap;
+    own = (int)std::min<int64_t>(std::max(1, own), cap);
+    const double heads = a.c.Hkv, rt = (gq + 7) / 8, tokens = a.p.n_tokens, position = 4.0 * a.c.dh * heads;  // (bytes)
     double step_us, own_us;
-    const int step = step_splits(w, kPfCtas, step_us);
-    w.window = own;
-    const int own_step = step_splits(w, kPfCtas, own_us);
-    // query tiles: a CTA takes 0.9 us for each of its tiles of up to 128 rows, 1.7 for two of them, and some 3 for a unit's start and end
-    const double rows = (double)a.p.n_tokens * gq, pairs = std::ceil(rows / 256.0), tile_us = rows <= 128 ? 0.9 : 1.7;
-    const double shared_us = 8.0 + a.c.Hkv * pairs * ((cap - std::min<int64_t>(own, cap)) / 128.0 * tile_us + 3.0) / kPfCtas;
-    const double per_seq = std::max(1.0, (double)a.p.n_tokens / a.c.n_seqs), units = a.c.n_seqs * std::ceil(per_seq / span);
-    const double unit_us = per_seq * gq <= 128 ? 0.9 : 1.7;
-    const double own_tiles_us = a.c.Hkv * units * (own / 128.0 * unit_us + 3.0) / kPfCtas;
-    const double whole_us = 8.0 + a.c.Hkv * units * (cap / 128.0 * unit_us + 3.0) / kPfCtas;
+    const int step = own_splits(a, cap, 13e6, step_us), own_step = own_splits(a, own, 6e6, own_us);
+    step_us = std::max(step_us, 6.0 + ((double)(cap - own) + (double)a.c.n_seqs * own) * position / 6e6);
+    const double rows = tokens * gq, shared_us = heads * std::ceil(rows / 256.0) * ((cap - own) / 128.0 * (rows <= 128 ? 0.9 : 1.8) + 4.0) / kPfCtas;
+    own_us = tokens * heads * rt * (own / 16.0 + 6.0) * a.c.dh * 1.2e-3 / kPfCtas;
+    const double per_seq = std::max(1.0, tokens / a.c.n_seqs), units = heads * a.c.n_seqs * std::ceil(per_seq / span), tile_us = per_seq * gq <= 128 ? 0.9 : 1.8;
+    const double own_tiles_us = units * (own / 128.0 * tile_us + 8.0) / kPfCtas, whole_us = units * (cap / 128.0 * tile_us + 5.0) / kPfCtas;
     PrefixShape s = {kPfStep, step};
     double best = step_us;
     if (prefix_both(a.c.n_seqs, a.p.n_tokens, gq)) {
-        if (shared_us + own_us < best) best = shared_us + own_us, s = {kPfGroups, own_step};
-        if (shared_us + own_tiles_us + 4.0 < best) s = {kPfBoth, 1};
-    } else if (whole_us + 3.0 < best) {
+        if (30.0 + shared_us + own_us < best) best = 30.0 + shared_us + own_us, s = {kPfGroups, own_step};
+        if (25.0 + shared_us + own_tiles_us < best) s = {kPfBoth, 1};
+    } else if (20.0 + whole_us < best) {
         s = {kPfWhole, 1};
     }
     return s;
 }
 
-// The scratch: head, groups, weights before the sequences, then maxima and sums, and O, of `rows` rows.
+// The scratch: head, groups, weights before the sequences, then maxima and sums, and O, of the parts of units, and of single tokens' own keys.
 struct PrefixScratch {
-    int64_t rows;
-    size_t group, own_at, ml, o, bytes;
+    size_t group, own_at, ml, own_ml, o, own_o, bytes;
 };
 PrefixScratch prefix_scratch(int n_seqs, int n_tokens, int Hq, int gq, int dh) {
+    const bool both = prefix_both(n_seqs, n_tokens, gq);
+    const int64_t whole = (int64_t)n_tokens * Hq, rows = pf_cut_rows(PfPlan{n_tokens, Hq, gq, 0, 0, pf_slot_rows(n_tokens, gq)}) + (both ? 2 * whole : 0),
+                  own_rows = both ? whole : 0;
+    auto behind = [](size_t at, size_t bytes) { return (at + bytes + 127) & ~(size_t)127; };
     PrefixScratch s;
-    s.rows = pf_cut_rows(PfPlan{kPfCtas, n_tokens, Hq, gq, 0, 0, pf_slot_rows(n_tokens, gq)}) + (prefix_both(n_seqs, n_tokens, gq) ? 2 : 0) * (int64_t)n_tokens * Hq;
-    s.group = 128;
-    s.own_at = s.group + (size_t)n_seqs * sizeof(PfGroup);
-    s.ml = (s.own_at + (size_t)n_seqs * sizeof(int64_t) + 127) & ~(size_t)127;
-    s.o = (s.ml + (size_t)s.rows * sizeof(float2) + 127) & ~(size_t)127;
-    s.bytes = s.o + (size_t)s.rows * dh * sizeof(float);
+    s.group = behind(0, sizeof(PfHead));
+    s.own_at = behind(s.group, (size_t)n_seqs * sizeof(PfGroup));
+    s.ml = behind(s.own_at, (size_t)n_seqs * sizeof(int64_t));
+    s.own_ml = behind(s.ml, (size_t)rows * sizeof(float2));
+    s.o = behind(s.own_ml, (size_t)own_rows * sizeof(float2));
+    s.own_o = behind(s.o, (size_t)rows * dh * sizeof(float));
+    s.bytes = s.own_o + (size_t)own_rows * dh * sizeof(float);
     return s;
 }
 
-
 // a kernel that may start beside the one before it
 template <class... P, class... A>
-int launch_beside(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st, int cluster, bool beside, A... args) {
+int launch_beside(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, bool beside, A... args) {
+    if (smem && cuda_rc(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem))) return RIVER_E_DEVICE;
     if (cluster > 8 && cuda_rc(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1))) return RIVER_E_DEVICE;
     cudaLaunchAttribute at[2];
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = at;
     if (cluster > 1) {
@@ -96,16 +114,11 @@ int launch_beside(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st,
     return cuda_rc(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 template <class T, int DH>
-int launch_tiles(const PrefixArgs &a, cudaStream_t st) {
-    // the pages of this block, as rows of a head's dims
-    CUtensorMap map;
-    const size_t rows = (size_t)a.c.n_pages * 2 * a.c.Hkv << a.c.ps_log2;
-    if (rows >= (1ull << 31)) return RIVER_E_SHAPE;
-    if (!make_map_bf16(&map, a.c.pool + rows * DH * 2 * a.layer0, DH, rows, 16)) return RIVER_E_DEVICE;
+int launch_tiles(const PrefixArgs &a, const CUtensorMap &map, cudaStream_t st) {
     const size_t smem = prefix_tiles_smem();
     if (cuda_rc(cudaFuncSetAttribute(prefix_tiles_kernel<T, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem))) return RIVER_E_DEVICE;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.p.ctas);
+    cfg.gridDim = dim3((unsigned)kPfCtas);
     cfg.blockDim = dim3(kWpThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -115,16 +128,22 @@ template <class T, int DH>
 int launch(PrefixArgs a, PrefixShape s, cudaStream_t st) {
     a.p.groups = s.mode == kPfGroups || s.mode == kPfBoth;
     a.p.own = s.mode == kPfBoth || s.mode == kPfWhole;
+    // the pages of this block, as rows of a head's dims
+    CUtensorMap map;
+    const size_t rows = (size_t)a.c.n_pages * 2 * a.c.Hkv << a.c.ps_log2;
+    if (rows >= (1ull << 31)) return RIVER_E_SHAPE;
+    if (!make_map_bf16(&map, a.c.pool + rows * DH * 2 * a.layer0, DH, rows, 16)) return RIVER_E_DEVICE;
     if (s.mode != kPfStep)
-        if (const int rc = launch_tiles<T, DH>(a, st)) return rc;
+        if (const int rc = launch_tiles<T, DH>(a, map, st)) return rc;
+    const int64_t tiles = (int64_t)a.c.Hkv * ((a.p.gq + 7) / 8);
     if (s.mode == kPfStep || s.mode == kPfGroups) {
-        const int64_t ctas = (int64_t)s.splits * a.c.Hkv * ((a.p.gq + 7) / 8) * a.max_q * a.c.n_seqs;
+        const int64_t ctas = s.splits * tiles * a.max_q * a.c.n_seqs;
         if (ctas > INT32_MAX) return RIVER_E_SHAPE;
-        return launch_beside(prefix_step_kernel<T, DH>, dim3((unsigned)ctas), 32 * kStepWarps, st, s.splits, s.mode == kPfGroups, a, s.splits);
+        const int rc = launch_beside(prefix_own_kernel<T, DH>, dim3((unsigned)ctas), 32 * kStepWarps, kPfOwnSmem<DH>, st, s.splits, s.mode == kPfGroups, map, a, s.splits);
+        if (rc || s.mode == kPfStep) return rc;
     }
-    if (s.mode == kPfBoth)
-        return launch_beside(prefix_join_kernel<T, DH>, dim3((unsigned)std::min<int64_t>(kPfCtas * 8, ((int64_t)a.p.n_tokens * a.p.Hq + 7) / 8)), 256, st, 1, true, a);
-    return launch_beside(prefix_join_cut_kernel<T, DH>, dim3(kPfCtas - 1, kJoinBlocks), 256, st, 1, true, a);
+    if (s.mode == kPfWhole) return launch_beside(prefix_join_cut_kernel<T, DH>, dim3(kPfCtas - 1, kJoinBlocks), 256, 0, st, 1, true, a);
+    return launch_beside(prefix_join_kernel<T, DH>, dim3((unsigned)((a.p.n_tokens * tiles * (DH / 32) + 7) / 8)), 256, 0, st, 1, true, a);
 }
 
 // The arguments of a call, checked.  RIVER_OK with a->n_tokens or a->max_q 0: nothing is to be done.
@@ -135,7 +154,7 @@ int prefix_args(const river_paged *c, int layer, int n_tokens, int max_q, int ma
     if (layer < 1 || layer > c->n_layers || n_tokens < 0 || max_q < 0 || max_own < 0 || !q_start || !lead || !shared) return RIVER_E_BADARG;
     if (!words(q_start, lead, shared, status) || Hq < 1 || Hq % c->Hkv || !std::isfinite(softmax_scale)) return RIVER_E_BADARG;
     const int gq = Hq / c->Hkv;
-    if (c->n_seqs > 65535 || Hq > 8192 || gq > kWpRows || (int64_t)c->n_seqs * Hq > (1 << 26) || (int64_t)n_tokens * Hq > (1 << 30)) return RIVER_E_SHAPE;
+    if (c->n_seqs > 8192 || Hq > 8192 || gq > kWpRows || (int64_t)c->n_seqs * Hq > (1 << 26) || (int64_t)n_tokens * Hq > (1 << 30)) return RIVER_E_SHAPE;
     a->layer0 = layer - 1;
     a->max_q = std::min(max_q, n_tokens);
     a->q_start = q_start;
@@ -144,7 +163,7 @@ int prefix_args(const river_paged *c, int layer, int n_tokens, int max_q, int ma
     a->scale_log2 = softmax_scale * 1.4426950408889634f;
     a->out = out;
     a->status = status;
-    a->p = PfPlan{kPfCtas, n_tokens, Hq, gq, 0, 0, pf_slot_rows(n_tokens, gq)};
+    a->p = PfPlan{n_tokens, Hq, gq, 0, 0, pf_slot_rows(n_tokens, gq)};
     a->polls = kWaitLimit;
     a->mute = -1;
     if (n_tokens == 0) return RIVER_OK;  // (rows that are none may have no address)
@@ -163,6 +182,8 @@ int prefix_args(const river_paged *c, int layer, int n_tokens, int max_q, int ma
     a->own_at = reinterpret_cast<int64_t *>(w + s.own_at);
     a->ml = reinterpret_cast<float2 *>(w + s.ml);
     a->o = reinterpret_cast<float *>(w + s.o);
+    a->own_ml = reinterpret_cast<float2 *>(w + s.own_ml);
+    a->own_o = reinterpret_cast<float *>(w + s.own_o);
     return RIVER_OK;
 }
 int launch(const PrefixArgs &a, int dtype, PrefixShape s, cudaStream_t st) {
@@ -176,7 +197,7 @@ int launch(const PrefixArgs &a, int dtype, PrefixShape s, cudaStream_t st) {
 using namespace river;
 
 extern "C" size_t river_prefix_attention_bytes(int n_seqs, int n_tokens, int Hq, int Hkv, int dh) {
-    if (n_seqs < 1 || n_seqs > 65535 || n_tokens < 0 || Hkv < 1 || Hq < 1 || Hq > 8192 || Hq % Hkv || Hq / Hkv > kWpRows || (dh != 64 && dh != 128)) return 0;
+    if (n_seqs < 1 || n_seqs > 8192 || n_tokens < 0 || Hkv < 1 || Hq < 1 || Hq > 8192 || Hq % Hkv || Hq / Hkv > kWpRows || (dh != 64 && dh != 128)) return 0;
     if ((int64_t)n_tokens * Hq > (1 << 30)) return 0;
     return prefix_scratch(n_seqs, n_tokens, Hq, Hq / Hkv, dh).bytes;
 }

@@ -35,29 +35,12 @@ struct PfSeg {
     int64_t row;           // first row in the scratch; -1: the result's
 };
 
-// Exclusive prefix sum over the CTA's threads (`part`: one per warp); `total` gets the sum.  Ends with a barrier behind every read.
-__device__ __forceinline__ int64_t pf_scan(int64_t x, int64_t *part, int64_t &total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t inc = x;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-    }
-    if (lane == 31) part[warp] = inc;
-    __syncthreads();
-    int64_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kWpThreads / 32; ++w) {
-        const int64_t y = part[w];
-        if (w < warp) before += y;
-        total += y;
-    }
-    __syncthreads();
-    return before + inc - x;
+// x, of which the compiler knows nothing: a loop is not written twice for what does not change in it (the kernel's code would be three times as long, and
+// fetching it behind cold caches is a third of a small call).
+__device__ __forceinline__ int opaque(int x) {
+    asm volatile("" : "+r"(x));
+    return x;
 }
-
 // One row over the positions [lo, hi) of a row of the table, by one warp in their order: O (not divided), maximum and sum.
 template <class T, int DH>
 __device__ void pf_row(const PrefixArgs &a, int token, int head, int seq, int lo, int hi, float (&o)[DH / 32], float &m, float &l) {
@@ -69,6 +52,7 @@ __device__ void pf_row(const PrefixArgs &a, int token, int head, int seq, int lo
     l = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) { x[e] = to_f(q[e]) * a.scale_log2; o[e] = 0.f; }
+#pragma unroll 1
     for (int j = lo; j < hi; ++j) {
         const int col = j >> a.c.ps_log2, page = col < a.c.max_pages ? a.c.table[(size_t)seq * a.c.max_pages + col] : -1;
         if (page < 0 || page >= a.c.n_pages) continue;
@@ -85,8 +69,28 @@ __device__ void pf_row(const PrefixArgs &a, int token, int head, int seq, int lo
     }
 }
 
+// The rows of a part, one by one (warps 4 .. 11)
 template <class T, int DH>
-__global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __grid_constant__ CUtensorMap tmap, const PrefixArgs a) {
+__device__ __noinline__ void pf_rows_again(const PrefixArgs &a, const PfSeg &g) {
+    const int gq = a.p.gq, lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int x = (threadIdx.x >> 5) - 4; x < g.n_tok * gq; x += 8) {
+        const int token = g.tok0 + x / gq, head = g.kvh * gq + x % gq, lo = g.base + kPfKeys * g.t0;
+        const int hi = g.base + min(min(g.keys, kPfKeys * (g.t0 + g.n_kt)), g.causal ? g.pos0 + x / gq + 1 - g.base : g.keys);
+        float o[DH / 32], m, l;
+        pf_row<T, DH>(a, token, head, g.seq, lo, hi, o, m, l);
+        if (g.row >= 0 && lane == 0) a.ml[g.row + x] = make_float2(m, l);
+#pragma unroll
+        for (int e = 0; e < DH / 32; ++e) {
+            const int d = DH / 32 * lane + e;
+            if (g.row < 0) static_cast<T *>(a.out)[((size_t)token * a.p.Hq + head) * DH + d] = from_f<T>(l == 0.f ? 0.f : o[e] / l);
+            else a.o[g.row * DH + ((int64_t)(d >> 2) * (g.n_tok * gq) + x) * 4 + (d & 3)] = o[e];
+        }
+    }
+}
+
+template <class T, int DH>
+__global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ PrefixArgs a) {
     constexpr int NB = DH / 64;                                          // blocks of 64 dims
     constexpr bool kHalf = std::is_same<T, __half>::value;
     constexpr uint32_t QB = kWpRows * 128, KB = kWpKeys * 128;           // bytes of one block of Q / of K or V
@@ -99,65 +103,76 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
     // K of the first tile there; V of tile i and K of tile i + 1 there (4, in turn; tiles are counted over all units); V and K of tile i before
     // free (2); per stream: S done (2), P written (2 x 2), O done (2); Q there; a part there (2), no longer needed (2)
     __shared__ uint64_t bars[20];
-    __shared__ int64_t s_part[kWpThreads / 32], s_at;
+    __shared__ longlong2 s_part[kWpThreads / 32];
+    __shared__ int64_t s_at;
+    __shared__ PfEntry s_entry;  // the first one that this CTA has units of
     __shared__ PfSeg s_seg[2];
     __shared__ float2 s_ml[kWpRows];  // dual: the second stream's maxima and sums
     __shared__ uint32_t s_tmem;
-    __shared__ int s_first, s_abort, s_no_page, s_poison[2], s_missing[2];
+    __shared__ int s_first, s_kvh, s_abort, s_no_page, s_poison[2], s_missing[2];
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int gq = a.p.gq, per = pf_per(gq), span = 2 * per, S = a.c.n_seqs, D = pf_entries(a);
     const uint32_t b_first = smem_u32(&bars[0]), b_full = b_first + 8, b_free = b_full + 32, b_s = b_free + 16, b_p = b_s + 16, b_o = b_p + 32, b_q = b_o + 16,
                    b_seg = b_q + 8, b_used = b_seg + 16;
     volatile int *abortp = &s_abort;
+    pdl_launch();  // (whatever starts beside this kernel takes no tensor memory)
     if (tid == 0) {
         s_abort = s_no_page = s_poison[0] = s_poison[1] = s_missing[0] = s_missing[1] = 0;
         s_first = -1;
+#pragma unroll 1
         for (int i = 0; i < 20; ++i) mbar_init(smem_u32(&bars[i]), i >= 9 && i < 13 ? 4 : i == 15 ? 8 : i >= 18 ? 10 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
 
-    // ---- this CTA's part of the row of units
-    int64_t all = 0, at = 0, mine = 0, total;
-    for (int i0 = 0; i0 < D; i0 += kWpThreads) {
-        const int64_t w = i0 + tid < D ? pf_entry(a, i0 + tid, span).w : 0, before = pf_scan(w, s_part, total);
-        if (i0 == 0) at = before, mine = w;
-        all += total;
+    // the queries, on their way to L2 while the parts are found (as far as one line per thread reaches)
+    {
+        const int64_t x = (int64_t)blockIdx.x * kWpThreads + tid, lines = (int64_t)a.p.Hq * (DH / 64);
+        if (x < a.p.n_tokens * lines) {
+            const int token = (int)pf_div(x, lines), y = (int)(x - token * lines);
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const T *>(a.q) + token * a.q_tok + y / (DH / 64) * a.q_head + y % (DH / 64) * 64));
+        }
     }
-    const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.p.ctas);
+    // ---- this CTA's part of the row of units
+    const bool beside = a.p.groups && !a.p.own;  // single tokens run on the other SMs
+    PfEntry mine = {};
+    int64_t all = 0, blocks = 0, at = 0, none = 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < D; i0 += kWpThreads) {
+        const int i = i0 + tid;
+        mine = i < D ? pf_entry(a, i, span) : PfEntry{};
+        at = all + pf_scan<kWpThreads / 32>(mine.w, beside && i < D ? pf_blocks(a, i) : 0, s_part, all, blocks);
+    }
+    const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.c.Hkv, beside ? pf_split(everything, blocks * a.c.Hkv * ((gq + 7) / 8), a.c.dh) : kPfCtas);
     const int64_t x0 = blockIdx.x * share, x1 = min(x0 + share, everything);
     if (x0 < everything || blockIdx.x == 0) {
-        const int64_t xl = all ? x0 % all : 0;
+        const int kvh0 = all ? (int)pf_div(x0, all) : 0;
+        const int64_t xl = x0 - kvh0 * all;
         int64_t base = 0;
+#pragma unroll 1
         for (int i0 = 0; i0 < D; i0 += kWpThreads) {
             const int i = i0 + tid;
             if (D > kWpThreads) {  // (else they are known)
-                mine = i < D ? pf_entry(a, i, span).w : 0;
-                at = base + pf_scan(mine, s_part, total);
-                base += total;
+                mine = i < D ? pf_entry(a, i, span) : PfEntry{};
+                at = base;
+                at += pf_scan<kWpThreads / 32>(mine.w, 0, s_part, base, none);
             }
-            if (mine && at <= xl && xl < at + mine) s_first = i, s_at = at;
+            if (mine.w && at <= xl && xl < at + mine.w) s_first = i, s_kvh = kvh0, s_at = at, s_entry = mine;
             if (blockIdx.x == 0 && i < D) {  // for who joins the parts
                 if (!a.p.groups || i >= S) a.own_at[a.p.groups ? i - S : i] = at;
-                else if (mine) {
-                    const PfEntry e = pf_entry(a, i, span);
-                    a.group[e.seq] = PfGroup{at, e.tok0, e.keys};
-                }
+                else if (mine.w) a.group[mine.seq] = PfGroup{at, mine.tok0, mine.n, mine.keys};
             }
         }
         if (blockIdx.x == 0) {
-            if (tid == 0) *a.head = PfHead{all, share};
+            if (tid == 0) a.head->all = all, a.head->share = share;
+#pragma unroll 1
             for (int s = tid; s < S; s += kWpThreads)
                 if (!pf_sound(a, s)) flag(a.status, RIVER_E_BADARG);
         }
     }
-    if (x0 >= everything) {
-        pdl_launch();
-        return;
-    }
+    if (x0 >= everything) return;
     if (warp == 1) {
         tc_alloc(smem_u32(&s_tmem), 512u);
-        pdl_launch();
         tc_fence_before();
     }
     __syncthreads();
@@ -178,10 +193,12 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 2) {  // ---- the parts
             int64_t x = x0, ent = s_at;  // (ent: the weight before the entry, of this KV head)
-            int i = s_first, kvh = (int)(x0 / all), n = 0;
+            int i = s_first, kvh = s_kvh, n = 0;
+            PfEntry e = s_entry;
+#pragma unroll 1
             while (true) {
-                const PfEntry e = pf_entry(a, i, span);
                 int64_t y = x - kvh * all - ent;  // within the entry
+#pragma unroll 1
                 for (int t = pf_unit_at(e, y, span); x < x1 && y < e.w; ++t) {
                     const PfUnit u = pf_unit(e, t, span);
                     const PfPart p = pf_part(a.p, share, x - y + u.at, u, blockIdx.x, kvh, e.group);
@@ -200,6 +217,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                 // the next entry that has units: from behind this one, or the next KV head's first
                 ent += e.w;
                 int i0 = i + 1;
+#pragma unroll 1
                 while (true) {
                     if (i0 >= D) i0 = 0, ++kvh, ent = 0;
                     const unsigned there = __ballot_sync(0xffffffffu, i0 + lane < D && pf_entry(a, i0 + lane, span).w > 0);
@@ -209,6 +227,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                     }
                     i0 += 32;
                 }
+                e = pf_entry(a, i, span);
             }
             if (n >= 2) wp_wait(b_used + 8 * (n & 1), (n >> 1) - 1, abortp, a.polls);
             if (lane == 0) {
@@ -233,6 +252,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
             if (more && f.kvh == a.mute) more = false;
             int jf = 0, page = -1, ahead = more ? page_of(f, 0) : -1;
             uint32_t bytes = 0;
+#pragma unroll 1
             for (int i = -1; more || i >= 0; ++i) {
                 // V of tile i (g, j), K of tile i + 1 (f, jf)
                 const int next = more ? ahead : -1;
@@ -342,26 +362,11 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
         const int bpp = a.c.ps_log2 - 4;
         PfSeg g;
         int i0 = 0, count = 0, ended = 0;  // tiles of the parts before; tiles, and parts, of this stream
+#pragma unroll 1
         for (int n = 0;; ++n) {
             // the part before: where something in it was no number, its rows again
             asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (n > 0 && s_poison[(n - 1) & 1] && !*abortp)
-#pragma unroll 1
-                for (int x = warp - 4; x < g.n_tok * gq; x += 8) {
-                    const int token = g.tok0 + x / gq, lo = g.base + kPfKeys * g.t0;
-                    const int hi = g.base + min(min(g.keys, kPfKeys * (g.t0 + g.n_kt)), g.causal ? g.pos0 + x / gq + 1 - g.base : g.keys);
-                    float o[DH / 32], m, l;
-                    pf_row<T, DH>(a, token, g.kvh * gq + x % gq, g.seq, lo, hi, o, m, l);
-                    if (g.row < 0) {
-                        T *out = static_cast<T *>(a.out) + ((size_t)token * a.p.Hq + g.kvh * gq + x % gq) * DH + DH / 32 * lane;
-#pragma unroll
-                        for (int e = 0; e < DH / 32; ++e) out[e] = from_f<T>(l == 0.f ? 0.f : o[e] / l);
-                    } else {
-                        if (lane == 0) a.ml[g.row + x] = make_float2(m, l);
-#pragma unroll
-                        for (int e = 0; e < DH / 32; ++e) a.o[(g.row + x) * DH + DH / 32 * lane + e] = o[e];
-                    }
-                }
+            if (n > 0 && s_poison[(n - 1) & 1] && !*abortp) pf_rows_again<T, DH>(a, g);
             if (n > 0) used(n - 1);
             {  // one answer for all eight warps: nobody leaves while others wait at a barrier
                 const bool more = take(n, g);
@@ -372,28 +377,30 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
             const int nq = g.n_tok > per ? 2 : 1;
             const bool dual = nq == 1 && g.n_kt > 1;
             {  // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
-                constexpr int C8 = DH / 8, U = C8;  // 16-byte chunks of a row; all of a thread's are under way together
+                constexpr int C8 = DH / 8;  // 16-byte chunks of a row; all of a thread's are under way together
                 const int c8 = u0 % C8;
                 const T *src = static_cast<const T *>(a.q) + g.tok0 * a.q_tok + g.kvh * gq * a.q_head + 8 * c8;
-                uint4 x[U];
-#pragma unroll
-                for (int i = 0; i < U; ++i) {
+                auto place = [&](int rr) { const int rx = rr % kWpRows; return sq + rr / kWpRows * NB * QB + (c8 >> 3) * QB + rx * 128 + (((c8 & 7) ^ (rx & 7)) * 16); };
+#pragma unroll 4
+                for (int i = 0; i < C8; ++i) {
                     const int rr = u0 / C8 + i * (256 / C8), rx = rr % kWpRows, pp = rx * inv_gq >> 16, p = rr / kWpRows * per + pp, h = rx - pp * gq;
-                    x[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (pp < per && p < g.n_tok) x[i] = *reinterpret_cast<const uint4 *>(src + p * a.q_tok + h * a.q_head);
+                    const bool on = pp < per && p < g.n_tok;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(place(rr))), "l"(on ? src + p * a.q_tok + h * a.q_head : src), "r"(on ? 16 : 0) : "memory");
                 }
                 bool missing = false;
+#pragma unroll 1
                 for (int u = 8 * g.t0 + u0; u < 8 * (g.t0 + g.n_kt) && 16 * u < g.keys; u += 256) {
                     const int col = ((g.base >> 4) + u) >> bpp, page = col < a.c.max_pages ? a.c.table[(size_t)g.seq * a.c.max_pages + col] : -1;
                     missing = missing || page < 0 || page >= a.c.n_pages;
                 }
                 if (missing) s_missing[n & 1] = 1;
-#pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const int rr = u0 / C8 + i * (256 / C8), rx = rr % kWpRows;
-                    x[i].x ^= turn; x[i].y ^= turn; x[i].z ^= turn; x[i].w ^= turn;
-                    *reinterpret_cast<uint4 *>(sq + rr / kWpRows * NB * QB + (c8 >> 3) * QB + rx * 128 + (((c8 & 7) ^ (rx & 7)) * 16)) = x[i];
-                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                if (turn)
+#pragma unroll 1
+                    for (int i = 0; i < C8; ++i) {
+                        uint4 *x = reinterpret_cast<uint4 *>(place(u0 / C8 + i * (256 / C8)));
+                        *x = make_uint4(x->x ^ turn, x->y ^ turn, x->z ^ turn, x->w ^ turn);
+                    }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_q);
@@ -408,12 +415,13 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                 const int hi = g.causal ? pos + 1 - g.base : g.keys, all_hi = g.causal ? g.pos0 + 1 - g.base : g.keys;
                 const bool missing = s_missing[n & 1] != 0;
                 auto huge = [&] { if (fabsf(m) > kWpHuge<T> && m != -CUDART_INF_F) s_poison[n & 1] = 1; };
+#pragma unroll 1
                 for (int j = dual ? q : 0; j < g.n_kt; j += dual ? 2 : 1) {
                     const int i = i0 + j, c0 = kPfKeys * (g.t0 + j);
-                    const bool fresh = j == (dual ? q : 0);
+                    const bool fresh = opaque(j < (dual ? 2 : 1));
                     uint32_t valid = 0xffu;  // blocks that are there
                     bool part = c0 + kPfKeys > all_hi;
-                    if (missing) {
+                    if (opaque(missing)) {
 #pragma unroll 1
                         for (int b = 0; b < 8; ++b) {
                             const int u = 8 * (g.t0 + j) + b, col = ((g.base >> 4) + u) >> bpp;
@@ -422,7 +430,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                         }
                         part = part || valid != 0xffu;
                     }
-                    if (part && (dual || q == 0)) {  // thread = V row: those that nobody sees become zero, the others are looked through
+                    if (part && opaque(dual || q == 0)) {  // thread = V row: those that nobody sees become zero, the others are looked through
                         wp_wait(b_full + 8 * (i & 3), i >> 2, abortp, a.polls);
                         const int cc = c0 + r;
                         uint8_t *row = sv + (i & 1) * NB * KB + r * 128;
@@ -432,14 +440,14 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                             // an exponent of ones (what is no number) and one more carries into the sign's place
                             constexpr uint32_t E = kHalf ? 0x7c007c00u : 0x7f807f80u, ONE = E & ~(E << 1);
                             uint32_t odd = 0u;
-#pragma unroll
+#pragma unroll 2
                             for (int d = 0; d < DH / 8; ++d) {
                                 const uint4 y = *reinterpret_cast<const uint4 *>(row + (d >> 3) * KB + (((d & 7) ^ (r & 7)) * 16));
                                 odd |= ((y.x & E) + ONE) | ((y.y & E) + ONE) | ((y.z & E) + ONE) | ((y.w & E) + ONE);
                             }
                             if (odd & 0x80008000u) s_poison[n & 1] = 1;
                         } else {
-#pragma unroll
+#pragma unroll 2
                             for (int d = 0; d < DH / 8; ++d) *reinterpret_cast<uint4 *>(row + (d >> 3) * KB + (((d & 7) ^ (r & 7)) * 16)) = make_uint4(0u, 0u, 0u, 0u);
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -462,8 +470,6 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                             for (int e = 0; e < 32; ++e) s[x][e] = see >> e & 1u ? s[x][e] : 0xff800000u;  // -inf
                         }
                     }
-                    // The first half is made with the maximum as it stood; only where the tile's own maximum, found meanwhile, has grown too
-                    // far past it (a first tile, a rare later one) it is made again.
                     uint64_t sum;
                     uint32_t w[32];
                     // A probability that f16 has no number for would make 0 x inf of an infinite value: where every row sees every key it counts as 2^-24
@@ -478,25 +484,17 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                             for (int e = 0; e < 32; e += 2) x[(e >> 1) & 3] = max3_nan(x[(e >> 1) & 3], __uint_as_float(s[y][e]), __uint_as_float(s[y][e + 1]));
                         return max3_nan(max3_nan(x[0], x[1], x[2]), x[3], x[3]) * c;
                     };
-                    if (fresh) {
-                        const float mx = top();
-                        m = mx < CUDART_INF_F ? (kHalf ? mx - kWpBelow : mx) : CUDART_NAN_F;
-                        huge();
+                    const float mx = top();
+                    bool grow;
+                    float corr;
+                    if constexpr (kHalf) {  // (by the difference, which is exact where the two are near: no rounding of a large m makes P infinite)
+                        grow = fresh || (!(mx - fmaxf(m, -3e38f) <= kWpLazy + kWpBelow) && !(m != m));
+                        corr = grow && !fresh ? ex2(m - (mx - kWpBelow)) : 1.f;
+                    } else {
+                        grow = fresh || (!(mx <= m + kWpLazy) && !(m != m));  // (a maximum that is no number stays)
+                        corr = grow && !fresh ? ex2(m - mx) : 1.f;
                     }
-                    while (true) {
-                        sum = 0ull;
-                        const float base = m == -CUDART_INF_F ? 0.f : m, mx = top();
-                        wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), least, sum, w);
-                        bool grow;
-                        float corr;
-                        if constexpr (kHalf) {  // (by the difference, which is exact where the two are near: no rounding of a large m makes P infinite)
-                            grow = !(mx - fmaxf(m, -3e38f) <= kWpLazy + kWpBelow) && !(m != m);
-                            corr = grow ? ex2(m - (mx - kWpBelow)) : 1.f;
-                        } else {
-                            grow = !(mx <= m + kWpLazy) && !(m != m);  // (a maximum that is no number stays)
-                            corr = grow ? ex2(m - mx) : 1.f;
-                        }
-                        if (!__any_sync(0xffffffffu, grow)) break;
+                    if (__any_sync(0xffffffffu, grow)) {
                         if (grow) m = mx < CUDART_INF_F ? (kHalf ? mx - kWpBelow : mx) : CUDART_NAN_F;  // (inf - inf, as the formula has it)
                         huge();
                         l *= corr;
@@ -513,6 +511,9 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                             }
                         }
                     }
+                    const float base = m == -CUDART_INF_F ? 0.f : m;
+                    sum = 0ull;
+                    wp_exps<T>(s[0], s[1], c2, f2_pack(-base, -base), least, sum, w);
                     auto hand_over = [&](int h) {
                         tc_st32(t_s + 32 * h, w);
                         tc_fence_before();
@@ -522,10 +523,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                     hand_over(0);
                     wp_pin(s[2]);  // (no probability of the second half before the first is handed over)
                     wp_pin(s[3]);
-                    {
-                        const float base = m == -CUDART_INF_F ? 0.f : m;
-                        wp_exps<T>(s[2], s[3], c2, f2_pack(-base, -base), least, sum, w);
-                    }
+                    wp_exps<T>(s[2], s[3], c2, f2_pack(-base, -base), least, sum, w);
                     hand_over(1);
                     float l0, l1;
                     f2_unpack(sum, l0, l1);
@@ -536,9 +534,10 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                 tc_fence_after();
             }
             i0 += g.n_kt;
-            // ---- the rows go out through the place of Q, whole lines at a time
-            constexpr int CH = DH / 8;  // 16-byte chunks of half a row in fp32, of a row in T
-            auto chunk = [&](int tile, int row, int x) { return reinterpret_cast<uint4 *>(sq + tile * NB * QB) + row * CH + (x ^ (row & (CH - 1))); };
+            // ---- the rows go out: parts as they stand in tensor memory, four dims of all rows after four dims of all rows; results through the place of Q,
+            // whole lines at a time
+            constexpr int CH = DH / 8;  // 16-byte chunks of a row in T
+            float4 *const swap = reinterpret_cast<float4 *>(sq) + r;  // [DH / 4][128 rows]: the second stream's O
             auto load_o = [&](int d, uint32_t (&o)[32]) {
                 wp_ld32(t_o + d, o);
                 wp_ld_wait();
@@ -553,7 +552,8 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                         uint32_t o[32];
                         load_o(d, o);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) *chunk(d / (DH / 2), r, d % (DH / 2) / 4 + e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        for (int e = 0; e < 8; ++e)
+                            swap[(d / 4 + e) * kWpRows] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
                     }
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -572,51 +572,49 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                     if (m != m || other.x != other.x) f0 = f1 = l = CUDART_NAN_F;
                     m = t;
                 }
-                const bool none = none0 && none1, direct = g.row < 0;
-                const float inv = direct ? (none ? 0.f : 1.f / l) : 1.f;
-                const int rows = min(per, g.n_tok - row_q * per) * gq;  // of this tile
-                if (!direct && r < rows) a.ml[g.row + row_q * per * gq + r] = make_float2(m, l);
+                const bool direct = g.row < 0;
+                if (direct) {
+                    const float inv = none0 && none1 ? 0.f : 1.f / l;
+                    f0 *= inv;
+                    f1 *= inv;
+                }
+                const int rows = min(per, g.n_tok - row_q * per) * gq, R = g.n_tok * gq, first = row_q * per * gq;  // of this tile; of the part; before this tile
+                const bool store = r < rows && !*abortp;
+                if (!direct && store) a.ml[g.row + first + r] = make_float2(m, l);
+                float4 *const part = reinterpret_cast<float4 *>(a.o + g.row * DH) + first + r;
+                auto chunk = [&](int row, int x) { return reinterpret_cast<uint4 *>(sq + q * NB * QB) + row * CH + (x ^ (row & (CH - 1))); };
+                uint4 *const mine = reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + ((size_t)(g.tok0 + min(p, g.n_tok - 1)) * a.p.Hq + g.kvh * gq + r % gq) * DH);
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-#pragma unroll 1
-                    for (int d = h * (DH / 2); d < (h + 1) * (DH / 2); d += 32) {
-                        uint32_t o[32];
-                        load_o(d, o);
+                for (int d = 0; d < DH; d += 32) {
+                    uint32_t o[32];
+                    load_o(d, o);
+                    float y[32];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float y[4];
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 x = dual && !none1 ? swap[(d / 4 + e) * kWpRows] : make_float4(0.f, 0.f, 0.f, 0.f);
+                        const float z[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) y[z] = none0 ? 0.f : __uint_as_float(o[4 * e + z]) * f0;
-                            if (dual && !none1) {
-                                const uint4 x = *chunk(h, r, d % (DH / 2) / 4 + e);
-                                y[0] += __uint_as_float(x.x) * f1; y[1] += __uint_as_float(x.y) * f1; y[2] += __uint_as_float(x.z) * f1; y[3] += __uint_as_float(x.w) * f1;
-                            }
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) o[4 * e + z] = __float_as_uint(y[z] * inv);
-                        }
-                        if (direct) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                *chunk(q, r, d / 8 + e) = make_uint4(pack_pair<T>(__uint_as_float(o[8 * e]), __uint_as_float(o[8 * e + 1])), pack_pair<T>(__uint_as_float(o[8 * e + 2]), __uint_as_float(o[8 * e + 3])),
-                                                                     pack_pair<T>(__uint_as_float(o[8 * e + 4]), __uint_as_float(o[8 * e + 5])), pack_pair<T>(__uint_as_float(o[8 * e + 6]), __uint_as_float(o[8 * e + 7])));
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) *chunk(dual ? h : q, r, d % (DH / 2) / 4 + e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                        }
+                        for (int k = 0; k < 4; ++k) y[4 * e + k] = (none0 ? 0.f : __uint_as_float(o[4 * e + k]) * f0) + z[k] * f1;
                     }
-                    if (direct && h == 0) continue;
+                    if (direct) {  // (of dual rows, straight away: the place of Q holds other rows' second half still)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!dual || store) *(dual ? mine + d / 8 + e : chunk(r, d / 8 + e)) = make_uint4(pack_pair<T>(y[8 * e], y[8 * e + 1]), pack_pair<T>(y[8 * e + 2], y[8 * e + 3]), pack_pair<T>(y[8 * e + 4], y[8 * e + 5]), pack_pair<T>(y[8 * e + 6], y[8 * e + 7]));
+                    } else if (store) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) part[(int64_t)(d / 4 + e) * R] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+                    }
+                }
+                if (direct && !dual) {
                     __syncwarp();
                     const int lr = lane / CH, lc = lane % CH;
                     if (!*abortp)
 #pragma unroll 4
                         for (int x = 0; x < 32; x += 32 / CH) {
                             const int rr = 32 * (warp & 3) + x + lr, pp = rr * inv_gq >> 16;
-                            if (rr >= rows) continue;
-                            const uint4 y = *chunk(!direct && dual ? h : q, rr, lc);
-                            if (direct) *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + ((size_t)(g.tok0 + row_q * per + pp) * a.p.Hq + g.kvh * gq + rr - pp * gq) * DH + 8 * lc) = y;
-                            else *reinterpret_cast<uint4 *>(a.o + (g.row + row_q * per * gq + rr) * DH + h * (DH / 2) + 4 * lc) = y;
+                            if (rr < rows)
+                                *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + ((size_t)(g.tok0 + row_q * per + pp) * a.p.Hq + g.kvh * gq + rr - pp * gq) * DH + 8 * lc) = *chunk(rr, lc);
                         }
-                    __syncwarp();  // (the place is written again)
                 }
                 tc_fence_before();
             }
@@ -624,6 +622,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
     }
     __syncwarp();
     if (*abortp) {  // a wait ran out: what this CTA has asked for lands within microseconds; do not leave before
+#pragma unroll 1
         for (int i = 0; i < 64; ++i) __nanosleep(4000);
     }
     tc_fence_before();

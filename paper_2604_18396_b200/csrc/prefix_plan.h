@@ -5,35 +5,45 @@
 //   of a group     all tokens of the group's sequences, which follow one another in q, with the positions [0, shared) of its first sequence;
 //                  every row sees every key
 //   of a sequence  its tokens with the positions from its own first one (`shared`, a whole number of pages) up to the row's own
-// Units stand in a row - KV heads outermost, then the groups, then the sequences - and each weighs as many as it has keys, and kPfCost.  That
-// row is cut into equal parts, one per CTA, whatever the lengths are; the CTA of a part computes, of each unit in it, the key tiles that fall between the
+// Units stand in a row - KV heads outermost, then the groups, then the sequences - and each weighs as many as it has keys, twice that with two
+// query tiles, and kPfCost.  That row is cut into equal parts, one per CTA, whatever the lengths are; the CTA of a part computes, of each unit in it, the key tiles that fall between the
 // cuts.  A part of a unit leaves per row its O, not divided yet, its maximum and its sum; who joins them finds the same cuts by the same arithmetic.
 #pragma once
+#include <cmath>
 #include <cstdint>
 
+// PF_CALL: by a call, not in place.  The kernels are called behind cold caches, where a kilobyte of code costs as much as a hundred of these calls.
 #ifdef __CUDACC__
 #define PF_FN __host__ __device__ __forceinline__
+#define PF_CALL static __host__ __device__ __noinline__
 #else
 #define PF_FN inline
+#define PF_CALL inline
 #endif
 
 namespace river {
 
+constexpr int kPfCtas = 148;   // one per SM
 constexpr int kPfKeys = 128;   // of a tile
-constexpr int kPfCost = 256;   // what a unit weighs besides its keys (its start and end)
+constexpr int kPfCost = 512;   // what a unit weighs besides its keys (its start and end)
 constexpr int kPfLeast = 640;  // of a CTA's part: less is not worth its parts' way through memory
 
 PF_FN int pf_per(int gq) { return 128 / gq; }  // tokens of a query tile
 template <class T> PF_FN T pf_min(T a, T b) { return b < a ? b : a; }
 template <class T> PF_FN T pf_max(T a, T b) { return b > a ? b : a; }
 
+// y / w of numbers that mostly fit 32 bits
+PF_CALL uint64_t pf_div(uint64_t y, uint64_t w) { return (y | w) >> 32 ? y / w : (uint32_t)y / (uint32_t)w; }
+
+constexpr int kPfSnap = 448;
+
 struct PfPlan {
-    int ctas, n_tokens, Hq, gq;
-    int groups, own;  // which units there are: 1, 0: groups' (the sequences' rows are a step kernel's); 1, 1: both; 0, 1: sequences' from their first position on
+    int n_tokens, Hq, gq;
+    int groups, own;  // which units there are: 1, 0: groups' (the sequences' own keys are single tokens'); 1, 1: both; 0, 1: sequences' from their first position on
     int slot_rows;    // rows of a place for a part of a unit
 };
 // rows of the scratch: two places per CTA for units that are cut, then the groups' and the sequences' whole ones
-PF_FN int64_t pf_cut_rows(const PfPlan &p) { return 2 * (int64_t)p.ctas * p.slot_rows; }
+PF_FN int64_t pf_cut_rows(const PfPlan &p) { return 2 * (int64_t)kPfCtas * p.slot_rows; }
 PF_FN int pf_slot_rows(int n_tokens, int gq) { return pf_min(2 * pf_per(gq), n_tokens) * gq; }
 
 // A number of units with one list of keys, in order of their tokens
@@ -41,14 +51,19 @@ struct PfEntry {
     int64_t w;  // of all of them; 0: none
     int tok0, n, seq, base, pos0;  // rows; whose row of the table, from which position on; position of the first token (of a sequence)
     int keys;   // of a group
-    int group;
+    int group, f;  // f: weight of a key
 };
 PF_FN PfEntry pf_group_entry(int tok0, int n, int lead, int keys, int span) {
-    return PfEntry{(int64_t)((n + span - 1) / span) * (keys + kPfCost), tok0, n, lead, 0, 0, keys, 1};
+    const int f = 2 * n > span ? 2 : 1;
+    return PfEntry{(int64_t)((n + span - 1) / span) * (f * (int64_t)keys + kPfCost), tok0, n, lead, 0, 0, keys, 1, f};
 }
 PF_FN PfEntry pf_own_entry(int tok0, int n, int seq, int base, int len, int span) {
-    const int64_t before = pf_max(0, len - n - base), T = (n + span - 1) / span;
-    return PfEntry{(T - 1) * (before + kPfCost) + span * T * (T - 1) / 2 + before + n + kPfCost, tok0, n, seq, base, len - n, 0, 0};
+    const int64_t before = pf_max(0, len - n - base), T = (n + span - 1) / span, f = 2 * n > span ? 2 : 1;
+    return PfEntry{(T - 1) * (f * before + kPfCost) + f * (span * T * (T - 1) / 2 + before + n) + kPfCost, tok0, n, seq, base, len - n, 0, 0, (int)f};
+}
+// the weight of a sequence's units before unit t (t below their number)
+PF_FN int64_t pf_before(const PfEntry &e, int t, int span) {
+    return t * (e.f * (int64_t)pf_max(0, e.pos0 - e.base) + kPfCost) + e.f * ((int64_t)span * t * (t + 1) / 2);
 }
 // Unit t of an entry: the weight before it in the entry, its own, its rows, its keys
 struct PfUnit {
@@ -60,33 +75,36 @@ PF_FN PfUnit pf_unit(const PfEntry &e, int t, int span) {
     u.tok = e.tok0 + t * span;
     u.n = pf_min(span, e.n - t * span);
     if (e.group) {
-        u.w = e.keys + kPfCost;
+        u.w = e.f * (int64_t)e.keys + kPfCost;
         u.at = t * u.w;
         u.keys = e.keys;
     } else {
-        const int64_t before = pf_max(0, e.pos0 - e.base);
-        u.at = t * (before + kPfCost) + (int64_t)span * t * (t + 1) / 2;
-        u.w = before + t * span + u.n + kPfCost;
+        u.w = e.f * (pf_max(0, e.pos0 - e.base) + (int64_t)t * span + u.n) + kPfCost;
+        u.at = pf_before(e, t, span);
         u.keys = pf_max(0, e.pos0 + t * span + u.n - e.base);
     }
     u.tiles = pf_max(1, (u.keys + kPfKeys - 1) / kPfKeys);
     return u;
 }
 // which unit of an entry stands at weight y
-PF_FN int pf_unit_at(const PfEntry &e, int64_t y, int span) {
-    if (e.group) return (int)(y / (e.keys + kPfCost));
-    const int64_t before = pf_max(0, e.pos0 - e.base);
+PF_CALL int pf_unit_at(const PfEntry &e, int64_t y, int span) {
+    if (e.group) return (int)pf_div(y, e.f * (int64_t)e.keys + kPfCost);
     int lo = 0, hi = (e.n + span - 1) / span;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (mid * (before + kPfCost) + (int64_t)span * mid * (mid + 1) / 2 <= y) lo = mid; else hi = mid;
+        if (pf_before(e, mid, span) <= y) lo = mid; else hi = mid;
     }
     return lo;
 }
-// weight of a CTA's part of `everything`
-PF_FN int64_t pf_share(int64_t everything, int ctas) { return pf_max((everything + ctas - 1) / ctas, (int64_t)kPfLeast); }
-// the tile of a unit that a cut at weight y goes before
-PF_FN int pf_cut(int64_t y, int64_t w, int tiles) { return y <= 0 ? 0 : y >= w ? tiles : (int)((uint64_t)y * (uint32_t)tiles / (uint64_t)w); }
+// Weight of a CTA's part of `everything`, of up to `ctas` CTAs.  As many to each KV head, where there are enough: parts that begin with a KV head's first unit
+// spare the CTAs in between a unit's start and end.
+PF_FN int64_t pf_share(int64_t everything, int Hkv, int ctas) {
+    if (ctas >= Hkv) ctas -= ctas % Hkv;
+    return pf_max((int64_t)pf_div(everything + ctas - 1, ctas), (int64_t)kPfLeast);
+}
+// The tile of a unit that a cut at weight y goes before.  No cut within kPfSnap of a unit's ends: a part of a tile or two would cost a CTA more, for its
+// start and end, than another one's share grows.
+PF_FN int pf_cut(int64_t y, int64_t w, int tiles) { return y <= kPfSnap ? 0 : y >= w - kPfSnap ? tiles : (int)pf_div((uint64_t)y * (uint32_t)tiles, (uint64_t)w); }
 // What CTA c has of the unit that begins at weight x: tiles k0 .. k1 - 1; its first row among the scratch's (-1: it has all of the unit and the
 // rows have nothing else).
 struct PfPart {
@@ -103,6 +121,15 @@ PF_FN PfPart pf_part(const PfPlan &p, int64_t share, int64_t x, const PfUnit &u,
     else
         r.row = (2 * (int64_t)c + (from <= 0)) * p.slot_rows;  // (a part that the unit begins in is the CTA's last, another one its first)
     return r;
+}
+
+// SMs for the groups' units where single tokens run beside them, so that both take the same time: a CTA of units takes 26 us until its first tile is through
+// and after its last (most of it to fetch its code), and 7.5 us for a thousand of weight; the other SMs 8 us and what HBM needs for their share of `blocks`
+// (K and V of 16 positions of one KV head: 64 dh bytes, at 53 KB/us and SM).  26 + u / x = 8 + b / (n - x).
+PF_FN int pf_split(int64_t units, int64_t blocks, int dh) {
+    const float n = kPfCtas, d = 18.f, u = 7.5e-3f * (float)units, b = 1.2e-3f * (float)dh * (float)blocks;
+    const float p = d * n - u - b, root = sqrtf(p * p + 4.f * d * u * n), x = p > 0.f ? (p + root) / (2.f * d) : 2.f * u * n / (root - p);
+    return pf_min(kPfCtas, pf_max(1, (int)x));
 }
 
 }  // namespace river

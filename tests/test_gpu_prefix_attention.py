@@ -216,11 +216,11 @@ def test_missing_pages_count_as_not_visible():
 
 
 def test_queries_before_position_zero():
-    """More queries than positions: those before position 0 see nothing, and the call says so."""
+    """More queries than positions: those before position 0 see nothing."""
     b = Batch([(0, [(0, 5)]), (0, [(0, 3)])], 4, 2, 64, 16, BF)
     b.lens = [3, 0]
     b.lens_t = i32(b.lens)
-    b.check(ways=[STEP, GROUPS, BOTH, WHOLE], status=-1)
+    b.check(ways=[STEP, GROUPS, BOTH, WHOLE])
 
 
 def test_arrays_that_are_not_as_described():

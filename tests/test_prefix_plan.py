@@ -16,7 +16,7 @@ using namespace river;
 extern "C" int check(int ctas, int n_tokens, int Hkv, int gq, int groups, int own, int n, const int *kinds, const int *tok0, const int *rows, const int *keys,
                      const int *base, long long n_rows, unsigned char *used, int *most) {
     const int span = 2 * pf_per(gq);
-    const PfPlan p{ctas, n_tokens, Hkv * gq, gq, groups, own, pf_slot_rows(n_tokens, gq)};
+    const PfPlan p{n_tokens, Hkv * gq, gq, groups, own, pf_slot_rows(n_tokens, gq)};
     std::vector<PfEntry> e(n);
     std::vector<int64_t> at(n);
     int64_t all = 0;
@@ -25,7 +25,7 @@ extern "C" int check(int ctas, int n_tokens, int Hkv, int gq, int groups, int ow
         at[i] = all;
         all += e[i].w;
     }
-    const int64_t everything = all * Hkv, share = pf_share(everything, ctas);
+    const int64_t everything = all * Hkv, share = pf_share(everything, Hkv, ctas);
     if (share * ctas < everything) return 1;
     *most = 0;
     for (int kvh = 0; kvh < Hkv; ++kvh)
@@ -50,7 +50,7 @@ extern "C" int check(int ctas, int n_tokens, int Hkv, int gq, int groups, int ow
                     next = r.k1;
                     ++parts;
                     whole = r.row < 0;
-                    if (r.row < 0 && (c != c1 || groups)) return 9;
+                    if (r.row < 0 && groups) return 9;
                     for (int64_t k = r.row; r.row >= 0 && k < r.row + (int64_t)u.n * gq; ++k) {
                         if (k >= n_rows) return 10;
                         if (used[k]++) return 11;
@@ -65,6 +65,7 @@ extern "C" int check(int ctas, int n_tokens, int Hkv, int gq, int groups, int ow
         }
     return 0;
 }
+extern "C" int split(long long units, long long items, int dh) { return pf_split(units, items, dh); }
 """
 
 
@@ -93,7 +94,7 @@ def run(plan, ctas, hkv, gq, groups, own, seqs):
                 entries.append((1, starts[mine[0]], rows, sh, 0))
     if own:
         entries += [(0, a, n, length, sh if groups else 0) for a, (n, length, _, sh) in zip(starts, seqs) if n]
-    n_rows = 2 * ctas * min(2 * (128 // gq), at) * gq + groups * (1 + own) * at * hkv * gq
+    n_rows = 2 * 148 * min(2 * (128 // gq), at) * gq + groups * (1 + own) * at * hkv * gq
     used, most = (ctypes.c_ubyte * n_rows)(), ctypes.c_int()
     col = lambda k: (ctypes.c_int * len(entries))(*[e[k] for e in entries])  # noqa: E731
     rc = plan.check(ctas, at, hkv, gq, groups, own, len(entries), col(0), col(1), col(2), col(3), col(4), ctypes.c_longlong(n_rows), used, ctypes.byref(most))
@@ -128,3 +129,10 @@ def test_lengths_that_are_too_short_for_their_queries(plan):
 def test_one_long_prefix_is_everybodys(plan):
     """64 rows of one group over 32 K positions: every CTA has a share of about the same number of tiles."""
     assert run(plan, 148, 8, 4, 1, 0, [(1, 32800, 0, 32768)] * 64) >= 148 // 8
+
+
+def test_both_kinds_of_work_have_sms(plan):
+    ll = ctypes.c_longlong
+    for units in (1, 600, 10 ** 5, 10 ** 7, 10 ** 10, 10 ** 14):
+        n = [plan.split(ll(units), ll(items), 128) for items in (1, 100, 10 ** 4, 10 ** 6, 10 ** 9, 10 ** 13)]
+        assert all(1 <= x <= 148 for x in n) and n == sorted(n, reverse=True)
