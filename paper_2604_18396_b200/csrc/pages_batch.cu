@@ -16,24 +16,43 @@ struct AdmitArgs {
     Paged c;
     const int32_t *refs, *like, *begin, *total;
     int32_t *table_out, *lens_out, *refs_out, *n_new, *status;
+    int rest;  // the entries behind the requests' pages are another kernel's
 };
 
+// Table entries behind a request's pages, by all SMs, beside the deciding cluster.
+__global__ void __launch_bounds__(256) pages_admit_rest_kernel(const AdmitArgs a) {
+    pdl_launch();
+    const int P = a.c.max_pages, up = (1 << a.c.ps_log2) - 1;
+    for (int i = blockIdx.x; i < a.c.n_seqs; i += gridDim.x) {
+        const int64_t total = max(0, a.total[i]);
+        for (int64_t j = ((total + up) >> a.c.ps_log2) + threadIdx.x; j < P; j += 256) a.table_out[(size_t)i * P + j] = -1;
+    }
+}
+
 // Passes like those of pages_reorder_kernel (pages.cu): refs copied, rows written with their entries counted, free ids counted, then handed out.
+// Bound by them, and by what 16 SMs read and write in them: 512 sequences of 2048 pages on 262144 ids 44 us with a row's entries 32 at a time and the
+// lowest ids given by the cluster's first CTA, 30 with 512 entries and every CTA giving, less with the empty entries left to the other SMs.
+constexpr int kAdUnder = 16;  // times 32 entries of a row under way
 __global__ void __launch_bounds__(kPgThreads) pages_admit_kernel(const AdmitArgs a) {
     extern __shared__ int pg_raw[];
     __shared__ PagesScan s;
     cg::cluster_group cluster = cg::this_cluster();
     const int S = a.c.n_seqs, P = a.c.max_pages, N = a.c.n_pages, lg = a.c.ps_log2, up = (1 << lg) - 1, cap = P << lg;
     const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), thread = rank * kPgThreads + threadIdx.x, threads = ctas * kPgThreads;
-    // every CTA for itself: lengths held, positions that a request begins with, pages wanted before its own
-    int *const len = pg_raw, *const keep = len + S, *const start = keep + S;
+    // every CTA for itself: whom a request begins like, lengths held and wanted, positions that it begins with, pages wanted before its own
+    int *const like = pg_raw, *const len = like + S, *const total = len + S, *const keep = total + S, *const start = keep + S;
     if (threadIdx.x == 0) s.bad = s.full = s.odd = 0, s.wanted = 0;
+    for (int i = threadIdx.x; i < S; i += kPgThreads) {
+        like[i] = a.like[i];
+        len[i] = a.c.lens[i];
+        total[i] = a.total[i];
+        keep[i] = a.begin[i];
+    }
     copy_ints(a.refs_out, a.refs, N, thread, threads);
-    for (int i = threadIdx.x; i < S; i += kPgThreads) len[i] = a.c.lens[i];
     __syncthreads();
     long long mine = 0;
     for (int i = threadIdx.x; i < S; i += kPgThreads) {
-        const int p = a.like[i], b = a.begin[i], n = a.total[i];
+        const int p = like[i], b = keep[i], n = total[i];
         int k = 0, want = 0;
         if (p < -1 || p >= S || b < 0 || n < 0 || len[i] < 0 || len[i] > cap) s.bad = 1;
         else if (n > cap) s.full = 1;
@@ -57,19 +76,30 @@ __global__ void __launch_bounds__(kPgThreads) pages_admit_kernel(const AdmitArgs
     if (code == RIVER_OK) {
         // a warp per sequence
         for (int i = thread >> 5; i < S; i += threads / 32) {
-            const int p = a.like[i], old_n = (len[i] + up) >> lg, n = (keep[i] + up) >> lg;
-            const int32_t *old_row = a.c.table + (size_t)i * P, *row = a.c.table + (size_t)max(p, 0) * P;
+            const int old_n = (len[i] + up) >> lg, n = (keep[i] + up) >> lg, end = a.rest ? max(old_n, n) : P, mine_to = (total[i] + up) >> lg;
+            const int32_t *old_row = a.c.table + (size_t)i * P, *row = a.c.table + (size_t)max(like[i], 0) * P;
             int32_t *to = a.table_out + (size_t)i * P;
-            for (int j = threadIdx.x & 31; j < P; j += 32) {
-                const int old = j < old_n ? old_row[j] : -1, page = j < n ? max(row[j], -1) : -1;
-                if (page >= N || old >= N) {
-                    atomicExch(cluster.map_shared_rank(&s.odd, 0), 1);
-                    continue;
+            for (int j0 = threadIdx.x & 31; j0 < end; j0 += 32 * kAdUnder) {
+                int old[kAdUnder], page[kAdUnder];
+#pragma unroll
+                for (int e = 0; e < kAdUnder; ++e) {
+                    const int j = j0 + 32 * e;
+                    old[e] = j < old_n ? old_row[j] : -1;
+                    page[e] = j < n ? max(row[j], -1) : -1;
                 }
-                to[j] = page;
-                if (page == old) continue;  // (a sequence that goes on)
-                if (page >= 0) atomicAdd(a.refs_out + page, 1);
-                if (old >= 0) atomicSub(a.refs_out + old, 1);
+#pragma unroll
+                for (int e = 0; e < kAdUnder; ++e) {
+                    const int j = j0 + 32 * e;
+                    if (j >= end) continue;
+                    if (page[e] >= N || old[e] >= N) {
+                        atomicExch(cluster.map_shared_rank(&s.odd, 0), 1);
+                        continue;
+                    }
+                    if (!a.rest || j < mine_to) to[j] = page[e];
+                    if (page[e] == old[e]) continue;  // (a sequence that goes on)
+                    if (page[e] >= 0) atomicAdd(a.refs_out + page[e], 1);
+                    if (old[e] >= 0) atomicSub(a.refs_out + old[e], 1);
+                }
             }
         }
         cluster.sync();
@@ -82,14 +112,15 @@ __global__ void __launch_bounds__(kPgThreads) pages_admit_kernel(const AdmitArgs
             }))
             code = RIVER_E_NOPAGE;
     }
+    if (a.rest) pdl_wait();  // (the other entries are written; and this kernel ends behind that one)
     if (code != RIVER_OK) {  // the state as it was
         cluster.sync();
         copy_ints(a.table_out, a.c.table, (size_t)S * P, thread, threads);
         copy_ints(a.refs_out, a.refs, N, thread, threads);
     }
     for (int i = thread; i < S; i += threads) {
-        a.lens_out[i] = code == RIVER_OK ? a.total[i] : len[i];
-        a.n_new[i] = code == RIVER_OK ? a.total[i] - keep[i] : 0;
+        a.lens_out[i] = code == RIVER_OK ? total[i] : len[i];
+        a.n_new[i] = code == RIVER_OK ? total[i] - keep[i] : 0;
     }
     if (thread == 0) *a.status = code;
     cluster.sync();  // (nobody leaves while its shared memory may be read)
@@ -158,7 +189,7 @@ __device__ __forceinline__ int equal_pages(const GroupsArgs &a, int i) {
     auto whole = [&](int s) { return (int)max((int64_t)0, min((int64_t)a.c.lens[s] - max((int64_t)0, (int64_t)a.q_start[s + 1] - a.q_start[s]), (int64_t)P << a.c.ps_log2)) >> a.c.ps_log2; };
     const int w = min(whole(i - 1), whole(i));
     const int32_t *x = a.c.table + (size_t)(i - 1) * P, *y = x + P;
-    constexpr int U = 8;
+    constexpr int U = 16;
     for (int j0 = 0; j0 < w; j0 += 32 * U) {
         int p[U], r[U];
 #pragma unroll
@@ -191,10 +222,9 @@ __device__ __forceinline__ void groups_of(const GroupsArgs &a, const int32_t *c,
         if (lane == 31) part[warp] = l;
         if (i < S) prefix[i] = INT32_MAX;
         __syncthreads();
-        int before = carry;
-        for (int w = 0; w < warp; ++w) before = max(before, part[w]);
-        l = max(l, before);
-        for (int w = 0; w < 32; ++w) carry = max(carry, part[w]);
+        const int first = part[lane];  // of warp `lane`
+        l = max(l, max(carry, __reduce_max_sync(0xffffffffu, lane < warp ? first : -1)));
+        carry = max(carry, __reduce_max_sync(0xffffffffu, first));
         if (i < S) a.lead[i] = l;
         if (linked) atomicMin(&prefix[l], n);
         __syncthreads();
@@ -251,7 +281,12 @@ extern "C" int river_pages_admit(const river_paged *c, const int32_t *refs, cons
     a.refs_out = refs_out;
     a.n_new = n_new;
     a.status = status;
-    return launch_deciding(pages_admit_kernel, a, (size_t)c->n_seqs * c->max_pages + c->n_pages, 3 * sizeof(int) * (size_t)c->n_seqs, static_cast<cudaStream_t>(cuda_stream));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const size_t entries = (size_t)c->n_seqs * c->max_pages;
+    a.rest = entries >= (1u << 18);
+    if (a.rest)
+        if (const int rc = launch_plain(pages_admit_rest_kernel, dim3(std::min(c->n_seqs, 4 * 148)), dim3(256), st, a)) return rc;
+    return launch_deciding(pages_admit_kernel, a, entries + c->n_pages, kPgSeqInts * sizeof(int) * (size_t)c->n_seqs, st, a.rest);
 }
 
 extern "C" int river_pages_slots(const river_paged *c, const int32_t *n_new, int n_tokens, int32_t *q_start, int32_t *positions, int32_t *seqs,

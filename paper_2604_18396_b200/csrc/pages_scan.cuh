@@ -14,10 +14,12 @@ constexpr int kPgThreads = 1024;
 constexpr int kPgSeqs = 8192;    // sequences whose prefix sums are held in shared memory
 constexpr int kPgSeqInts = 5;    // of a reordering, per sequence in (dynamic) shared memory
 constexpr int kPgCtas = 8;       // of the deciding cluster (a portable size)
+constexpr int kPgRuns = 4;       // of page ids per warp, where free ones are looked for
 
 // Shared memory of a deciding CTA; `count` is read and the first one's `odd` written by the other CTAs of the cluster.
 struct PagesScan {
     int part[33], count[2];
+    int runs[kPgRuns * 32 * 2 * kPgCtas];  // free ids per run, written by all CTAs of the cluster, then how many there are before
     int bad, full;  // what every CTA finds for itself: a sequence or length out of range, a row too long
     int odd;        // a page out of range: the first CTA's tells, behind a barrier of the cluster
     unsigned long long wanted;  // of all sequences, where 32 bits may not hold it
@@ -110,20 +112,56 @@ __device__ __forceinline__ int cluster_scan(int mine, PagesScan &s, cg::cluster_
 }
 
 // give(k, id) for the `want` lowest ids with refs 0, ascending, if there are as many; returns whether there are.  All threads of the cluster.
+// A warp has kPgRuns runs of ids, and neighbouring runs are different CTAs': the lowest ids, which are given, are everybody's.
 template <class F>
 __device__ inline bool lowest_free(const int32_t *refs, int n_pages, int want, PagesScan &s, cg::cluster_group &cluster, F give) {
-    const Run run(n_pages, cluster.block_rank(), cluster.num_blocks());
-    int mine = 0, all;
-    run.each(refs, [&](int, int r) { mine += r == 0; });
-    int k = cluster_scan(mine, s, cluster, all);
-    if (all < want) return false;
-    if (mine > 0 && k < want)
-        run.each(refs, [&](int p, int r) {
-            if (r == 0) {
-                if (k < want) give(k, p);
-                ++k;
+    constexpr int U = 4;  // times 32 ids under way
+    const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = kPgRuns * 32 * ctas;
+    const int64_t per = ((int64_t)n_pages + 32 * (int64_t)n - 1) / (32 * n) * 32;
+    auto run_of = [&](int t) { return (32 * t + warp) * ctas + rank; };
+    // f(id, lanes whose ids are free) over a run until it answers no
+    auto each = [&](int run, auto f) {
+        const int64_t lo = min((int64_t)n_pages, run * per), hi = min((int64_t)n_pages, lo + per);
+        for (int64_t p0 = lo; p0 < hi; p0 += 32 * U) {
+            int r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t p = p0 + 32 * u + lane;
+                r[u] = p < hi ? __ldcg(refs + p) : 1;
             }
-        });
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (!f((int)(p0 + 32 * u + lane), __ballot_sync(0xffffffffu, r[u] == 0))) return;
+        }
+    };
+#pragma unroll
+    for (int t = 0; t < kPgRuns; ++t) {
+        int mine = 0;
+        each(run_of(t), [&](int, unsigned free) { mine += __popc(free); return true; });
+        if (lane < ctas) *cluster.map_shared_rank(&s.runs[run_of(t)], lane) = mine;
+    }
+    cluster.sync();
+    // free ids before each run
+    int all = 0;
+    for (int i0 = 0; i0 < n; i0 += kPgThreads) {
+        const int i = i0 + threadIdx.x;
+        int total;
+        const int before = cta_scan(i < n ? s.runs[i] : 0, s.part, total);
+        if (i < n) s.runs[i] = all + before;
+        all += total;
+    }
+    __syncthreads();
+    if (all < want) return false;
+    for (int t = 0; t < kPgRuns; ++t) {
+        int k = s.runs[run_of(t)];
+        if (k < want)
+            each(run_of(t), [&](int p, unsigned free) {
+                const int rank_of = k + __popc(free & ((1u << lane) - 1u));
+                if ((free >> lane & 1u) && rank_of < want) give(rank_of, p);
+                k += __popc(free);
+                return k < want;
+            });
+    }
     return true;
 }
 // the last i < n with prefix[i] <= k (prefix[0] = 0): whose want number k is
@@ -157,23 +195,26 @@ __device__ __forceinline__ void copy_ints(int32_t *to, const int32_t *from, size
 
 // work: table entries and page ids.  A few thousand are one CTA's; from 2^18 on twice the portable cluster pays (256 sequences of 2048
 // pages, 65536 ids: 24 -> 17 us).
+// beside: it may start before the kernel before it has ended.
 template <class A>
-int launch_deciding(void (*kernel)(A), const A &a, size_t work, size_t smem, cudaStream_t st) {
+int launch_deciding(void (*kernel)(A), const A &a, size_t work, size_t smem, cudaStream_t st, bool beside = false) {
     const unsigned ctas = work <= 4 * kPgThreads ? 1 : work < (1u << 18) ? kPgCtas : 2 * kPgCtas;
     if (ctas > 8 && cuda_rc(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1))) return RIVER_E_DEVICE;
     // the limit belongs to the kernel, not to the call: whoever sets it sets the same one, or a launch of another thread could fail by it
     constexpr int most = kPgSeqInts * sizeof(int) * kPgSeqs;
     if (smem > (32u << 10) && cuda_rc(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most))) return RIVER_E_DEVICE;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim = {ctas, 1, 1};
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {ctas, 1, 1};
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(kPgThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cfg.attrs = &at;
-    cfg.numAttrs = ctas > 1 ? 1 : 0;
+    cfg.attrs = at;
+    cfg.numAttrs = beside ? 2 : ctas > 1 ? 1 : 0;
     return cuda_rc(cudaLaunchKernelEx(&cfg, kernel, a));
 }
 
