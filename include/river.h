@@ -444,7 +444,8 @@ int river_prefix_groups(const river_paged *c, const int32_t *q_start, int least,
  *   max_own   about the most positions behind the shared ones that a sequence has, new ones included, by which the way of computing is chosen
  *             (0: as many as a row of the table holds); the result does not depend on it but for rounding
  *   workspace [dev] river_prefix_attention_bytes(n_seqs, n_tokens, Hq, Hkv, dh) bytes, 128-byte aligned; what it holds before does not matter, and calls
- *             that may run at the same time have one each
+ *             that may run at the same time have one each.  A small call may do without: where there is none, or less, the call is done or answers
+ *             RIVER_E_NOMEM before anything is queued
  *   status    [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as not visible);
  *             lead or shared is not as described, where the way of computing reads them (rows of sequences that it concerns may hold anything); q_start
  *             descends, a length is negative (it counts as 0) or more than a row of the table holds (it counts as that), or a sequence has more than max_q

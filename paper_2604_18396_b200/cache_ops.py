@@ -290,7 +290,7 @@ def prefix_attention(q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, 
 
     q: [tokens, Hq, dh] of the pool's type (any strides over tokens and heads that are multiples of 8); sequence s has the rows q_start[s] ..
     q_start[s + 1] - 1 (int32 [n_seqs + 1]), its last positions, at most max_q of them; max_own: about the most positions behind the shared ones (0: not
-    known); softmax_scale: default 1 / sqrt(dh); workspace (uint8): prefix_attention_bytes of them, for callers who keep one."""
+    known); softmax_scale: default 1 / sqrt(dh); workspace (uint8): prefix_attention_bytes of them, for callers who keep one; calls that may run at the same time have one each."""
     _ints(layer | max_q | max_own, "layer, max_q, max_own")
     dev, qs, n = pool.get_device(), q.shape, lens.shape
     c = _cache(pool, table, lens, dev)
@@ -298,14 +298,21 @@ def prefix_attention(q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, 
         _refuse("q: [tokens, Hq, dh] of the pool's type")
     if out.dtype is not q.dtype or out.shape != qs or out.get_device() != dev or not out.is_contiguous():
         _refuse("out: contiguous, q's shape and type")
-    if workspace is None:
-        workspace = _scratch(-(-prefix_attention_bytes(table.shape[0], qs[0], qs[1], pool.shape[3], qs[2]) // 4), pool.device, stream)
-    elif workspace.dtype is not torch.uint8 or workspace.dim() != 1 or workspace.get_device() != dev or not workspace.is_contiguous():
+    if workspace is not None and (workspace.dtype is not torch.uint8 or workspace.dim() != 1 or workspace.get_device() != dev or not workspace.is_contiguous()):
         _refuse("workspace: contiguous CUDA uint8 [bytes]")
-    _run(load().river_prefix_attention, dev, stream, (q, out, q_start, pool, table, lens, lead, shared, workspace, status), c, layer, qs[0], max_q, max_own,
-         _i32(q_start, (table.shape[0] + 1,), dev, "q_start"), _i32(lead, n, dev, "lead"), _i32(shared, n, dev, "shared"), qs[1], _rows(q, dev, "q"),
-         qs[2] ** -0.5 if softmax_scale is None else softmax_scale, out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
-         0 if status is None else _i32(status, (1,), dev, "status"))
+    args = (c, layer, qs[0], max_q, max_own, _i32(q_start, (table.shape[0] + 1,), dev, "q_start"), _i32(lead, n, dev, "lead"), _i32(shared, n, dev, "shared"),
+            qs[1], _rows(q, dev, "q"), qs[2] ** -0.5 if softmax_scale is None else softmax_scale, out.data_ptr())
+    word = 0 if status is None else _i32(status, (1,), dev, "status")
+    fn, used = load().river_prefix_attention, (q, out, q_start, pool, table, lens, lead, shared, workspace, status)
+    if workspace is None:
+        try:  # (a small call needs none, and asking the allocator takes as long as the rest of the call)
+            return _run(fn, dev, stream, used, *args, 0, 0, word)
+        except RiverError as e:
+            if e.code != -3:
+                raise
+        workspace = _scratch(-(-prefix_attention_bytes(table.shape[0], qs[0], qs[1], pool.shape[3], qs[2]) // 4), pool.device, stream)
+        used = (*used[:8], workspace, status)
+    _run(fn, dev, stream, used, *args, workspace.data_ptr(), workspace.nbytes, word)
 
 
 def prefix_attention_bytes(n_seqs: int, tokens: int, hq: int, hkv: int, dh: int) -> int:

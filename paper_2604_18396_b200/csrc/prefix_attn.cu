@@ -126,6 +126,7 @@ int launch_tiles(const PrefixArgs &a, const CUtensorMap &map, cudaStream_t st) {
 }
 template <class T, int DH>
 int launch(PrefixArgs a, PrefixShape s, cudaStream_t st) {
+    if (s.mode != kPfStep && !a.head) return RIVER_E_NOMEM;
     a.p.groups = s.mode == kPfGroups || s.mode == kPfBoth;
     a.p.own = s.mode == kPfBoth || s.mode == kPfWhole;
     // the pages of this block, as rows of a head's dims
@@ -174,8 +175,8 @@ int prefix_args(const river_paged *c, int layer, int n_tokens, int max_q, int ma
     a->q_tok = q->token;
     a->q_head = q->head;
     const PrefixScratch s = prefix_scratch(c->n_seqs, n_tokens, Hq, gq, c->dh);
-    if (!workspace || !aligned_to(workspace, 128)) return RIVER_E_BADARG;
-    if (workspace_bytes < s.bytes) return RIVER_E_NOMEM;
+    if (!aligned_to(workspace, 128)) return RIVER_E_BADARG;
+    if (!workspace || workspace_bytes < s.bytes) return RIVER_OK;  // (not every way needs one)
     uint8_t *const w = static_cast<uint8_t *>(workspace);
     a->head = reinterpret_cast<PfHead *>(w);
     a->group = reinterpret_cast<PfGroup *>(w + s.group);

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
         mine = i < D ? pf_entry(a, i, span) : PfEntry{};
         at = all + pf_scan<kWpThreads / 32>(mine.w, beside && i < D ? pf_blocks(a, i) : 0, s_part, all, blocks);
     }
-    const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.c.Hkv, beside ? pf_split(everything, blocks * a.c.Hkv * ((gq + 7) / 8), a.c.dh) : kPfCtas);
+    const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.c.Hkv, beside ? pf_split(everything, blocks * a.c.Hkv * ((gq + 7) / 8), a.c.dh) : kPfCtas, a.p.own);
     const int64_t x0 = blockIdx.x * share, x1 = min(x0 + share, everything);
     if (x0 < everything || blockIdx.x == 0) {
         const int kvh0 = all ? (int)pf_div(x0, all) : 0;

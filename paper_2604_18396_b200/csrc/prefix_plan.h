@@ -12,20 +12,17 @@
 #include <cmath>
 #include <cstdint>
 
-// PF_CALL: by a call, not in place.  The kernels are called behind cold caches, where a kilobyte of code costs as much as a hundred of these calls.
 #ifdef __CUDACC__
 #define PF_FN __host__ __device__ __forceinline__
-#define PF_CALL static __host__ __device__ __noinline__
 #else
 #define PF_FN inline
-#define PF_CALL inline
 #endif
 
 namespace river {
 
 constexpr int kPfCtas = 148;   // one per SM
 constexpr int kPfKeys = 128;   // of a tile
-constexpr int kPfCost = 512;   // what a unit weighs besides its keys (its start and end)
+constexpr int kPfCost = 800;   // what a unit weighs besides its keys (its start and end: 6 us)
 constexpr int kPfLeast = 640;  // of a CTA's part: less is not worth its parts' way through memory
 
 PF_FN int pf_per(int gq) { return 128 / gq; }  // tokens of a query tile
@@ -33,7 +30,7 @@ template <class T> PF_FN T pf_min(T a, T b) { return b < a ? b : a; }
 template <class T> PF_FN T pf_max(T a, T b) { return b > a ? b : a; }
 
 // y / w of numbers that mostly fit 32 bits
-PF_CALL uint64_t pf_div(uint64_t y, uint64_t w) { return (y | w) >> 32 ? y / w : (uint32_t)y / (uint32_t)w; }
+PF_FN uint64_t pf_div(uint64_t y, uint64_t w) { return (y | w) >> 32 ? y / w : (uint32_t)y / (uint32_t)w; }
 
 constexpr int kPfSnap = 448;
 
@@ -87,7 +84,7 @@ PF_FN PfUnit pf_unit(const PfEntry &e, int t, int span) {
     return u;
 }
 // which unit of an entry stands at weight y
-PF_CALL int pf_unit_at(const PfEntry &e, int64_t y, int span) {
+PF_FN int pf_unit_at(const PfEntry &e, int64_t y, int span) {
     if (e.group) return (int)pf_div(y, e.f * (int64_t)e.keys + kPfCost);
     int lo = 0, hi = (e.n + span - 1) / span;
     while (hi - lo > 1) {
@@ -96,10 +93,10 @@ PF_CALL int pf_unit_at(const PfEntry &e, int64_t y, int span) {
     }
     return lo;
 }
-// Weight of a CTA's part of `everything`, of up to `ctas` CTAs.  As many to each KV head, where there are enough: parts that begin with a KV head's first unit
-// spare the CTAs in between a unit's start and end.
-PF_FN int64_t pf_share(int64_t everything, int Hkv, int ctas) {
-    if (ctas >= Hkv) ctas -= ctas % Hkv;
+// Weight of a CTA's part of `everything`, of up to `ctas` CTAs.  Where units are long, of groups that is, as many to each KV head, if there are enough: parts that
+// begin with a KV head's first unit spare the CTAs in between a unit's start and end.
+PF_FN int64_t pf_share(int64_t everything, int Hkv, int ctas, int own) {
+    if (!own && ctas >= Hkv) ctas = pf_min((ctas + Hkv / 2) / Hkv, kPfCtas / Hkv) * Hkv;
     return pf_max((int64_t)pf_div(everything + ctas - 1, ctas), (int64_t)kPfLeast);
 }
 // The tile of a unit that a cut at weight y goes before.  No cut within kPfSnap of a unit's ends: a part of a tile or two would cost a CTA more, for its
@@ -124,10 +121,10 @@ PF_FN PfPart pf_part(const PfPlan &p, int64_t share, int64_t x, const PfUnit &u,
 }
 
 // SMs for the groups' units where single tokens run beside them, so that both take the same time: a CTA of units takes 26 us until its first tile is through
-// and after its last (most of it to fetch its code), and 7.5 us for a thousand of weight; the other SMs 8 us and what HBM needs for their share of `blocks`
+// and after its last (most of it to fetch its code), and 8 us for a thousand of weight; the other SMs 8 us and what HBM needs for their share of `blocks`
 // (K and V of 16 positions of one KV head: 64 dh bytes, at 53 KB/us and SM).  26 + u / x = 8 + b / (n - x).
 PF_FN int pf_split(int64_t units, int64_t blocks, int dh) {
-    const float n = kPfCtas, d = 18.f, u = 7.5e-3f * (float)units, b = 1.2e-3f * (float)dh * (float)blocks;
+    const float n = kPfCtas, d = 18.f, u = 8e-3f * (float)units, b = 1.2e-3f * (float)dh * (float)blocks;
     const float p = d * n - u - b, root = sqrtf(p * p + 4.f * d * u * n), x = p > 0.f ? (p + root) / (2.f * d) : 2.f * u * n / (root - p);
     return pf_min(kPfCtas, pf_max(1, (int)x));
 }

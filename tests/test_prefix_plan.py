@@ -25,8 +25,8 @@ extern "C" int check(int ctas, int n_tokens, int Hkv, int gq, int groups, int ow
         at[i] = all;
         all += e[i].w;
     }
-    const int64_t everything = all * Hkv, share = pf_share(everything, Hkv, ctas);
-    if (share * ctas < everything) return 1;
+    const int64_t everything = all * Hkv, share = pf_share(everything, Hkv, ctas, own);
+    if (share * kPfCtas < everything) return 1;
     *most = 0;
     for (int kvh = 0; kvh < Hkv; ++kvh)
         for (int i = 0; i < n; ++i) {
@@ -41,9 +41,9 @@ extern "C" int check(int ctas, int n_tokens, int Hkv, int gq, int groups, int ow
                 if ((int64_t)u.tiles * kPfKeys < u.keys) return 5;
                 const int64_t x = kvh * all + at[i] + y;
                 const int c0 = (int)(x / share), c1 = (int)((x + u.w - 1) / share);
-                if (c1 >= ctas) return 6;
+                if (c1 >= kPfCtas) return 6;
                 int next = 0, parts = 0, whole = 0;
-                for (int c = 0; c < ctas; ++c) {
+                for (int c = 0; c < kPfCtas; ++c) {
                     const PfPart r = pf_part(p, share, x, u, c, kvh, kinds[i]);
                     if (r.k1 <= r.k0) { if (r.k1 != r.k0) return 7; continue; }
                     if (c < c0 || c > c1 || r.k0 != next) return 8;
