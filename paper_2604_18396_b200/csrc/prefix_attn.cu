@@ -20,14 +20,15 @@ enum PrefixMode {
 // of about 16 SMs, takes whole ones.
 int own_splits(const PrefixArgs &a, int64_t positions, double rate, double &best_t) {
     const int per_sm = a.c.dh == 128 ? kPfOwnCtas<128> : kPfOwnCtas<64>;
-    const double units = (double)a.p.n_tokens * a.c.Hkv * ((a.p.gq + 7) / 8), blocks = positions / 16 + 1.0, block_us = 64.0 * a.c.dh / rate;
+    const double tiles = a.c.Hkv * ((a.p.gq + 7) / 8), units = a.p.n_tokens * tiles, blocks = positions / 16 + 1.0, block_us = 64.0 * a.c.dh / rate;
+    const double places_of_queries = (double)a.c.n_seqs * a.max_q * tiles, idle = std::max(0.0, places_of_queries - units) * 0.0015;  // (a CTA leaves where there is no query)
     int best = 1;
     best_t = 1e300;
-    for (int s = 1; s <= kStepMaxSplits; ++s) {
+    for (int s = 1; s <= kStepMaxSplits && places_of_queries * s <= INT32_MAX; ++s) {
         const double places = s <= 4 ? kPfCtas * per_sm : kPfCtas / 18 * (16 * per_sm / s) * s;
         const double turns = 0.5 * std::ceil(blocks / (s * kStepWarps)), stream = places * blocks / s * block_us, fixed = 4.0 + 0.25 * s;
         const double rounds = units * s / places, full = std::floor(rounds), rest = rounds - full;
-        const double t = full * (std::max(stream, turns) + fixed) + (rest > 0 ? std::max(stream * rest, turns) + fixed : 0.0);
+        const double t = full * (std::max(stream, turns) + fixed) + (rest > 0 ? std::max(stream * rest, turns) + fixed : 0.0) + idle * s;
         if (t < 0.99 * best_t) { best_t = t; best = s; }
     }
     return best;
@@ -57,7 +58,8 @@ PrefixShape prefix_shape(const PrefixArgs &a, int own) {
     const int step = own_splits(a, cap, 13e6, step_us), own_step = own_splits(a, own, 6e6, own_us);
     step_us = std::max(step_us, 6.0 + ((double)(cap - own) + (double)a.c.n_seqs * own) * position / 6e6);
     const double rows = tokens * gq, shared_us = heads * std::ceil(rows / 256.0) * ((cap - own) / 128.0 * (rows <= 128 ? 0.9 : 1.8) + 4.0) / kPfCtas;
-    own_us = tokens * heads * rt * (own / 16.0 + 6.0) * a.c.dh * 1.2e-3 / kPfCtas;
+    const double idle_us = own_us > 1e299 ? 1e300 : std::max(0.0, (double)a.c.n_seqs * a.max_q - tokens) * heads * rt * 0.0015 * own_step;
+    own_us = tokens * heads * rt * (own / 16.0 + 6.0) * a.c.dh * 1.2e-3 / kPfCtas + idle_us;
     const double per_seq = std::max(1.0, tokens / a.c.n_seqs), units = heads * a.c.n_seqs * std::ceil(per_seq / span), tile_us = per_seq * gq <= 128 ? 0.9 : 1.8;
     const double own_tiles_us = units * (own / 128.0 * tile_us + 8.0) / kPfCtas, whole_us = units * (cap / 128.0 * tile_us + 5.0) / kPfCtas;
     PrefixShape s = {kPfStep, step};
@@ -127,6 +129,8 @@ int launch_tiles(const PrefixArgs &a, const CUtensorMap &map, cudaStream_t st) {
 template <class T, int DH>
 int launch(PrefixArgs a, PrefixShape s, cudaStream_t st) {
     if (s.mode != kPfStep && !a.head) return RIVER_E_NOMEM;
+    const int64_t tiles = (int64_t)a.c.Hkv * ((a.p.gq + 7) / 8), ctas = s.splits * tiles * a.max_q * a.c.n_seqs;  // (of single tokens)
+    if ((s.mode == kPfStep || s.mode == kPfGroups) && ctas > INT32_MAX) return RIVER_E_SHAPE;
     a.p.groups = s.mode == kPfGroups || s.mode == kPfBoth;
     a.p.own = s.mode == kPfBoth || s.mode == kPfWhole;
     // the pages of this block, as rows of a head's dims
@@ -136,10 +140,7 @@ int launch(PrefixArgs a, PrefixShape s, cudaStream_t st) {
     if (!make_map_bf16(&map, a.c.pool + rows * DH * 2 * a.layer0, DH, rows, 16)) return RIVER_E_DEVICE;
     if (s.mode != kPfStep)
         if (const int rc = launch_tiles<T, DH>(a, map, st)) return rc;
-    const int64_t tiles = (int64_t)a.c.Hkv * ((a.p.gq + 7) / 8);
     if (s.mode == kPfStep || s.mode == kPfGroups) {
-        const int64_t ctas = s.splits * tiles * a.max_q * a.c.n_seqs;
-        if (ctas > INT32_MAX) return RIVER_E_SHAPE;
         const int rc = launch_beside(prefix_own_kernel<T, DH>, dim3((unsigned)ctas), 32 * kStepWarps, kPfOwnSmem<DH>, st, s.splits, s.mode == kPfGroups, map, a, s.splits);
         if (rc || s.mode == kPfStep) return rc;
     }

@@ -298,6 +298,56 @@ def test_other_streams_graphs_and_two_calls_at_once():
             assert ((x.out.double() - want).abs() <= tol).all()
 
 
+def test_rows_behind_the_last_sequence_stay():
+    """A batch padded to a fixed number of rows, as a captured step has it."""
+    b = Batch([(320, [(4, 1), (20, 1), (9, 2)]), (0, [(70, 1)])], 8, 2, 64, 16, BF)
+    want, tol = b.statement()
+    t = b.q.shape[0]
+    b.q, b.out = torch.cat((b.q, torch.full((40, 8, 64), NAN, dtype=BF, device="cuda"))), torch.empty(t + 40, 8, 64, dtype=BF, device="cuda")
+    for way in [None] + b.ways():
+        b.out.fill_(7.0)
+        if way is None:
+            b.call()
+        else:
+            assert b.way(way) == 0
+        assert b.status.item() == 0 and ((b.out[:t].double() - want).abs() <= tol).all() and (b.out[t:] == 7.0).all(), way
+
+
+def test_one_long_prompt_among_many_single_tokens():
+    """Places of queries that are none, by the million: not a grid of single tokens."""
+    b = Batch([(64, [(3, 1)] * 200 + [(0, 900)] + [(5, 1)] * 100)], 4, 2, 64, 16, BF)
+    want, tol = b.statement()
+    b.call()
+    assert b.status.item() == 0 and ((b.out.double() - want).abs() <= tol).all()
+    b.out.fill_(NAN)
+    b.call(max_q=2 ** 31 - 1)  # (as many as there are rows)
+    assert b.status.item() == 0 and ((b.out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("max_own", [0, 1, 100, 5000, 2 ** 31 - 1])
+def test_whatever_the_caller_expects(max_own):
+    for groups in ([(2000, [(30 * i, 1) for i in range(20)])], [(48, [(9, 30), (0, 2)])]):
+        b = Batch(groups, 8, 2, 128, 16, F16)
+        want, tol = b.statement()
+        b.call(max_own=max_own)
+        assert b.status.item() == 0 and ((b.out.double() - want).abs() <= tol).all()
+
+
+def test_a_workspace_of_the_callers():
+    b = Batch([(1008, [(5 * i, 1) for i in range(64)])], 8, 2, 128, 16, BF)
+    b.table = torch.nn.functional.pad(b.table, (0, 4096 - b.table.shape[1]), value=-1)  # (by the table's width, groups pay)
+    want, tol = b.statement()
+    n = prefix_attention_bytes(64, 64, 8, 2, 128)
+    work = torch.full((n,), 0xff, dtype=torch.uint8, device="cuda")
+    b.call(workspace=work, max_own=400)
+    assert b.status.item() == 0 and ((b.out.double() - want).abs() <= tol).all()
+    with pytest.raises(binding.RiverError):
+        b.call(workspace=work[: n - 128], max_own=400)
+    for bad in (work.view(torch.int32), work.view(2, -1)[:, :5], work.cpu()):
+        with pytest.raises(ValueError):
+            b.call(workspace=bad)
+
+
 def test_no_tokens():
     b = Batch([(64, [(4, 1), (20, 1)])], 4, 2, 64, 16, BF)
     b.q, b.out = b.q[:0], b.out[:0]
