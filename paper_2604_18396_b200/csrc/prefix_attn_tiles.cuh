@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
     // K of the first tile there; V of tile i and K of tile i + 1 there (4, in turn; tiles are counted over all units); V and K of tile i before
     // free (2); per stream: S done (2), P written (2 x 2), O done (2); Q there; a part there (2), no longer needed (2)
     __shared__ uint64_t bars[20];
-    __shared__ longlong2 s_part[kWpThreads / 32];
+    __shared__ longlong2 s_part[4];
     __shared__ int64_t s_at;
     __shared__ PfEntry s_entry;  // the first one that this CTA has units of
     __shared__ PfSeg s_seg[2];
@@ -133,44 +133,6 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
             asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const T *>(a.q) + token * a.q_tok + y / (DH / 64) * a.q_head + y % (DH / 64) * 64));
         }
     }
-    // ---- this CTA's part of the row of units
-    const bool beside = a.p.groups && !a.p.own;  // single tokens run on the other SMs
-    PfEntry mine = {};
-    int64_t all = 0, blocks = 0, at = 0, none = 0;
-#pragma unroll 1
-    for (int i0 = 0; i0 < D; i0 += kWpThreads) {
-        const int i = i0 + tid;
-        mine = i < D ? pf_entry(a, i, span) : PfEntry{};
-        at = all + pf_scan<kWpThreads / 32>(mine.w, beside && i < D ? pf_blocks(a, i) : 0, s_part, all, blocks);
-    }
-    const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.c.Hkv, beside ? pf_split(everything, blocks * a.c.Hkv * ((gq + 7) / 8), a.c.dh) : kPfCtas, a.p.own);
-    const int64_t x0 = blockIdx.x * share, x1 = min(x0 + share, everything);
-    if (x0 < everything || blockIdx.x == 0) {
-        const int kvh0 = all ? (int)pf_div(x0, all) : 0;
-        const int64_t xl = x0 - kvh0 * all;
-        int64_t base = 0;
-#pragma unroll 1
-        for (int i0 = 0; i0 < D; i0 += kWpThreads) {
-            const int i = i0 + tid;
-            if (D > kWpThreads) {  // (else they are known)
-                mine = i < D ? pf_entry(a, i, span) : PfEntry{};
-                at = base;
-                at += pf_scan<kWpThreads / 32>(mine.w, 0, s_part, base, none);
-            }
-            if (mine.w && at <= xl && xl < at + mine.w) s_first = i, s_kvh = kvh0, s_at = at, s_entry = mine;
-            if (blockIdx.x == 0 && i < D) {  // for who joins the parts
-                if (!a.p.groups || i >= S) a.own_at[a.p.groups ? i - S : i] = at;
-                else if (mine.w) a.group[mine.seq] = PfGroup{at, mine.tok0, mine.n, mine.keys};
-            }
-        }
-        if (blockIdx.x == 0) {
-            if (tid == 0) a.head->all = all, a.head->share = share;
-#pragma unroll 1
-            for (int s = tid; s < S; s += kWpThreads)
-                if (!pf_sound(a, s)) flag(a.status, RIVER_E_BADARG);
-        }
-    }
-    if (x0 >= everything) return;
     if (warp == 1) {
         tc_alloc(smem_u32(&s_tmem), 512u);
         tc_fence_before();
@@ -191,12 +153,50 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        // ---- this CTA's part of the row of units
+        const bool beside = a.p.groups && !a.p.own;  // single tokens run on the other SMs
+        PfEntry mine = {};
+        int64_t all = 0, blocks = 0, at = 0, none = 0;
+#pragma unroll 1
+        for (int i0 = 0; i0 < D; i0 += 128) {
+            const int i = i0 + tid;
+            mine = i < D ? pf_entry(a, i, span) : PfEntry{};
+            at = all + pf_scan(mine.w, beside && i < D ? pf_blocks(a, i) : 0, s_part, all, blocks);
+        }
+        const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.c.Hkv, beside ? pf_split(everything, blocks * a.c.Hkv * ((gq + 7) / 8), a.c.dh) : kPfCtas, a.p.own);
+        const int64_t x0 = blockIdx.x * share, x1 = min(x0 + share, everything);
+        if (x0 < everything || blockIdx.x == 0) {
+            const int kvh0 = all ? (int)pf_div(x0, all) : 0;
+            const int64_t xl = x0 - kvh0 * all;
+            int64_t base = 0;
+#pragma unroll 1
+            for (int i0 = 0; i0 < D; i0 += 128) {
+                const int i = i0 + tid;
+                if (D > 128) {  // (else they are known)
+                    mine = i < D ? pf_entry(a, i, span) : PfEntry{};
+                    at = base;
+                    at += pf_scan(mine.w, 0, s_part, base, none);
+                }
+                if (mine.w && at <= xl && xl < at + mine.w) s_first = i, s_kvh = kvh0, s_at = at, s_entry = mine;
+                if (blockIdx.x == 0 && i < D) {  // for who joins the parts
+                    if (!a.p.groups || i >= S) a.own_at[a.p.groups ? i - S : i] = at;
+                    else if (mine.w) a.group[mine.seq] = PfGroup{at, mine.tok0, mine.n, mine.keys};
+                }
+            }
+            if (blockIdx.x == 0) {
+                if (tid == 0) a.head->all = all, a.head->share = share;
+#pragma unroll 1
+                for (int s = tid; s < S; s += 128)
+                    if (!pf_sound(a, s)) flag(a.status, RIVER_E_BADARG);
+            }
+        }
+        pf_scan_sync();
         if (warp == 2) {  // ---- the parts
             int64_t x = x0, ent = s_at;  // (ent: the weight before the entry, of this KV head)
             int i = s_first, kvh = s_kvh, n = 0;
             PfEntry e = s_entry;
 #pragma unroll 1
-            while (true) {
+            while (x < x1) {
                 int64_t y = x - kvh * all - ent;  // within the entry
 #pragma unroll 1
                 for (int t = pf_unit_at(e, y, span); x < x1 && y < e.w; ++t) {
@@ -362,8 +362,15 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
         const int bpp = a.c.ps_log2 - 4;
         PfSeg g;
         int i0 = 0, count = 0, ended = 0;  // tiles of the parts before; tiles, and parts, of this stream
+        // Part -1 is none: a tile of each stream on whatever tensor memory holds, without waits and arrivals, while this CTA's part of the units is looked for.
+        // It fetches the code: a first tile takes 6 us behind cold caches, where the others take 1.7.  (Not where single tokens take the SM if this CTA has no part:
+        // that the last third of the CTAs has none is likely.)
 #pragma unroll 1
-        for (int n = 0;; ++n) {
+        for (int n = a.p.own || blockIdx.x < 96 ? -1 : 0;; ++n) {
+            const bool dry = n < 0;
+            if (dry) {
+                g = PfSeg{2, 0, 0, 0, 0, 0, 0, 2 * kPfKeys, 0, 0, 0};
+            } else {
             // the part before: where something in it was no number, its rows again
             asm volatile("bar.sync 1, 256;" ::: "memory");
             if (n > 0 && s_poison[(n - 1) & 1] && !*abortp) pf_rows_again<T, DH>(a, g);
@@ -374,8 +381,6 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                 asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %0, 0;\n\tbarrier.cta.red.or.pred p, 1, 256, q;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "+r"(none)::"memory");
                 if (none) break;
             }
-            const int nq = g.n_tok > per ? 2 : 1;
-            const bool dual = nq == 1 && g.n_kt > 1;
             {  // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
                 constexpr int C8 = DH / 8;  // 16-byte chunks of a row; all of a thread's are under way together
                 const int c8 = u0 % C8;
@@ -407,18 +412,21 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                 asm volatile("bar.sync 1, 256;" ::: "memory");  // (s_missing; the part before is through with its s_poison)
                 if (tid == 128) s_missing[(n + 1) & 1] = s_poison[(n + 1) & 1] = 0;
             }
+            }
+            const int nq = g.n_tok > per ? 2 : 1;
+            const bool dual = nq == 1 && g.n_kt > 1;
             float m = -CUDART_INF_F, l = 0.f;
             const int row_q = dual ? 0 : q, p = row_q * per + r / gq;
             if (dual || q < nq) {
                 const int pos = g.pos0 + min(p, g.n_tok - 1);
                 // columns (positions from g.base on) that this row sees, that all rows of the unit see, that some row sees
                 const int hi = g.causal ? pos + 1 - g.base : g.keys, all_hi = g.causal ? g.pos0 + 1 - g.base : g.keys;
-                const bool missing = s_missing[n & 1] != 0;
-                auto huge = [&] { if (fabsf(m) > kWpHuge<T> && m != -CUDART_INF_F) s_poison[n & 1] = 1; };
+                const bool missing = !dry && s_missing[n & 1] != 0;
+                auto huge = [&] { if (fabsf(m) > kWpHuge<T> && m != -CUDART_INF_F && opaque(!dry)) s_poison[n & 1] = 1; };
 #pragma unroll 1
                 for (int j = dual ? q : 0; j < g.n_kt; j += dual ? 2 : 1) {
                     const int i = i0 + j, c0 = kPfKeys * (g.t0 + j);
-                    const bool fresh = opaque(j < (dual ? 2 : 1));
+                    const bool fresh = opaque(j < (dual ? 2 : 1)), run = opaque(!dry);
                     uint32_t valid = 0xffu;  // blocks that are there
                     bool part = c0 + kPfKeys > all_hi;
                     if (opaque(missing)) {
@@ -452,7 +460,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
-                    wp_wait(b_s + 8 * q, count++, abortp, a.polls);
+                    if (run) wp_wait(b_s + 8 * q, count++, abortp, a.polls);
                     __syncwarp();
                     tc_fence_after();
                     uint32_t s[4][32];
@@ -518,7 +526,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                         tc_st32(t_s + 32 * h, w);
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(b_p + 8 * (2 * q + h));
+                        if (lane == 0 && run) mbar_arrive(b_p + 8 * (2 * q + h));
                     };
                     hand_over(0);
                     wp_pin(s[2]);  // (no probability of the second half before the first is handed over)
@@ -529,6 +537,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                     f2_unpack(sum, l0, l1);
                     l += l0 + l1;
                 }
+                if (dry) continue;
                 wp_wait(b_o + 8 * q, ended++, abortp, a.polls);
                 __syncwarp();
                 tc_fence_after();

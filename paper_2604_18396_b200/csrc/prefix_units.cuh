@@ -39,7 +39,7 @@ __device__ __forceinline__ int pf_len(const Paged &c, int len) { return max(0, m
 // whether sequence s goes on with the group of the one before it
 __device__ __forceinline__ bool pf_linked(const PrefixArgs &a, int s) { return s > 0 && a.lead[s] != s && a.lead[s] == a.lead[s - 1] && a.shared[s] == a.shared[s - 1]; }
 // whether what the batch's arrays say of sequence s is as it should be
-static __device__ __noinline__ bool pf_sound(const PrefixArgs &a, int s) {
+__device__ __forceinline__ bool pf_sound(const PrefixArgs &a, int s) {
     const int x = a.q_start[s], y = a.q_start[s + 1], len = a.c.lens[s], sh = a.shared[s];
     return x >= 0 && y >= x && y <= a.p.n_tokens && y - x <= a.max_q && len >= 0 && len <= (a.c.max_pages << a.c.ps_log2) && sh == pf_shared(a.c, sh) && (sh == 0 || len - (y - x) >= sh) &&
            (a.lead[s] == s || pf_linked(a, s));
@@ -62,9 +62,9 @@ __device__ __forceinline__ int64_t pf_blocks(const PrefixArgs &a, int s) {
     return n > 0 && n <= a.p.n_tokens ? (int64_t)n * ((max(0, len - base) >> 4) + 6) : 0;
 }
 
-// Exclusive prefix sum of x over a CTA of 32 WARPS threads, whose sum is added to `total`, and that of y to `other` (part: two per warp).  Ends with a
-// barrier behind every read.
-template <int WARPS>
+// Exclusive prefix sum of x over the 128 threads of warps 0 .. 3, whose sum is added to `total`, and that of y to `other` (part: one per warp).  Ends with a
+// barrier of theirs (number 3) behind every read.
+__device__ __forceinline__ void pf_scan_sync() { asm volatile("bar.sync 3, 128;" ::: "memory"); }
 __device__ __forceinline__ int64_t pf_scan(int64_t x, int64_t y, longlong2 *part, int64_t &total, int64_t &other) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int64_t inc = x;
@@ -75,17 +75,17 @@ __device__ __forceinline__ int64_t pf_scan(int64_t x, int64_t y, longlong2 *part
         if (lane >= o) inc += z;
     }
     if (lane == 31) part[warp] = make_longlong2(inc, y);
-    __syncthreads();
+    pf_scan_sync();
     int64_t before = 0, sum = 0;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
+    for (int w = 0; w < 4; ++w) {
         const longlong2 z = part[w];
         if (w < warp) before += z.x;
         sum += z.x;
         other += z.y;
     }
     total += sum;
-    __syncthreads();
+    pf_scan_sync();
     return before + inc - x;
 }
 
