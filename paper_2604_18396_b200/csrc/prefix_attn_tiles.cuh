@@ -156,14 +156,14 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
         // ---- this CTA's part of the row of units
         const bool beside = a.p.groups && !a.p.own;  // single tokens run on the other SMs
         PfEntry mine = {};
-        int64_t all = 0, blocks = 0, at = 0, none = 0;
+        int64_t all = 0, blocks = 0, at = 0, none = 0;  // (blocks of single tokens; from bit 44 on, units of a KV head)
 #pragma unroll 1
         for (int i0 = 0; i0 < D; i0 += 128) {
             const int i = i0 + tid;
             mine = i < D ? pf_entry(a, i, span) : PfEntry{};
-            at = all + pf_scan(mine.w, beside && i < D ? pf_blocks(a, i) : 0, s_part, all, blocks);
+            at = all + pf_scan(mine.w, beside && i < D ? pf_blocks(a, i) + ((int64_t)((mine.n + span - 1) / span) << 44) : 0, s_part, all, blocks);
         }
-        const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.c.Hkv, beside ? pf_split(everything, blocks * a.c.Hkv * ((gq + 7) / 8), a.c.dh) : kPfCtas, a.p.own);
+        const int64_t everything = all * a.c.Hkv, share = pf_share(everything, a.c.Hkv, blocks >> 44, beside ? pf_split(everything, (blocks & ((1ll << 44) - 1)) * a.c.Hkv * ((gq + 7) / 8), a.c.dh) : kPfCtas, a.p.own);
         const int64_t x0 = blockIdx.x * share, x1 = min(x0 + share, everything);
         if (x0 < everything || blockIdx.x == 0) {
             const int kvh0 = all ? (int)pf_div(x0, all) : 0;

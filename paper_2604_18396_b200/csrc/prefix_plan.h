@@ -93,10 +93,16 @@ PF_FN int pf_unit_at(const PfEntry &e, int64_t y, int span) {
     }
     return lo;
 }
-// Weight of a CTA's part of `everything`, of up to `ctas` CTAs.  Where units are long, of groups that is, as many to each KV head, if there are enough: parts that
-// begin with a KV head's first unit spare the CTAs in between a unit's start and end.
-PF_FN int64_t pf_share(int64_t everything, int Hkv, int ctas, int own) {
-    if (!own && ctas >= Hkv) ctas = pf_min((ctas + Hkv / 2) / Hkv, kPfCtas / Hkv) * Hkv;
+// Weight of a CTA's part of `everything`, of about `ctas` CTAs.  Where units are long, of groups that is, as many to each unit, or to each KV head, if that is
+// near: parts that begin with a unit spare the CTAs in between a second start and end.
+PF_FN int64_t pf_share(int64_t everything, int Hkv, int64_t units, int ctas, int own) {
+    auto align = [&](int64_t n) {
+        const int64_t to = n > kPfCtas ? 0 : pf_min((ctas + n / 2) / n, kPfCtas / n) * n;
+        const bool near = to > 0 && 6 * (to > ctas ? to - ctas : ctas - to) <= ctas;
+        if (near) ctas = (int)to;
+        return near;
+    };
+    if (!own && !align(Hkv * pf_max((int64_t)1, units))) align(Hkv);
     return pf_max((int64_t)pf_div(everything + ctas - 1, ctas), (int64_t)kPfLeast);
 }
 // The tile of a unit that a cut at weight y goes before.  No cut within kPfSnap of a unit's ends: a part of a tile or two would cost a CTA more, for its
@@ -120,12 +126,14 @@ PF_FN PfPart pf_part(const PfPlan &p, int64_t share, int64_t x, const PfUnit &u,
     return r;
 }
 
-// SMs for the groups' units where single tokens run beside them, so that both take the same time: a CTA of units takes 26 us until its first tile is through
-// and after its last (most of it to fetch its code), and 8 us for a thousand of weight; the other SMs 8 us and what HBM needs for their share of `blocks`
-// (K and V of 16 positions of one KV head: 64 dh bytes, at 53 KB/us and SM).  26 + u / x = 8 + b / (n - x).
+// SMs for the groups' units where single tokens run beside them.  u: what the units take, 16 ms for a million of weight with HBM shared; b: what single tokens
+// take for `blocks` (K and V of 16 positions of one KV head, 64 dh bytes, at 53 KB/us and SM).  u / x = 10 + b / (n - x): units first, since single tokens
+// take the SMs that they leave.  (us, 8B-class heads, with x as said: 64 rows behind 8200 positions 48, x 24 less or more 54, 52; 256 rows behind 9000 to
+// 16400 165, 16 less 185, 40 more 170.)
 PF_FN int pf_split(int64_t units, int64_t blocks, int dh) {
-    const float n = kPfCtas, d = 18.f, u = 8e-3f * (float)units, b = 1.2e-3f * (float)dh * (float)blocks;
-    const float p = d * n - u - b, root = sqrtf(p * p + 4.f * d * u * n), x = p > 0.f ? (p + root) / (2.f * d) : 2.f * u * n / (root - p);
+    const float n = kPfCtas, d = -10.f, u = 16e-3f * (float)units, b = 1.2e-3f * (float)dh * (float)blocks;
+    // d x^2 - (d n - u - b) x - u n = 0
+    const float p = d * n - u - b, x = -2.f * u * n / (p - sqrtf(p * p + 4.f * d * u * n));
     return pf_min(kPfCtas, pf_max(1, (int)x));
 }
 

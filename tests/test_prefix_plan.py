@@ -19,13 +19,14 @@ extern "C" int check(int ctas, int n_tokens, int Hkv, int gq, int groups, int ow
     const PfPlan p{n_tokens, Hkv * gq, gq, groups, own, pf_slot_rows(n_tokens, gq)};
     std::vector<PfEntry> e(n);
     std::vector<int64_t> at(n);
-    int64_t all = 0;
+    int64_t all = 0, units = 0;
     for (int i = 0; i < n; ++i) {
         e[i] = kinds[i] ? pf_group_entry(tok0[i], rows[i], 0, keys[i], span) : pf_own_entry(tok0[i], rows[i], 0, base[i], keys[i], span);
         at[i] = all;
         all += e[i].w;
+        units += (e[i].n + span - 1) / span;
     }
-    const int64_t everything = all * Hkv, share = pf_share(everything, Hkv, ctas, own);
+    const int64_t everything = all * Hkv, share = pf_share(everything, Hkv, units, ctas, own);
     if (share * kPfCtas < everything) return 1;
     *most = 0;
     for (int kvh = 0; kvh < Hkv; ++kvh)
