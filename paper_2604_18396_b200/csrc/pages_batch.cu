@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(256) pages_admit_rest_kernel(const AdmitArgs a
 
 // Passes like those of pages_reorder_kernel (pages.cu): refs copied, rows written with their entries counted, free ids counted, then handed out.
 // Bound by them, and by what 16 SMs read and write in them: 512 sequences of 2048 pages on 262144 ids 44 us with a row's entries 32 at a time and the
-// lowest ids given by the cluster's first CTA, 30 with 512 entries and every CTA giving, less with the empty entries left to the other SMs.
+// lowest ids given by the cluster's first CTA, 30 with 512 entries and every CTA giving, 20 with the empty entries left to the other SMs.
 constexpr int kAdUnder = 16;  // times 32 entries of a row under way
 __global__ void __launch_bounds__(kPgThreads) pages_admit_kernel(const AdmitArgs a) {
     extern __shared__ int pg_raw[];
@@ -135,7 +135,8 @@ struct SlotsArgs {
     int32_t *status;
 };
 
-// Every CTA sums up the batch for itself; a thread then finds its tokens' sequences among the sums.
+// Every CTA sums up the batch for itself; a thread then finds its tokens' sequences among the sums.  Bound by those steps one after the other: 8 sequences with
+// a token each 4.6 us, 256 with up to 512 each 6.
 constexpr int kSlTokens = 2;  // of a thread
 __global__ void __launch_bounds__(kPgThreads) pages_slots_kernel(const SlotsArgs a) {
     __shared__ PagesShared s;
@@ -235,7 +236,7 @@ __device__ __forceinline__ void groups_of(const GroupsArgs &a, const int32_t *c,
     }
 }
 
-// equal pages, a warp per sequence
+// Equal pages, a warp per sequence: 1000 rows that share 60 to 1250 pages 5.6 us.  The leads, by one CTA, 5 more, of which the start runs beside it; 8 rows by one CTA 3.5.
 __global__ void __launch_bounds__(256) prefix_equal_kernel(const GroupsArgs a) {
     pdl_launch();
     const int i = blockIdx.x * 8 + (threadIdx.x >> 5);
