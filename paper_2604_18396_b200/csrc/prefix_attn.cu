@@ -73,9 +73,9 @@ PrefixShape prefix_shape(const PrefixArgs &a, int own) {
     return s;
 }
 
-// The scratch: head, groups, weights before the sequences, then maxima and sums, and O, of the parts of units, and of single tokens' own keys.
+// The scratch: head, cut units, groups, weights before the sequences, then maxima and sums, and O, of the parts of units, and of single tokens' own keys.
 struct PrefixScratch {
-    size_t group, own_at, ml, own_ml, o, own_o, bytes;
+    size_t cut, group, own_at, ml, own_ml, o, own_o, bytes;
 };
 PrefixScratch prefix_scratch(int n_seqs, int n_tokens, int Hq, int gq, int dh) {
     const bool both = prefix_both(n_seqs, n_tokens, gq);
@@ -83,7 +83,8 @@ PrefixScratch prefix_scratch(int n_seqs, int n_tokens, int Hq, int gq, int dh) {
                   own_rows = both ? whole : 0;
     auto behind = [](size_t at, size_t bytes) { return (at + bytes + 127) & ~(size_t)127; };
     PrefixScratch s;
-    s.group = behind(0, sizeof(PfHead));
+    s.cut = behind(0, sizeof(PfHead));
+    s.group = behind(s.cut, kPfCtas * sizeof(PfCut));
     s.own_at = behind(s.group, (size_t)n_seqs * sizeof(PfGroup));
     s.ml = behind(s.own_at, (size_t)n_seqs * sizeof(int64_t));
     s.own_ml = behind(s.ml, (size_t)rows * sizeof(float2));
@@ -180,6 +181,7 @@ int prefix_args(const river_paged *c, int layer, int n_tokens, int max_q, int ma
     if (!workspace || workspace_bytes < s.bytes) return RIVER_OK;  // (not every way needs one)
     uint8_t *const w = static_cast<uint8_t *>(workspace);
     a->head = reinterpret_cast<PfHead *>(w);
+    a->cut = reinterpret_cast<PfCut *>(w + s.cut);
     a->group = reinterpret_cast<PfGroup *>(w + s.group);
     a->own_at = reinterpret_cast<int64_t *>(w + s.own_at);
     a->ml = reinterpret_cast<float2 *>(w + s.ml);

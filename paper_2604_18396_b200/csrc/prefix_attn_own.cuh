@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(32 * kStepWarps, kPfOwnCtas<DH>) prefix_own_ke
 // Joining.  A part of a unit lies in the scratch as its CTA had it: its R rows' (the unit's tokens x heads) maxima and sums from ml[row] on, O from o[row * DH]
 // on with four dims of all rows after four dims of all rows.  A warp joins 32 dims of up to eight rows: lane = row k = lane & 7, dims 4 (c + 4 i) .. + 3 of the
 // 32, c = lane >> 3.  Bound by what each step waits for: code, the head, a unit's place, its parts' rows; 5 us for 64 rows of a group beside their own keys (one
-// thread per dim of a row, O in the order of rows: 9), 15 to 20 for the cut units of a batch of prompts, two parts of 256 rows for most of 147 cuts.
+// thread per dim of a row, O in the order of rows: 9), 10 for the cut units of a batch of prompts, two parts of 256 rows for most of 147 cuts.
 __device__ __forceinline__ float pf_inf() { return CUDART_INF_F; }
 __device__ __forceinline__ float pf_nan() { return CUDART_NAN_F; }
 struct PfRows {
@@ -403,35 +403,22 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     }
     if ((lane & 7) < heads) rows.store(static_cast<T *>(a.out) + row * DH + 4 * d4);
 }
-// Sequences' units that were cut: block (c, y) has the unit that the end of CTA c's part cuts, if it is the first cut in there, and a share
-// of its rows.
+// Sequences' units that were cut: block (c, y) has the one that begins in CTA c's part, and a share of its rows.  Its parts are where those CTAs noted that
+// they are: finding them by the arithmetic again, in cold code, took 4 to 8 us more.  (Two rows of a warp under way together gain nothing.)
 constexpr int kJoinBlocks = 4;
 template <class T, int DH>
 __global__ void __launch_bounds__(256, 4) prefix_join_cut_kernel(const __grid_constant__ PrefixArgs a) {
-    const int gq = a.p.gq, span = 2 * pf_per(gq), lane = threadIdx.x & 31;
+    const int gq = a.p.gq, lane = threadIdx.x & 31, c = blockIdx.x;
     pdl_wait();
-    const PfHead h = *a.head;
-    const int64_t cut = (blockIdx.x + 1) * h.share;
-    if (cut >= h.all * a.c.Hkv) return;
-    const int kvh = (int)pf_div(cut, h.all);
-    const int64_t y = cut - kvh * h.all;
-    int lo = 0, hi = a.c.n_seqs;  // the last sequence that begins at or before y (those without units weigh nothing)
+    const PfCut u = a.cut[c];
+    auto head = [&](int k) { return c + k < kPfCtas && a.cut[c + k].head ? 2ll * (c + k) * a.p.slot_rows : -1; };  // first row of CTA c + k's part; -1: nothing there
+    int64_t first = head(lane);
+    if (u.n == 0) return;
+    const int parts = u.last - c + 1;
+    if (lane == 0) first = u.here ? (2ll * c + 1) * a.p.slot_rows : -1;
+    bool any = __any_sync(0xffffffffu, lane < parts && first >= 0);  // (no: one CTA has every tile and the rows are written)
 #pragma unroll 1
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.own_at[mid] <= y) lo = mid; else hi = mid;
-    }
-    const PfEntry e = pf_entry(a, lo, span);
-    if (e.w == 0) return;
-    const int64_t at = a.own_at[lo];
-    const PfUnit u = pf_unit(e, pf_unit_at(e, y - at, span), span);
-    const int64_t x = kvh * h.all + at + u.at;
-    if (x == cut || (int64_t)blockIdx.x * h.share > x) return;  // (not cut here, or cut before)
-    const int parts = pf_parts(h.share, x, u);
-    const int64_t first = pf_part_row(a.p, h.share, x, u, lane, kvh, 0);
-    bool any = false;  // (no: one CTA has every tile and the rows are written)
-#pragma unroll 1
-    for (int k = 0; k < parts; k += 32) any = any || __any_sync(0xffffffffu, pf_part_row(a.p, h.share, x, u, k + lane, kvh, 0) >= 0);
+    for (int k = 32; k < parts; k += 32) any = any || __any_sync(0xffffffffu, k + lane < parts && head(k + lane) >= 0);
     if (!any) return;
     constexpr int Q = DH / 32;
     const int R = u.n * gq, w = blockIdx.y * 8 + (threadIdx.x >> 5), d4 = 8 * (w % Q) + (lane >> 3);
@@ -439,8 +426,9 @@ __global__ void __launch_bounds__(256, 4) prefix_join_cut_kernel(const __grid_co
     for (int r0 = 8 * (w / Q); r0 < R; r0 += 64 * kJoinBlocks / Q) {
         const int r = min(r0 + (lane & 7), R - 1);  // (lanes without a row repeat the last one)
         PfRows rows;
-        rows.add_unit<2>(a, h.share, x, u, kvh, 0, first, r, DH, d4);
-        if (r0 + (lane & 7) < R) rows.store(static_cast<T *>(a.out) + ((size_t)(u.tok + r / gq) * a.p.Hq + kvh * gq + r % gq) * DH + 4 * d4);
+#pragma unroll 1
+        for (int k = 0; k < parts; k += 32) rows.add<2>(a, k ? head(k + lane) : first, min(32, parts - k), r, R, DH, d4);
+        if (r0 + (lane & 7) < R) rows.store(static_cast<T *>(a.out) + ((size_t)(u.tok + r / gq) * a.p.Hq + u.kvh * gq + r % gq) * DH + 4 * d4);
     }
 }
 

@@ -199,6 +199,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
         if (warp == 2) {  // ---- the parts
             int64_t x = x0, ent = s_at;  // (ent: the weight before the entry, of this KV head)
             int i = s_first, kvh = s_kvh, n = 0;
+            if (lane == 0) a.cut[blockIdx.x] = PfCut{};
             PfEntry e = s_entry;
 #pragma unroll 1
             while (x < x1) {
@@ -214,6 +215,12 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                             mbar_arrive(b_seg + 8 * (n & 1));
                         }
                         ++n;
+                    }
+                    if (lane == 0) {  // for who joins the parts
+                        const int64_t from = x - y + u.at, to = from + u.w;
+                        const int there = p.k1 > p.k0 && p.row >= 0;
+                        if (from < x0) a.cut[blockIdx.x].head = there;
+                        else if (to > x0 + share) *reinterpret_cast<int4 *>(a.cut + blockIdx.x) = make_int4(u.tok, u.n, kvh, (int)pf_div(to - 1, share)), a.cut[blockIdx.x].here = there;
                     }
                     x += u.at + u.w - y;
                     y = u.at + u.w;

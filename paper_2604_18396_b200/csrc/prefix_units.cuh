@@ -8,6 +8,10 @@ namespace river {
 struct PfHead {
     int64_t all, share;  // weight of one KV head's units; of a CTA's part
 };
+struct alignas(16) PfCut {  // of a CTA's part: the unit that begins in it and goes on behind it (n 0: none)
+    int32_t tok, n, kvh, last;  // its tokens, the CTA that has its last part
+    int32_t here, head;         // whether this CTA's rows of it are in the scratch; and those of the unit that began before
+};
 struct PfGroup {  // at a group's first sequence
     int64_t at;  // the weight before it
     int32_t tok0, n, keys;
@@ -25,6 +29,7 @@ struct PrefixArgs {
     int32_t *status;
     // scratch
     PfHead *head;
+    PfCut *cut;       // [kPfCtas]
     PfGroup *group;   // [n_seqs]
     int64_t *own_at;        // [n_seqs] the weight before a sequence's units
     float2 *ml, *own_ml;    // [rows]: maximum (log2), sum; of units' parts, of single tokens' own keys
