@@ -7,7 +7,8 @@
 //   of a sequence  its tokens with the positions from its own first one (`shared`, a whole number of pages) up to the row's own
 // Units stand in a row - KV heads outermost, then the groups, then the sequences - and each weighs as many as it has keys, twice that with two
 // query tiles, and kPfCost.  That row is cut into equal parts, one per CTA, whatever the lengths are; the CTA of a part computes, of each unit in it, the key tiles that fall between the
-// cuts.  A part of a unit leaves per row its O, not divided yet, its maximum and its sum; who joins them finds the same cuts by the same arithmetic.
+// cuts.  A part of a unit leaves per row its O, not divided yet, its maximum and its sum; who joins them finds the same
+// cuts by the same arithmetic, or by what the CTAs noted.
 #pragma once
 #include <cmath>
 #include <cstdint>
