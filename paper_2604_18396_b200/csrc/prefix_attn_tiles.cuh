@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                 ent += e.w;
                 int i0 = i + 1;
 #pragma unroll 1
-                while (true) {
+                while (kvh < a.c.Hkv) {  // (always: there is weight left, unless somebody writes the batch's arrays meanwhile)
                     if (i0 >= D) i0 = 0, ++kvh, ent = 0;
                     const unsigned there = __ballot_sync(0xffffffffu, i0 + lane < D && pf_entry(a, i0 + lane, span).w > 0);
                     if (there) {
@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                     }
                     i0 += 32;
                 }
+                if (kvh >= a.c.Hkv) break;
                 e = pf_entry(a, i, span);
             }
             if (n >= 2) wp_wait(b_used + 8 * (n & 1), (n >> 1) - 1, abortp, a.polls);
