@@ -46,9 +46,10 @@ bool prefix_both(int n_seqs, int n_tokens, int gq) { return n_tokens < (int64_t)
 //   single tokens     what is shared comes out of L2, at 13 TB/s, but once
 //   query tiles       a CTA takes 0.9 us for each of its tiles of up to 128 rows, 1.8 for two of them, and 4 to 8 for a unit's start and end
 //   beside them       SMs' shares of HBM (pf_split); 30 us until everything is under way and joined
-// (us, single tokens / groups / both / whole; 8B-class heads: 64 rows behind 8200 positions, 20 to 600 of their own 200 / 51 / 77 / 370; 200 rows in groups of
-// five, 24 query heads, 100 to 2100 shared, f16 97 / 111 / 173 / 260; four beams behind 1500 of the 1B class 16 / 27 / 30 / 30; questions of 17 to 333
-// tokens in groups of four behind 700 to 2300 1120 / - / - / 90.)
+// (us behind cold caches, single tokens / groups / both / whole; 8B-class heads: 64 rows behind 8200 positions, 20 to 600 of their own 197 / 50 / 72 / 360; 200
+// rows in groups of five, 24 query heads, 100 to 2100 shared, f16 97 / 97 / 190 / 266; four beams behind 1500 of the 1B class 12 / 28 / 29 / 25; 108 sequences of
+// 6 to 37 tokens in six groups behind up to 332, two heads 190 / 208 / 64 / 36; questions of 17 to 333 tokens in groups of four behind 700 to 2300
+// 860 / - / - / 86.)
 PrefixShape prefix_shape(const PrefixArgs &a, int own) {
     const int gq = a.p.gq, span = 2 * pf_per(gq);
     const int64_t cap = (int64_t)a.c.max_pages << a.c.ps_log2;
@@ -56,20 +57,21 @@ PrefixShape prefix_shape(const PrefixArgs &a, int own) {
     const double heads = a.c.Hkv, rt = (gq + 7) / 8, tokens = a.p.n_tokens, position = 4.0 * a.c.dh * heads;  // (bytes)
     double step_us, own_us;
     const int step = own_splits(a, cap, 13e6, step_us), own_step = own_splits(a, own, 6e6, own_us);
-    step_us = std::max(step_us, 6.0 + ((double)(cap - own) + (double)a.c.n_seqs * own) * position / 6e6);
+    const double floor_us = ((double)(cap - own) + (double)a.c.n_seqs * own) * position / 6e6;  // (out of HBM)
+    step_us = std::max(step_us, 6.0 + floor_us);
     const double rows = tokens * gq, shared_us = heads * std::ceil(rows / 256.0) * ((cap - own) / 128.0 * (rows <= 128 ? 0.9 : 1.8) + 4.0) / kPfCtas;
     const double idle_us = own_us > 1e299 ? 1e300 : std::max(0.0, (double)a.c.n_seqs * a.max_q - tokens) * heads * rt * 0.0015 * own_step;
     own_us = tokens * heads * rt * (own / 16.0 + 6.0) * a.c.dh * 1.2e-3 / kPfCtas + idle_us;
     const double per_seq = std::max(1.0, tokens / a.c.n_seqs), units = heads * a.c.n_seqs * std::ceil(per_seq / span), tile_us = per_seq * gq <= 128 ? 0.9 : 1.8;
-    const double own_tiles_us = units * (own / 128.0 * tile_us + 8.0) / kPfCtas, whole_us = units * (cap / 128.0 * tile_us + 5.0) / kPfCtas;
+    const double own_tiles_us = units * (own / 128.0 * tile_us + 8.0) / kPfCtas, whole_us = std::max(units * (cap / 128.0 * tile_us + 5.0) / kPfCtas, floor_us);
     PrefixShape s = {kPfStep, step};
     double best = step_us;
+    const double join_us = std::max(0.0, tokens * heads * rt * (a.c.dh / 32) / (8 * 4 * kPfCtas) - 1.0) * 6.0;  // (rounds behind the first, which 25 and 30 have)
     if (prefix_both(a.c.n_seqs, a.p.n_tokens, gq)) {
-        if (30.0 + shared_us + own_us < best) best = 30.0 + shared_us + own_us, s = {kPfGroups, own_step};
-        if (25.0 + shared_us + own_tiles_us < best) s = {kPfBoth, 1};
-    } else if (20.0 + whole_us < best) {
-        s = {kPfWhole, 1};
+        if (30.0 + shared_us + own_us + join_us < best) best = 30.0 + shared_us + own_us + join_us, s = {kPfGroups, own_step};
+        if (25.0 + shared_us + own_tiles_us + join_us < best) best = 25.0 + shared_us + own_tiles_us + join_us, s = {kPfBoth, 1};
     }
+    if (20.0 + whole_us < best) s = {kPfWhole, 1};
     return s;
 }
 
@@ -146,7 +148,8 @@ int launch(PrefixArgs a, PrefixShape s, cudaStream_t st) {
         if (rc || s.mode == kPfStep) return rc;
     }
     if (s.mode == kPfWhole) return launch_beside(prefix_join_cut_kernel<T, DH>, dim3(kPfCtas - 1, kJoinBlocks), 256, 0, st, 1, true, a);
-    return launch_beside(prefix_join_kernel<T, DH>, dim3((unsigned)((a.p.n_tokens * tiles * (DH / 32) + 7) / 8)), 256, 0, st, 1, true, a);
+    const int64_t joins = (a.p.n_tokens * tiles * (DH / 32) + 7) / 8;
+    return launch_beside(joins <= 2 * kPfCtas ? prefix_join_kernel<T, DH, 8, 2> : prefix_join_kernel<T, DH, 3, 4>, dim3((unsigned)joins), 256, 0, st, 1, true, a);
 }
 
 // The arguments of a call, checked.  RIVER_OK with a->n_tokens or a->max_q 0: nothing is to be done.

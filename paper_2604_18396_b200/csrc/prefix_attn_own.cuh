@@ -356,8 +356,10 @@ __device__ __forceinline__ void PfRows::add_unit(const PrefixArgs &a, int64_t sh
 }
 
 // Rows with parts of a group's keys and of their own, a warp per token, up to eight heads of one KV head and 32 dims: 256 / DH tokens' tiles of eight heads per CTA.
-template <class T, int DH>
-__global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant__ PrefixArgs a) {
+// U parts are under way, CTAS CTAs share an SM: 8, 2 where all of them find a place at once, else 3, 4 - calls of 64 rows of one group, 256 of four, 2354 of six
+// take 43, 164, 91 us by the first and 45, 160, 64 by the second.
+template <class T, int DH, int U, int CTAS>
+__global__ void __launch_bounds__(256, CTAS) prefix_join_kernel(const __grid_constant__ PrefixArgs a) {
     constexpr int Q = DH / 32, TILES = 8 / Q;  // warps of a tile; tiles of a CTA
     __shared__ int s_seq[TILES];
     const int gq = a.p.gq, span = 2 * pf_per(gq), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, S = a.c.n_seqs, rt = (gq + 7) / 8, tiles = a.c.Hkv * rt;
@@ -393,13 +395,13 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     if (grouped && g.tok0 >= 0 && g.tok0 <= token && g.n > token - g.tok0 && g.keys > 0 && g.at >= 0 && g.at < h.all) {  // (else lead is no group's first sequence)
         const PfUnit u = pf_unit(pf_group_entry(g.tok0, g.n, lead, g.keys, span), (token - g.tok0) / span, span);
         const int64_t x = kvh * h.all + g.at + u.at;
-        rows.add_unit<8>(a, h.share, x, u, kvh, 1, pf_part_row(a.p, h.share, x, u, lane, kvh, 1), (token - u.tok) * gq + g0 + k, DH, d4);
+        rows.add_unit<U>(a, h.share, x, u, kvh, 1, pf_part_row(a.p, h.share, x, u, lane, kvh, 1), (token - u.tok) * gq + g0 + k, DH, d4);
     }
     if (a.p.own) {
         const PfEntry e = pf_entry(a, S + seq, span);
         const PfUnit u = pf_unit(e, (token - e.tok0) / span, span);
         const int64_t x = kvh * h.all + a.own_at[seq] + u.at;
-        rows.add_unit<8>(a, h.share, x, u, kvh, 0, pf_part_row(a.p, h.share, x, u, lane, kvh, 0), (token - u.tok) * gq + g0 + k, DH, d4);
+        rows.add_unit<U>(a, h.share, x, u, kvh, 0, pf_part_row(a.p, h.share, x, u, lane, kvh, 0), (token - u.tok) * gq + g0 + k, DH, d4);
     }
     if ((lane & 7) < heads) rows.store(static_cast<T *>(a.out) + row * DH + 4 * d4);
 }
