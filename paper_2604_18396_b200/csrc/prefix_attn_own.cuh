@@ -347,7 +347,7 @@ static __device__ __noinline__ int64_t pf_part_row(const PfPlan &p, int64_t shar
 }
 template <int U>
 __device__ __forceinline__ void PfRows::add_unit(const PrefixArgs &a, int64_t share, int64_t x, const PfUnit &u, int kvh, int group, int64_t first, int r, int dh, int d4) {
-    const int n = pf_parts(share, x, u);
+    const int n = min(pf_parts(share, x, u), kPfCtas);
 #pragma unroll 1
     for (int k = 0; k < n; k += 32) {
         if (k) first = pf_part_row(a.p, share, x, u, k + (threadIdx.x & 31), kvh, group);
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(256, CTAS) prefix_join_kernel(const __grid_con
     }
     const PfHead h = *a.head;
     const PfGroup g = grouped ? a.group[lead] : PfGroup{};
-    if (grouped && g.tok0 >= 0 && g.tok0 <= token && g.n > token - g.tok0 && g.keys > 0 && g.at >= 0 && g.at < h.all) {  // (else lead is no group's first sequence)
+    if (grouped && pf_group_has(a.p, g.tok0, g.n, g.keys, token) && g.at >= 0 && g.at < h.all) {  // (else lead is no group's first sequence)
         const PfUnit u = pf_unit(pf_group_entry(g.tok0, g.n, lead, g.keys, span), (token - g.tok0) / span, span);
         const int64_t x = kvh * h.all + g.at + u.at;
         rows.add_unit<U>(a, h.share, x, u, kvh, 1, pf_part_row(a.p, h.share, x, u, lane, kvh, 1), (token - u.tok) * gq + g0 + k, DH, d4);

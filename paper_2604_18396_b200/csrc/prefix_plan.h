@@ -127,6 +127,13 @@ PF_FN PfPart pf_part(const PfPlan &p, int64_t share, int64_t x, const PfUnit &u,
     return r;
 }
 
+// Whether a group of n tokens from tok0 on, as it was noted at its first sequence, can have the row `token`: then its unit's rows, and the places of their parts
+// in the scratch, lie within the batch's.  (Where starts descend, no CTA may have noted the group that a sequence names, and what the scratch held before
+// stands there.  INT32_MAX / 2: no row of a table holds more positions.)
+PF_FN bool pf_group_has(const PfPlan &p, int tok0, int n, int keys, int token) {
+    return tok0 >= 0 && tok0 <= token && token < p.n_tokens && n > token - tok0 && n <= p.n_tokens - tok0 && keys > 0 && keys <= INT32_MAX / 2;
+}
+
 // SMs for the groups' units where single tokens run beside them.  u: what the units take, 16 ms for a million of weight with HBM shared; b: what single tokens
 // take for `blocks` (K and V of 16 positions of one KV head, 64 dh bytes, at 53 KB/us and SM).  u / x = 10 + b / (n - x): units first, since single tokens
 // take the SMs that they leave.  (us, 8B-class heads, with x as said: 64 rows behind 8200 positions 48, x 24 less or more 54, 52; 256 rows behind 9000 to
