@@ -18,8 +18,8 @@
 //
 // Hidden positions: scores are replaced, not added to; V rows that no row of the unit sees are set to zero in shared memory.  A row of V
 // that some rows see and others do not is harmless as long as it is finite (0 x v); tiles that have such rows are looked through (f16: all
-// of their rows), and where one holds an infinity or no number the part is computed again row by row (pf_row).  So it is for scores beyond
-// kWpHuge.
+// of their rows), and where one holds an infinity or no number the part is computed again row by row (pf_row), while the CTA's other warps
+// wait for as long as that moves on.  So it is for scores beyond kWpHuge.  (256 rows of 4096 positions: 60 ms.)
 //
 // Bound by the tensor pipe and the special-function units alike, both two thirds active: 16 prompts of 512 behind 8192 positions, 8B-class heads, 1.13
 // TFLOP in 855 us, 1.32 PFLOP/s (a burst; in a loop of seconds 1.12, by the power cap).  A key tile of two query tiles takes 1.65 us, of one 0.9, and 2.3 beside
@@ -46,9 +46,10 @@ __device__ __forceinline__ int opaque(int x) {
     asm volatile("" : "+r"(x));
     return x;
 }
-// One row over the positions [lo, hi) of a row of the table, by one warp in their order: O (not divided), maximum and sum.
+// One row over the positions [lo, hi) of a row of the table, by one warp in their order: O (not divided), maximum and sum.  A position takes half a microsecond:
+// `moved` goes up every 128 of them, for those who wait.
 template <class T, int DH>
-__device__ void pf_row(const PrefixArgs &a, int token, int head, int seq, int lo, int hi, float (&o)[DH / 32], float &m, float &l) {
+__device__ void pf_row(const PrefixArgs &a, int token, int head, int seq, int lo, int hi, float (&o)[DH / 32], float &m, float &l, int *moved) {
     constexpr int E = DH / 32;
     const int lane = threadIdx.x & 31, kvh = head / a.p.gq, pmask = (1 << a.c.ps_log2) - 1;
     const T *q = static_cast<const T *>(a.q) + token * a.q_tok + head * a.q_head + E * lane, *pool = reinterpret_cast<const T *>(a.c.pool);
@@ -59,6 +60,7 @@ __device__ void pf_row(const PrefixArgs &a, int token, int head, int seq, int lo
     for (int e = 0; e < E; ++e) { x[e] = to_f(q[e]) * a.scale_log2; o[e] = 0.f; }
 #pragma unroll 1
     for (int j = lo; j < hi; ++j) {
+        if (lane == 0 && ((j - lo) & 127) == 0) atomicAdd(moved, 1);
         const int col = j >> a.c.ps_log2, page = col < a.c.max_pages ? a.c.table[(size_t)seq * a.c.max_pages + col] : -1;
         if (page < 0 || page >= a.c.n_pages) continue;
         const T *k = pool + a.c.row(a.layer0, page, 0, kvh, j & pmask) + E * lane, *v = pool + a.c.row(a.layer0, page, 1, kvh, j & pmask) + E * lane;
@@ -76,14 +78,14 @@ __device__ void pf_row(const PrefixArgs &a, int token, int head, int seq, int lo
 
 // The rows of a part, one by one (warps 4 .. 11)
 template <class T, int DH>
-__device__ __noinline__ void pf_rows_again(const PrefixArgs &a, const PfSeg &g) {
+__device__ __noinline__ void pf_rows_again(const PrefixArgs &a, const PfSeg &g, int *moved) {
     const int gq = a.p.gq, lane = threadIdx.x & 31;
 #pragma unroll 1
     for (int x = (threadIdx.x >> 5) - 4; x < g.n_tok * gq; x += 8) {
         const int token = g.tok0 + x / gq, head = g.kvh * gq + x % gq, lo = g.base + kPfKeys * g.t0;
         const int hi = g.base + min(min(g.keys, kPfKeys * (g.t0 + g.n_kt)), g.causal ? g.pos0 + x / gq + 1 - g.base : g.keys);
         float o[DH / 32], m, l;
-        pf_row<T, DH>(a, token, head, g.seq, lo, hi, o, m, l);
+        pf_row<T, DH>(a, token, head, g.seq, lo, hi, o, m, l, moved);
         if (g.row >= 0 && lane == 0) a.ml[g.row + x] = make_float2(m, l);
 #pragma unroll
         for (int e = 0; e < DH / 32; ++e) {
@@ -115,6 +117,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
     __shared__ float2 s_ml[kWpRows];  // dual: the second stream's maxima and sums
     __shared__ uint32_t s_tmem;
     __shared__ int s_first, s_kvh, s_abort, s_no_page, s_poison[2], s_missing[2];
+    __shared__ int s_moved;  // counted up while rows are computed again, which may take longer than the polls of those who wait for its end
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int gq = a.p.gq, per = pf_per(gq), span = 2 * per, S = a.c.n_seqs, D = pf_entries(a);
     const uint32_t b_first = smem_u32(&bars[0]), b_full = b_first + 8, b_free = b_full + 32, b_s = b_free + 16, b_p = b_s + 16, b_o = b_p + 32, b_q = b_o + 16,
@@ -122,7 +125,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
     volatile int *abortp = &s_abort;
     pdl_launch();  // (whatever starts beside this kernel takes no tensor memory)
     if (tid == 0) {
-        s_abort = s_no_page = s_poison[0] = s_poison[1] = s_missing[0] = s_missing[1] = 0;
+        s_abort = s_moved = s_no_page = s_poison[0] = s_poison[1] = s_missing[0] = s_missing[1] = 0;
         s_first = -1;
 #pragma unroll 1
         for (int i = 0; i < 20; ++i) mbar_init(smem_u32(&bars[i]), i >= 9 && i < 13 ? 4 : i == 15 ? 8 : i >= 18 ? 10 : 1);
@@ -147,7 +150,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
     const uint32_t tmem = uniform(s_tmem);
     // the next part; whether there is one.  `used`: told at once that it has been read
     auto take = [&](int n, PfSeg &g) {
-        wp_wait(b_seg + 8 * (n & 1), n >> 1, abortp, a.polls);
+        wp_wait(b_seg + 8 * (n & 1), n >> 1, &s_moved, abortp, a.polls);
         g = s_seg[n & 1];
         return g.n_kt > 0 && !__any_sync(0xffffffffu, *abortp);
     };
@@ -209,7 +212,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                     const PfUnit u = pf_unit(e, t, span);
                     const PfPart p = pf_part(a.p, share, x - y + u.at, u, blockIdx.x, kvh, e.group);
                     if (p.k1 > p.k0) {
-                        if (n >= 2) wp_wait(b_used + 8 * (n & 1), (n >> 1) - 1, abortp, a.polls);
+                        if (n >= 2) wp_wait(b_used + 8 * (n & 1), (n >> 1) - 1, &s_moved, abortp, a.polls);
                         if (lane == 0) {
                             s_seg[n & 1] = PfSeg{p.k1 - p.k0, p.k0, u.tok, u.n, kvh, e.seq, e.base, u.keys, !e.group, e.pos0 + u.tok - e.tok0, p.row};
                             mbar_arrive(b_seg + 8 * (n & 1));
@@ -242,7 +245,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                 if (kvh >= a.c.Hkv) break;
                 e = pf_entry(a, i, span);
             }
-            if (n >= 2) wp_wait(b_used + 8 * (n & 1), (n >> 1) - 1, abortp, a.polls);
+            if (n >= 2) wp_wait(b_used + 8 * (n & 1), (n >> 1) - 1, &s_moved, abortp, a.polls);
             if (lane == 0) {
                 s_seg[n & 1].n_kt = 0;
                 mbar_arrive(b_seg + 8 * (n & 1));
@@ -274,7 +277,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                     ahead = page_of(f, jf + 1);  // (under way while this tile waits for its place)
                 }
                 const uint32_t k_bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, next >= 0)) * 2048u, bar = i < 0 ? b_first : b_full + 8 * (i & 3);
-                if (i >= 2) wp_wait(b_free + 8 * (i & 1), (i >> 1) - 1, abortp, a.polls);
+                if (i >= 2) wp_wait(b_free + 8 * (i & 1), (i >> 1) - 1, &s_moved, abortp, a.polls);
                 if (__any_sync(0xffffffffu, *abortp)) break;
                 if (lane == 0) mbar_expect_tx(bar, bytes + k_bytes);
                 __syncwarp();
@@ -333,7 +336,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
                 if (!more) break;
                 const int n_t = uniform(g.n_kt), nq = g.n_tok > per ? 2 : 1;
                 const bool dual = nq == 1 && n_t > 1;
-                wp_wait(b_q, n, abortp, a.polls);
+                wp_wait(b_q, n, &s_moved, abortp, a.polls);
                 scores(0, 0);
                 if (dual) {
                     next_k();
@@ -386,7 +389,7 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
             } else {
             // the part before: where something in it was no number, its rows again
             asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (n > 0 && s_poison[(n - 1) & 1] && !*abortp) pf_rows_again<T, DH>(a, g);
+            if (n > 0 && s_poison[(n - 1) & 1] && !*abortp) pf_rows_again<T, DH>(a, g, &s_moved);
             if (n > 0) used(n - 1);
             {  // one answer for all eight warps: nobody leaves while others wait at a barrier
                 const bool more = take(n, g);

@@ -98,6 +98,17 @@ __device__ __forceinline__ void wp_wait(uint32_t bar, uint32_t parity, volatile 
     }
     *abort_flag = 1;
 }
+// The same beside warps that may work for longer than that: they count `moved` up while they do, and polls count from its last step.  (Their work ends.)
+__device__ __forceinline__ void wp_wait(uint32_t bar, uint32_t parity, const volatile int *moved, volatile int *abort_flag, uint32_t polls) {
+    int seen = 0;
+    for (uint32_t it = 0; it < polls; ++it) {
+        if (mbar_try_wait(bar, parity & 1u)) return;
+        if (*abort_flag) return;
+        const int now = *moved;
+        if (now != seen) seen = now, it = 0;
+    }
+    *abort_flag = 1;
+}
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // bits lo .. hi - 1 of a word, whatever the ends

@@ -1,0 +1,33 @@
+"""What attention over shared prefixes has to keep at its limits: of waits, of the scratch, of 32 bits (needs a B200).
+
+Tolerances: `paged_reference.attention` derives its own.
+"""
+import pytest
+import torch
+
+from tests import paged_reference as ref
+from tests.test_gpu_prefix_attention import ALL, BF, F16, NAN, WHOLE, Batch, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [BF, F16])
+def test_waits_last_while_rows_are_computed_again(dtype):
+    """300 prompts of two tokens behind the same 4094 positions, two units of 256 rows to a CTA; the last value, which only the second token sees, is infinite.
+    Each part with it takes some 60 ms, a hundred times as long as 4096 polls of the warps that wait for its end may be counted upon."""
+    n, seqs = 4096, 300
+    b = Batch([(0, [(n - 2, 2)])], 128, 1, 64, 64, dtype)
+    page = b.table[0, n // 64 - 1].long()
+    b.pool[0, page, 1, 0, 63, 3] = 0.0
+    want, tol = ref.attention(b.q, b.starts, b.pool, 1, b.table, b.lens, ALL, 0, b.scale)
+    b.pool[0, page, 1, 0, 63, 3] = float("inf")
+    b.lens, b.starts = [n] * seqs, list(range(0, 2 * seqs + 1, 2))
+    b.table, b.lens_t, b.q_start, b.lead, b.shared = b.table.repeat(seqs, 1), i32(b.lens), i32(b.starts), i32(list(range(seqs))), i32([0] * seqs)
+    b.q = b.q.repeat(seqs, 1, 1)
+    b.out = torch.full_like(b.q, NAN)
+    assert b.way(WHOLE, polls=4096) == 0
+    assert b.status.item() == 0
+    out = b.out.double().view(seqs, 2, 128, 64)
+    assert (out[:, 1, :, 3] == float("inf")).all()
+    out[:, 1, :, 3] = want[1, :, 3]
+    assert ((out - want).abs() <= tol).all()
