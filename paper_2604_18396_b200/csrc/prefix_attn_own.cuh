@@ -189,10 +189,11 @@ __global__ void __launch_bounds__(32 * kStepWarps, kPfOwnCtas<DH>) prefix_own_ke
         l0 += __shfl_xor_sync(0xffffffffu, l0, y);
         l1 += __shfl_xor_sync(0xffffffffu, l1, y);
     }
-    // (O and l are held times kStepScale: that goes into the maximum, as other parts have none)
+    // (O and l are held times kStepScale, other parts are not.  It is taken out of them, which is exact, and not out of the maximum: from 2^24 on that has no units.)
+    constexpr float kUnscale = 1.f / kStepScale<T>;
     if (g == 0) {
-        s_ml[warp][2 * t] = make_float2(kHalf ? m0 - 15.f : m0, l0);
-        s_ml[warp][2 * t + 1] = make_float2(kHalf ? m1 - 15.f : m1, l1);
+        s_ml[warp][2 * t] = make_float2(m0, l0 * kUnscale);
+        s_ml[warp][2 * t + 1] = make_float2(m1, l1 * kUnscale);
     }
     if (*abortp) {  // a wait ran out: what has been asked for lands within microseconds; do not use its place before
         if (lane == 0) flag(a.status, RIVER_E_TIMEOUT);
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(32 * kStepWarps, kPfOwnCtas<DH>) prefix_own_ke
 #pragma unroll
     for (int d = 0; d < DH / 16; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s_o[warp][2 * t + (e & 1)][16 * d + g + 8 * (e >> 1)] = o[d][e];
+        for (int e = 0; e < 4; ++e) s_o[warp][2 * t + (e & 1)][16 * d + g + 8 * (e >> 1)] = o[d][e] * kUnscale;
     __syncthreads();
     // the warps' parts: a warp per head, lane = dims
     constexpr int E = DH / 32;

@@ -31,3 +31,26 @@ def test_waits_last_while_rows_are_computed_again(dtype):
     assert (out[:, 1, :, 3] == float("inf")).all()
     out[:, 1, :, 3] = want[1, :, 3]
     assert ((out - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("big", [2048.0, 8192.0, 32768.0])
+def test_equal_scores_of_many_millions_on_both_sides(big):
+    """One key of the shared positions and one of each sequence's own score the same 2^25 and more, all others far less: the mean of their two values.
+
+    Queries and keys are powers of two, so every way has the same score to the last bit, and the probabilities are 1/2 and 1/2 (exact in every type): what is
+    left is one rounding of the result and a few of 32 bits."""
+    for dtype in (F16, BF):
+        b = Batch([(160, [(4, 1), (30, 1), (300, 1)])], 4, 2, 64, 16, dtype)
+        b.q.fill_(big)
+        b.pool[0, :, 0] = torch.where(torch.isnan(b.pool[0, :, 0]), b.pool[0, :, 0], 1.0)
+        b.pool[0, b.table[0, 3].long(), 0, :, 7] = big  # position 55, for all
+        for s, at in enumerate((161, 175, 400)):
+            b.pool[0, b.table[s, at // 16].long(), 0, :, at % 16] = big
+        for way in b.ways():
+            b.out.fill_(NAN)
+            assert b.way(way) == 0 and b.status.item() == 0
+            for s, at in enumerate((161, 175, 400)):
+                v = torch.stack((b.pool[0, b.table[0, 3].long(), 1, :, 7], b.pool[0, b.table[s, at // 16].long(), 1, :, at % 16])).double()
+                want = v.mean(0).repeat_interleave(2, 0)
+                bound = torch.finfo(dtype).eps / 2 * want.abs() + 2.0 ** -20 * v.abs().sum(0).repeat_interleave(2, 0)
+                assert ((b.out[s].double() - want).abs() <= bound).all(), (dtype, way, s)
