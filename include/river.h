@@ -443,9 +443,9 @@ int river_prefix_groups(const river_paged *c, const int32_t *q_start, int least,
  *   shared    [dev] int32 [n_seqs]: a multiple of page_size, the same for a group's sequences, at most lens[s] - n; 0: none
  *   max_own   about the most positions behind the shared ones that a sequence has, new ones included, by which the way of computing is chosen
  *             (0: as many as a row of the table holds); the result does not depend on it but for rounding
- *   workspace [dev] river_prefix_attention_bytes(n_seqs, n_tokens, Hq, Hkv, dh) bytes, 128-byte aligned; what it holds before does not matter, and calls
- *             that may run at the same time have one each.  A small call may do without: where there is none, or less, the call is done or answers
- *             RIVER_E_NOMEM before anything is queued
+ *   workspace [dev] 128-byte aligned; what it holds before does not matter, and calls that may run at the same time have one each.
+ *             river_prefix_attention_bytes(n_seqs, n_tokens, Hq, Hkv, dh) bytes do for every call of at most that many sequences and tokens; this call,
+ *             by the way it goes, takes river_prefix_attention_needs bytes (small calls none).  With less it answers RIVER_E_NOMEM before anything is queued
  *   status    [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as not visible);
  *             lead or shared is not as described, where the way of computing reads them (rows of sequences that it concerns may hold anything); q_start
  *             descends, a length is negative (it counts as 0) or more than a row of the table holds (it counts as that), or a sequence has more than max_q
@@ -464,6 +464,8 @@ int river_selftest_prefix_attention(const river_paged *c, int layer, int n_token
                                     const int32_t *shared, int Hq, const river_rows *q, float softmax_scale, void *out, void *workspace,
                                     size_t workspace_bytes, int32_t *status, int way, int mute, int poll_limit, void *cuda_stream);
 size_t river_prefix_attention_bytes(int n_seqs, int n_tokens, int Hq, int Hkv, int dh); /* 0: a shape that has no kernel */
+/* Bytes of workspace that river_prefix_attention takes with these arguments; 0: none, or arguments that it refuses. */
+size_t river_prefix_attention_needs(const river_paged *c, int n_tokens, int max_q, int max_own, int Hq);
 
 int river_seq_len(const river_ctx *ctx, int slot);       /* tokens cached in the slot, or RIVER_E_BADSLOT */
 int river_release(river_ctx *ctx, int slot);             /* free the slot's pages, behind the work queued so far; does not wait */

@@ -61,7 +61,7 @@ EXPORTS = ("river_argmax_noalloc", "river_profile", "river_profile_read", "river
            "river_selftest_wait_timeout", "river_attention", "river_project_kv", "river_quantize_w4", "river_generate", "river_offload", "river_exit_histogram",
            "river_suggest_offload", "river_rope_frequencies", "river_rope_append", "river_window_attention", "river_pages_advance",
            "river_pages_reorder", "river_pages_compact", "river_selftest_window_timeout", "river_pages_admit", "river_pages_slots", "river_prefix_groups",
-           "river_prefix_attention", "river_prefix_attention_bytes", "river_selftest_prefix_attention")
+           "river_prefix_attention", "river_prefix_attention_bytes", "river_prefix_attention_needs", "river_selftest_prefix_attention")
 
 _lib = None
 
@@ -118,6 +118,8 @@ def load():
     L.river_selftest_prefix_attention.argtypes = L.river_prefix_attention.argtypes[:4] + L.river_prefix_attention.argtypes[5:-1] + [C.c_int, C.c_int, C.c_int, vp]
     L.river_prefix_attention_bytes.argtypes = [C.c_int] * 5
     L.river_prefix_attention_bytes.restype = C.c_size_t
+    L.river_prefix_attention_needs.argtypes = [vp] + [C.c_int] * 4
+    L.river_prefix_attention_needs.restype = C.c_size_t
     L.river_clear_device_error.argtypes = [vp]
     L.river_selftest_wait_timeout.argtypes = [vp, C.c_int]
     L.river_destroy.argtypes = [vp]

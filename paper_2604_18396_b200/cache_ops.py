@@ -290,7 +290,8 @@ def prefix_attention(q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, 
 
     q: [tokens, Hq, dh] of the pool's type (any strides over tokens and heads that are multiples of 8); sequence s has the rows q_start[s] ..
     q_start[s + 1] - 1 (int32 [n_seqs + 1]), its last positions, at most max_q of them; max_own: about the most positions behind the shared ones (0: not
-    known); softmax_scale: default 1 / sqrt(dh); workspace (uint8): prefix_attention_bytes of them, for callers who keep one; calls that may run at the same time have one each."""
+    known); softmax_scale: default 1 / sqrt(dh); workspace (uint8): for callers who keep one,
+    prefix_attention_bytes of them; calls that may run at the same time have one each."""
     _ints(layer | max_q | max_own, "layer, max_q, max_own")
     dev, qs, n = pool.get_device(), q.shape, lens.shape
     c = _cache(pool, table, lens, dev)
@@ -310,12 +311,12 @@ def prefix_attention(q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, 
         except RiverError as e:
             if e.code != -3:
                 raise
-        workspace = _scratch(-(-prefix_attention_bytes(table.shape[0], qs[0], qs[1], pool.shape[3], qs[2]) // 4), pool.device, stream)
+        workspace = _scratch(-(-load().river_prefix_attention_needs(c, qs[0], max_q, max_own, qs[1]) // 4), pool.device, stream)
         used = (*used[:8], workspace, status)
     _run(fn, dev, stream, used, *args, workspace.data_ptr(), workspace.nbytes, word)
 
 
 def prefix_attention_bytes(n_seqs: int, tokens: int, hq: int, hkv: int, dh: int) -> int:
-    """river_prefix_attention_bytes: of the workspace of prefix_attention."""
+    """river_prefix_attention_bytes: of a workspace for every call of prefix_attention with at most that many sequences and tokens."""
     _ints(n_seqs | tokens | hq | hkv | dh, "n_seqs, tokens, heads, dh")
     return load().river_prefix_attention_bytes(n_seqs, tokens, hq, hkv, dh)

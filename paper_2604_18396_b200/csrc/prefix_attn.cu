@@ -38,7 +38,7 @@ struct PrefixShape {
     int splits;  // of single tokens
 };
 
-// whether a sequence has fewer rows than a unit has room for, on average: only then do groups' units save keys, and the scratch has room for them
+// whether a sequence has fewer rows than a unit has room for, on average: only then do groups' units save keys
 bool prefix_both(int n_seqs, int n_tokens, int gq) { return n_tokens < (int64_t)n_seqs * 2 * pf_per(gq); }
 
 // What a call costs in us by each way, and the one that costs least.  `cap`: positions that a row of the table holds, `own`: the most that are a
@@ -50,10 +50,10 @@ bool prefix_both(int n_seqs, int n_tokens, int gq) { return n_tokens < (int64_t)
 // rows in groups of five, 24 query heads, 100 to 2100 shared, f16 97 / 97 / 190 / 266; four beams behind 1500 of the 1B class 12 / 28 / 29 / 25; 108 sequences of
 // 6 to 37 tokens in six groups behind up to 332, two heads 190 / 208 / 64 / 36; questions of 17 to 333 tokens in groups of four behind 700 to 2300
 // 860 / - / - / 86.)
-PrefixShape prefix_shape(const PrefixArgs &a, int own) {
+PrefixShape prefix_shape(const PrefixArgs &a, int max_own) {
     const int gq = a.p.gq, span = 2 * pf_per(gq);
     const int64_t cap = (int64_t)a.c.max_pages << a.c.ps_log2;
-    own = (int)std::min<int64_t>(std::max(1, own), cap);
+    const int own = (int)(max_own ? std::min<int64_t>(max_own, cap) : cap);
     const double heads = a.c.Hkv, rt = (gq + 7) / 8, tokens = a.p.n_tokens, position = 4.0 * a.c.dh * heads;  // (bytes)
     double step_us, own_us;
     const int step = own_splits(a, cap, 13e6, step_us), own_step = own_splits(a, own, 6e6, own_us);
@@ -75,25 +75,30 @@ PrefixShape prefix_shape(const PrefixArgs &a, int own) {
     return s;
 }
 
-// The scratch: head, cut units, groups, weights before the sequences, then maxima and sums, and O, of the parts of units, and of single tokens' own keys.
+// The scratch of a call by one way: head, cut units, groups, weights before the sequences, then maxima and sums, and O: of the parts of units that are cut, of the
+// groups' whole ones, and of the sequences' whole ones or single tokens' own keys.
 struct PrefixScratch {
-    size_t cut, group, own_at, ml, own_ml, o, own_o, bytes;
+    size_t cut, group, own_at, ml, o, bytes;
+    int64_t own_row;  // the first row of the last kind
 };
-PrefixScratch prefix_scratch(int n_seqs, int n_tokens, int Hq, int gq, int dh) {
-    const bool both = prefix_both(n_seqs, n_tokens, gq);
-    const int64_t whole = (int64_t)n_tokens * Hq, rows = pf_cut_rows(PfPlan{n_tokens, Hq, gq, 0, 0, pf_slot_rows(n_tokens, gq)}) + (both ? 2 * whole : 0),
-                  own_rows = both ? whole : 0;
+PrefixScratch prefix_scratch(PrefixMode mode, int n_seqs, int n_tokens, int Hq, int gq, int dh) {
+    const int64_t whole = mode == kPfWhole ? 0 : (int64_t)n_tokens * Hq;
     auto behind = [](size_t at, size_t bytes) { return (at + bytes + 127) & ~(size_t)127; };
-    PrefixScratch s;
+    PrefixScratch s = {};
+    if (mode == kPfStep) return s;
+    s.own_row = pf_cut_rows(PfPlan{n_tokens, Hq, gq, 0, 0, pf_slot_rows(n_tokens, gq)}) + whole;
     s.cut = behind(0, sizeof(PfHead));
     s.group = behind(s.cut, kPfCtas * sizeof(PfCut));
     s.own_at = behind(s.group, (size_t)n_seqs * sizeof(PfGroup));
     s.ml = behind(s.own_at, (size_t)n_seqs * sizeof(int64_t));
-    s.own_ml = behind(s.ml, (size_t)rows * sizeof(float2));
-    s.o = behind(s.own_ml, (size_t)own_rows * sizeof(float2));
-    s.own_o = behind(s.o, (size_t)rows * dh * sizeof(float));
-    s.bytes = s.own_o + (size_t)own_rows * dh * sizeof(float);
+    s.o = behind(s.ml, (size_t)(s.own_row + whole) * sizeof(float2));
+    s.bytes = s.o + (size_t)(s.own_row + whole) * dh * sizeof(float);
     return s;
+}
+// what every call of up to n_seqs sequences and n_tokens tokens can do with, whichever way it goes
+size_t prefix_bytes(int n_seqs, int n_tokens, int Hq, int gq, int dh) {
+    const int both = (int)std::min<int64_t>(n_tokens, (int64_t)n_seqs * 2 * pf_per(gq) - 1);  // the most tokens for which groups' units come into question
+    return std::max(prefix_scratch(kPfBoth, n_seqs, both, Hq, gq, dh).bytes, prefix_scratch(kPfWhole, n_seqs, n_tokens, Hq, gq, dh).bytes);
 }
 
 // a kernel that may start beside the one before it
@@ -131,7 +136,6 @@ int launch_tiles(const PrefixArgs &a, const CUtensorMap &map, cudaStream_t st) {
 }
 template <class T, int DH>
 int launch(PrefixArgs a, PrefixShape s, cudaStream_t st) {
-    if (s.mode != kPfStep && !a.head) return RIVER_E_NOMEM;
     const int64_t tiles = (int64_t)a.c.Hkv * ((a.p.gq + 7) / 8), ctas = s.splits * tiles * a.max_q * a.c.n_seqs;  // (of single tokens)
     if ((s.mode == kPfStep || s.mode == kPfGroups) && ctas > INT32_MAX) return RIVER_E_SHAPE;
     a.p.groups = s.mode == kPfGroups || s.mode == kPfBoth;
@@ -152,24 +156,29 @@ int launch(PrefixArgs a, PrefixShape s, cudaStream_t st) {
     return launch_beside(joins <= 2 * kPfCtas ? prefix_join_kernel<T, DH, 8, 2> : prefix_join_kernel<T, DH, 3, 4>, dim3((unsigned)joins), 256, 0, st, 1, true, a);
 }
 
-// The arguments of a call, checked.  RIVER_OK with a->n_tokens or a->max_q 0: nothing is to be done.
-int prefix_args(const river_paged *c, int layer, int n_tokens, int max_q, int max_own, const int32_t *q_start, const int32_t *lead, const int32_t *shared,
-                int Hq, const river_rows *q, float softmax_scale, void *out, void *workspace, size_t workspace_bytes, int32_t *status, PrefixArgs *a) {
-    *a = PrefixArgs{};
-    if (const int rc = paged_check(c, true, true, &a->c)) return rc;
-    if (layer < 1 || layer > c->n_layers || n_tokens < 0 || max_q < 0 || max_own < 0 || !q_start || !lead || !shared) return RIVER_E_BADARG;
-    if (!words(q_start, lead, shared, status) || Hq < 1 || Hq % c->Hkv || !std::isfinite(softmax_scale)) return RIVER_E_BADARG;
+// The numbers of a call, checked: what the way of computing and the scratch follow from.
+int prefix_numbers(const river_paged *c, int n_tokens, int max_q, int max_own, int Hq, PrefixArgs *a) {
+    if (n_tokens < 0 || max_q < 0 || max_own < 0 || Hq < 1 || Hq % c->Hkv) return RIVER_E_BADARG;
     const int gq = Hq / c->Hkv;
     if (c->n_seqs > 8192 || Hq > 8192 || gq > kWpRows || (int64_t)c->n_seqs * Hq > (1 << 26) || (int64_t)n_tokens * Hq > (1 << 30)) return RIVER_E_SHAPE;
-    a->layer0 = layer - 1;
     a->max_q = std::min(max_q, n_tokens);
+    a->p = PfPlan{n_tokens, Hq, gq, 0, 0, pf_slot_rows(n_tokens, gq)};
+    return RIVER_OK;
+}
+// The arguments of a call, checked.  RIVER_OK with a->n_tokens or a->max_q 0: nothing is to be done.
+int prefix_args(const river_paged *c, int layer, int n_tokens, int max_q, int max_own, const int32_t *q_start, const int32_t *lead, const int32_t *shared,
+                int Hq, const river_rows *q, float softmax_scale, void *out, const void *workspace, int32_t *status, PrefixArgs *a) {
+    *a = PrefixArgs{};
+    if (const int rc = paged_check(c, true, true, &a->c)) return rc;
+    if (layer < 1 || layer > c->n_layers || !q_start || !lead || !shared || !words(q_start, lead, shared, status) || !std::isfinite(softmax_scale)) return RIVER_E_BADARG;
+    if (const int rc = prefix_numbers(c, n_tokens, max_q, max_own, Hq, a)) return rc;
+    a->layer0 = layer - 1;
     a->q_start = q_start;
     a->lead = lead;
     a->shared = shared;
     a->scale_log2 = softmax_scale * 1.4426950408889634f;
     a->out = out;
     a->status = status;
-    a->p = PfPlan{n_tokens, Hq, gq, 0, 0, pf_slot_rows(n_tokens, gq)};
     a->polls = kWaitLimit;
     a->mute = -1;
     if (n_tokens == 0) return RIVER_OK;  // (rows that are none may have no address)
@@ -179,21 +188,22 @@ int prefix_args(const river_paged *c, int layer, int n_tokens, int max_q, int ma
     a->q = q->p;
     a->q_tok = q->token;
     a->q_head = q->head;
-    const PrefixScratch s = prefix_scratch(c->n_seqs, n_tokens, Hq, gq, c->dh);
-    if (!aligned_to(workspace, 128)) return RIVER_E_BADARG;
-    if (!workspace || workspace_bytes < s.bytes) return RIVER_OK;  // (not every way needs one)
-    uint8_t *const w = static_cast<uint8_t *>(workspace);
-    a->head = reinterpret_cast<PfHead *>(w);
-    a->cut = reinterpret_cast<PfCut *>(w + s.cut);
-    a->group = reinterpret_cast<PfGroup *>(w + s.group);
-    a->own_at = reinterpret_cast<int64_t *>(w + s.own_at);
-    a->ml = reinterpret_cast<float2 *>(w + s.ml);
-    a->o = reinterpret_cast<float *>(w + s.o);
-    a->own_ml = reinterpret_cast<float2 *>(w + s.own_ml);
-    a->own_o = reinterpret_cast<float *>(w + s.own_o);
-    return RIVER_OK;
+    return aligned_to(workspace, 128) ? RIVER_OK : RIVER_E_BADARG;
 }
-int launch(const PrefixArgs &a, int dtype, PrefixShape s, cudaStream_t st) {
+int launch(PrefixArgs a, int dtype, PrefixShape s, void *workspace, size_t workspace_bytes, cudaStream_t st) {
+    const PrefixScratch x = prefix_scratch(s.mode, a.c.n_seqs, a.p.n_tokens, a.p.Hq, a.p.gq, a.c.dh);
+    if (x.bytes) {
+        if (!workspace || workspace_bytes < x.bytes) return RIVER_E_NOMEM;
+        uint8_t *const w = static_cast<uint8_t *>(workspace);
+        a.head = reinterpret_cast<PfHead *>(w);
+        a.cut = reinterpret_cast<PfCut *>(w + x.cut);
+        a.group = reinterpret_cast<PfGroup *>(w + x.group);
+        a.own_at = reinterpret_cast<int64_t *>(w + x.own_at);
+        a.ml = reinterpret_cast<float2 *>(w + x.ml);
+        a.o = reinterpret_cast<float *>(w + x.o);
+        a.own_ml = a.ml + x.own_row;
+        a.own_o = a.o + x.own_row * a.c.dh;
+    }
     return dtype == RIVER_BF16 ? (a.c.dh == 64 ? launch<__nv_bfloat16, 64>(a, s, st) : launch<__nv_bfloat16, 128>(a, s, st))
                                : (a.c.dh == 64 ? launch<__half, 64>(a, s, st) : launch<__half, 128>(a, s, st));
 }
@@ -206,27 +216,33 @@ using namespace river;
 extern "C" size_t river_prefix_attention_bytes(int n_seqs, int n_tokens, int Hq, int Hkv, int dh) {
     if (n_seqs < 1 || n_seqs > 8192 || n_tokens < 0 || Hkv < 1 || Hq < 1 || Hq > 8192 || Hq % Hkv || Hq / Hkv > kWpRows || (dh != 64 && dh != 128)) return 0;
     if ((int64_t)n_tokens * Hq > (1 << 30)) return 0;
-    return prefix_scratch(n_seqs, n_tokens, Hq, Hq / Hkv, dh).bytes;
+    return prefix_bytes(n_seqs, n_tokens, Hq, Hq / Hkv, dh);
+}
+
+extern "C" size_t river_prefix_attention_needs(const river_paged *c, int n_tokens, int max_q, int max_own, int Hq) {
+    PrefixArgs a = {};
+    if (paged_check(c, true, true, &a.c) || prefix_numbers(c, n_tokens, max_q, max_own, Hq, &a) || n_tokens == 0 || max_q == 0) return 0;
+    return prefix_scratch(prefix_shape(a, max_own).mode, a.c.n_seqs, n_tokens, Hq, a.p.gq, a.c.dh).bytes;
 }
 
 extern "C" int river_prefix_attention(const river_paged *c, int layer, int n_tokens, int max_q, int max_own, const int32_t *q_start, const int32_t *lead,
                                       const int32_t *shared, int Hq, const river_rows *q, float softmax_scale, void *out, void *workspace,
                                       size_t workspace_bytes, int32_t *status, void *cuda_stream) {
     PrefixArgs a;
-    if (const int rc = prefix_args(c, layer, n_tokens, max_q, max_own, q_start, lead, shared, Hq, q, softmax_scale, out, workspace, workspace_bytes, status, &a)) return rc;
+    if (const int rc = prefix_args(c, layer, n_tokens, max_q, max_own, q_start, lead, shared, Hq, q, softmax_scale, out, workspace, status, &a)) return rc;
     if (a.p.n_tokens == 0 || a.max_q == 0) return RIVER_OK;
-    const int64_t cap = (int64_t)a.c.max_pages << a.c.ps_log2;
-    return launch(a, c->dtype, prefix_shape(a, max_own ? (int)std::min<int64_t>(max_own, cap) : (int)cap), static_cast<cudaStream_t>(cuda_stream));
+    return launch(a, c->dtype, prefix_shape(a, max_own), workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" int river_selftest_prefix_attention(const river_paged *c, int layer, int n_tokens, int max_q, const int32_t *q_start, const int32_t *lead,
                                                const int32_t *shared, int Hq, const river_rows *q, float softmax_scale, void *out, void *workspace,
                                                size_t workspace_bytes, int32_t *status, int way, int mute, int poll_limit, void *cuda_stream) {
     PrefixArgs a;
-    if (const int rc = prefix_args(c, layer, n_tokens, max_q, 0, q_start, lead, shared, Hq, q, softmax_scale, out, workspace, workspace_bytes, status, &a)) return rc;
+    if (const int rc = prefix_args(c, layer, n_tokens, max_q, 0, q_start, lead, shared, Hq, q, softmax_scale, out, workspace, status, &a)) return rc;
     if (a.p.n_tokens == 0 || a.max_q == 0 || way < kPfStep || way > kPfWhole || poll_limit < 1 || poll_limit > (1 << 20)) return RIVER_E_BADARG;
     if ((way == kPfGroups || way == kPfBoth) && !prefix_both(c->n_seqs, n_tokens, a.p.gq)) return RIVER_E_SHAPE;
     a.polls = (uint32_t)poll_limit;
     a.mute = mute;
-    return launch(a, c->dtype, PrefixShape{(PrefixMode)way, way == kPfStep || way == kPfGroups ? 1 + n_tokens % 4 : 1}, static_cast<cudaStream_t>(cuda_stream));
+    return launch(a, c->dtype, PrefixShape{(PrefixMode)way, way == kPfStep || way == kPfGroups ? 1 + n_tokens % 4 : 1}, workspace, workspace_bytes,
+                  static_cast<cudaStream_t>(cuda_stream));
 }

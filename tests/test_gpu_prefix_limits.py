@@ -5,6 +5,7 @@ Tolerances: `paged_reference.attention` derives its own.
 import pytest
 import torch
 
+from paper_2604_18396_b200 import binding, cache_ops, prefix_attention_bytes
 from tests import paged_reference as ref
 from tests.test_gpu_prefix_attention import ALL, BF, F16, NAN, WHOLE, Batch, i32
 
@@ -54,3 +55,36 @@ def test_equal_scores_of_many_millions_on_both_sides(big):
                 want = v.mean(0).repeat_interleave(2, 0)
                 bound = torch.finfo(dtype).eps / 2 * want.abs() + 2.0 ** -20 * v.abs().sum(0).repeat_interleave(2, 0)
                 assert ((b.out[s].double() - want).abs() <= bound).all(), (dtype, way, s)
+
+
+def test_one_workspace_for_large_and_small_calls():
+    """Sized for the largest batch, taken for all: prompts, a few tokens each, single tokens."""
+    most = prefix_attention_bytes(16, 1200, 16, 4, 128)
+    work = torch.full((most,), 0xff, dtype=torch.uint8, device="cuda")
+    for members in ([(0, 75)] * 16, [(10 * i, 40) for i in range(16)], [(i, 60) for i in range(12)], [(3 * i, 9) for i in range(16)], [(5 * i, 1) for i in range(16)]):
+        b = Batch([(512, members)], 16, 4, 128, 16, BF)
+        b.table = torch.nn.functional.pad(b.table, (0, 2048 - b.table.shape[1]), value=-1)
+        want, tol = b.statement()
+        for own in (1, 100, 0):
+            b.out.fill_(NAN)
+            b.call(workspace=work, max_own=own)
+            assert b.status.item() == 0 and ((b.out.double() - want).abs() <= tol).all(), (len(members), own)
+
+
+@pytest.mark.parametrize("members", [[(5 * i, 1) for i in range(60)], [(i, 9) for i in range(16)], [(7 * i, 90) for i in range(5)], [(300, 700)]])
+def test_nothing_is_written_behind_what_a_call_needs(members):
+    b = Batch([(512, members)], 16, 4, 128, 16, BF)
+    want, tol = b.statement()
+    for width in (b.table.shape[1], 2048):
+        b.table = torch.nn.functional.pad(b.table, (0, width - b.table.shape[1]), value=-1)
+        for own in (1, 400, 0):
+            c = cache_ops._cache(b.pool, b.table, b.lens_t, 0)
+            n = binding.load().river_prefix_attention_needs(c, b.q.shape[0], b.max_q, own, 16)
+            work = torch.full((n + (1 << 20),), 0x5a, dtype=torch.uint8, device="cuda")
+            b.out.fill_(NAN)
+            b.call(workspace=work[:n], max_own=own)
+            assert b.status.item() == 0 and ((b.out.double() - want).abs() <= tol).all(), (width, own)
+            assert (work[n:] == 0x5a).all(), (width, own)
+            b.out.fill_(NAN)
+            b.call(max_own=own)
+            assert b.status.item() == 0 and ((b.out.double() - want).abs() <= tol).all(), (width, own)
