@@ -449,7 +449,7 @@ int river_prefix_groups(const river_paged *c, const int32_t *q_start, int least,
  *   status    [dev] int32 or NULL: RIVER_E_BADARG when a page of a visible position is missing or out of range (the position counts as not visible);
  *             lead or shared is not as described, where the way of computing reads them (rows of sequences that it concerns may hold anything); q_start
  *             descends, a length is negative (it counts as 0) or more than a row of the table holds (it counts as that), or a sequence has more than max_q
- *             queries (the rows behind the max_q-th may stay as they are); RIVER_E_TIMEOUT when a wait ran out (any row may then hold anything).
+ *             queries (the rows behind the max_q-th may stay as they are, and have their results else); RIVER_E_TIMEOUT when a wait ran out (any row may then hold anything).
  * Positions that a query does not see have no influence on its result, whatever the pool holds there.  Every result follows in a fixed order of
  * sums: the same inputs give the same bits. */
 int river_prefix_attention(const river_paged *c, int layer, int n_tokens, int max_q, int max_own, const int32_t *q_start, const int32_t *lead,

@@ -366,15 +366,15 @@ __global__ void __launch_bounds__(256, CTAS) prefix_join_kernel(const __grid_con
     const int gq = a.p.gq, span = 2 * pf_per(gq), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, S = a.c.n_seqs, rt = (gq + 7) / 8, tiles = a.c.Hkv * rt;
     const int64_t unit = (int64_t)blockIdx.x * TILES + warp / Q;
     const int first = (int)((int64_t)blockIdx.x * TILES / tiles), token = (int)(unit / tiles), tile = (int)(unit % tiles), kvh = tile / rt, g0 = tile % rt * 8;
-    // the sequences of this CTA's tokens
+    // the sequences of this CTA's tokens (single tokens' kernel has no place for those behind a sequence's max_q-th)
     if (threadIdx.x < TILES) s_seq[threadIdx.x] = -1;
     __syncthreads();
 #pragma unroll 1
     for (int s = threadIdx.x; s < S; s += 256) {
         const int x = a.q_start[s], y = a.q_start[s + 1];
-        if (x >= 0 && y <= a.p.n_tokens)
+        if (x >= 0 && x < y && y <= a.p.n_tokens)
 #pragma unroll 1
-            for (int t = max(x, first); t < min(y, first + TILES); ++t) s_seq[t - first] = s;
+            for (int t = max(x, first); t < min(a.p.own ? y : min(y, x + a.max_q), first + TILES); ++t) s_seq[t - first] = s;
     }
     __syncthreads();
     const int seq = token < a.p.n_tokens ? s_seq[token - first] : -1, lead = seq < 0 ? -1 : a.lead[seq], shared = seq < 0 ? 0 : pf_shared(a.c, a.shared[seq]);

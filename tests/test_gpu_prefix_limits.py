@@ -88,3 +88,21 @@ def test_nothing_is_written_behind_what_a_call_needs(members):
             b.out.fill_(NAN)
             b.call(max_own=own)
             assert b.status.item() == 0 and ((b.out.double() - want).abs() <= tol).all(), (width, own)
+
+
+@pytest.mark.parametrize("dtype", [BF, F16])
+def test_rows_behind_max_q_hold_their_result_or_what_they_held(dtype):
+    """By the way with single tokens nobody computes them, and the scratch (NaN) is not theirs."""
+    b = Batch([(64, [(4, 1), (20, 4), (0, 3)]), (32, [(9, 2), (7, 3)])], 8, 2, 64, 16, dtype)
+    want, tol = b.statement()
+    b.max_q = 2
+    for way in b.ways():
+        b.out.fill_(7.0)
+        b.status.zero_()
+        assert b.way(way) == 0 and b.status.item() == -1
+        right = ((b.out.double() - want).abs() <= tol).all(-1).all(-1)
+        stayed = (b.out == 7.0).all(-1).all(-1)
+        behind = torch.zeros_like(right)
+        for s, n in enumerate((1, 4, 3, 2, 3)):
+            behind[b.starts[s] + 2:b.starts[s] + n] = True
+        assert (right | (stayed & behind)).all(), way
