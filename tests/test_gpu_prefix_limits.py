@@ -1,13 +1,16 @@
-"""What attention over shared prefixes has to keep at its limits: of waits, of the scratch, of 32 bits (needs a B200).
+"""What the operators for requests that share prefixes have to keep at their limits: of waits, of the scratch, of 32 bits, of pages (needs a B200).
 
 Tolerances: `paged_reference.attention` derives its own.
 """
+import random
+
 import pytest
 import torch
 
 from paper_2604_18396_b200 import binding, cache_ops, prefix_attention_bytes
 from tests import paged_reference as ref
 from tests.test_gpu_prefix_attention import ALL, BF, F16, NAN, WHOLE, Batch, i32
+from tests.test_gpu_prefix_batches import run_admit, state
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +109,16 @@ def test_rows_behind_max_q_hold_their_result_or_what_they_held(dtype):
         for s, n in enumerate((1, 4, 3, 2, 3)):
             behind[b.starts[s] + 2:b.starts[s] + n] = True
         assert (right | (stayed & behind)).all(), way
+
+
+def test_admission_refused_leaves_the_state():
+    """Too few pages; one row too short, by a position and by all that 32 bits hold: each by itself, in a table that the deciding CTA writes alone."""
+    rng = random.Random(4)
+    table, lens, refs = state(rng, 5, 10, 16, 60, share=0)
+    refs = [max(r, int(i >= 20)) for i, r in enumerate(refs)]
+    free = sum(r == 0 for r in refs)
+    # (nobody begins with anything: what was held is free again, but for ids from 20 on that nobody held)
+    given_back = sum(-(-n // 16) for n in lens)
+    assert 5 * 10 > free + given_back
+    for total in ([160] * 5, [0, 0, 161, 0, 0], [16, 0, 0, 0, 161], [2 ** 31 - 1] * 5, [0, 2 ** 31 - 1, 0, 0, 0]):
+        assert run_admit(table, lens, refs, [-1] * 5, [0] * 5, total, 16) == [table, lens, refs, [0] * 5, -4], total
