@@ -379,55 +379,56 @@ __global__ void __launch_bounds__(kWpThreads, 1) prefix_tiles_kernel(const __gri
         PfSeg g;
         int i0 = 0, count = 0, ended = 0;  // tiles of the parts before; tiles, and parts, of this stream
         // Part -1 is none: a tile of each stream on whatever tensor memory holds, without waits and arrivals, while this CTA's part of the units is looked for.
-        // It fetches the code: a first tile takes 6 us behind cold caches, where the others take 1.7.  (Not where single tokens take the SM if this CTA has no part:
-        // that the last third of the CTAs has none is likely.)
+        // It fetches the code: a first tile takes 6 us behind cold caches, where the others take 1.7.  Not where single tokens take the SM if this CTA has no part: that
+        // the last third of the CTAs has none is likely.  (us, in no CTA / in the first 96 / in all: 64 rows of a group 46.3 / 44.9 / 43.4, 256 rows of four 147.4 /
+        // 146.7 / 147.8, 40 groups of five 90.8 / 88.7 / 88.4.)
 #pragma unroll 1
         for (int n = a.p.own || blockIdx.x < 96 ? -1 : 0;; ++n) {
             const bool dry = n < 0;
             if (dry) {
                 g = PfSeg{2, 0, 0, 0, 0, 0, 0, 2 * kPfKeys, 0, 0, 0};
             } else {
-            // the part before: where something in it was no number, its rows again
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (n > 0 && s_poison[(n - 1) & 1] && !*abortp) pf_rows_again<T, DH>(a, g, &s_moved);
-            if (n > 0) used(n - 1);
-            {  // one answer for all eight warps: nobody leaves while others wait at a barrier
-                const bool more = take(n, g);
-                uint32_t none = more ? 0u : 1u;
-                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %0, 0;\n\tbarrier.cta.red.or.pred p, 1, 256, q;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "+r"(none)::"memory");
-                if (none) break;
-            }
-            {  // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
-                constexpr int C8 = DH / 8;  // 16-byte chunks of a row; all of a thread's are under way together
-                const int c8 = u0 % C8;
-                const T *src = static_cast<const T *>(a.q) + g.tok0 * a.q_tok + g.kvh * gq * a.q_head + 8 * c8;
-                auto place = [&](int rr) { const int rx = rr % kWpRows; return sq + rr / kWpRows * NB * QB + (c8 >> 3) * QB + rx * 128 + (((c8 & 7) ^ (rx & 7)) * 16); };
-#pragma unroll 4
-                for (int i = 0; i < C8; ++i) {
-                    const int rr = u0 / C8 + i * (256 / C8), rx = rr % kWpRows, pp = rx * inv_gq >> 16, p = rr / kWpRows * per + pp, h = rx - pp * gq;
-                    const bool on = pp < per && p < g.n_tok;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(place(rr))), "l"(on ? src + p * a.q_tok + h * a.q_head : src), "r"(on ? 16 : 0) : "memory");
+                // the part before: where something in it was no number, its rows again
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (n > 0 && s_poison[(n - 1) & 1] && !*abortp) pf_rows_again<T, DH>(a, g, &s_moved);
+                if (n > 0) used(n - 1);
+                {  // one answer for all eight warps: nobody leaves while others wait at a barrier
+                    const bool more = take(n, g);
+                    uint32_t none = more ? 0u : 1u;
+                    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %0, 0;\n\tbarrier.cta.red.or.pred p, 1, 256, q;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "+r"(none)::"memory");
+                    if (none) break;
                 }
-                bool missing = false;
-#pragma unroll 1
-                for (int u = 8 * g.t0 + u0; u < 8 * (g.t0 + g.n_kt) && 16 * u < g.keys; u += 256) {
-                    const int col = ((g.base >> 4) + u) >> bpp, page = col < a.c.max_pages ? a.c.table[(size_t)g.seq * a.c.max_pages + col] : -1;
-                    missing = missing || page < 0 || page >= a.c.n_pages;
-                }
-                if (missing) s_missing[n & 1] = 1;
-                asm volatile("cp.async.wait_all;" ::: "memory");
-                if (turn)
-#pragma unroll 1
+                {  // ---- Q rows in the operand's swizzled order (a negative scale turns their signs); rows that are none are zero
+                    constexpr int C8 = DH / 8;  // 16-byte chunks of a row; all of a thread's are under way together
+                    const int c8 = u0 % C8;
+                    const T *src = static_cast<const T *>(a.q) + g.tok0 * a.q_tok + g.kvh * gq * a.q_head + 8 * c8;
+                    auto place = [&](int rr) { const int rx = rr % kWpRows; return sq + rr / kWpRows * NB * QB + (c8 >> 3) * QB + rx * 128 + (((c8 & 7) ^ (rx & 7)) * 16); };
+    #pragma unroll 4
                     for (int i = 0; i < C8; ++i) {
-                        uint4 *x = reinterpret_cast<uint4 *>(place(u0 / C8 + i * (256 / C8)));
-                        *x = make_uint4(x->x ^ turn, x->y ^ turn, x->z ^ turn, x->w ^ turn);
+                        const int rr = u0 / C8 + i * (256 / C8), rx = rr % kWpRows, pp = rx * inv_gq >> 16, p = rr / kWpRows * per + pp, h = rx - pp * gq;
+                        const bool on = pp < per && p < g.n_tok;
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(place(rr))), "l"(on ? src + p * a.q_tok + h * a.q_head : src), "r"(on ? 16 : 0) : "memory");
                     }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_q);
-                asm volatile("bar.sync 1, 256;" ::: "memory");  // (s_missing; the part before is through with its s_poison)
-                if (tid == 128) s_missing[(n + 1) & 1] = s_poison[(n + 1) & 1] = 0;
-            }
+                    bool missing = false;
+    #pragma unroll 1
+                    for (int u = 8 * g.t0 + u0; u < 8 * (g.t0 + g.n_kt) && 16 * u < g.keys; u += 256) {
+                        const int col = ((g.base >> 4) + u) >> bpp, page = col < a.c.max_pages ? a.c.table[(size_t)g.seq * a.c.max_pages + col] : -1;
+                        missing = missing || page < 0 || page >= a.c.n_pages;
+                    }
+                    if (missing) s_missing[n & 1] = 1;
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    if (turn)
+    #pragma unroll 1
+                        for (int i = 0; i < C8; ++i) {
+                            uint4 *x = reinterpret_cast<uint4 *>(place(u0 / C8 + i * (256 / C8)));
+                            *x = make_uint4(x->x ^ turn, x->y ^ turn, x->z ^ turn, x->w ^ turn);
+                        }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_q);
+                    asm volatile("bar.sync 1, 256;" ::: "memory");  // (s_missing; the part before is through with its s_poison)
+                    if (tid == 128) s_missing[(n + 1) & 1] = s_poison[(n + 1) & 1] = 0;
+                }
             }
             const int nq = g.n_tok > per ? 2 : 1;
             const bool dual = nq == 1 && g.n_kt > 1;
