@@ -431,18 +431,23 @@ int river_pages_slots(const river_paged *c, const int32_t *n_new, int n_tokens, 
  * that both held before their new tokens (lens[s] - (q_start[s + 1] - q_start[s])).  Sequence s goes on with the group of s - 1 where c[s] *
  * page_size >= max(least, page_size); lead[s] is the first sequence of its group, shared[s] page_size times the least c of the group's others (0 for a
  * sequence by itself).
+ * Only neighbours are compared: that requests behind the same prefix follow one another is the caller's order.  Where all requests begin with the same
+ * pages and some share more behind them, a `least` above what all share keeps those groups apart; with less there is one group that shares what all do.
  *   least >= 1;  lead, shared [dev] int32 [n_seqs];  n_seqs <= 8192;  c->pool may be NULL */
 int river_prefix_groups(const river_paged *c, const int32_t *q_start, int least, int32_t *lead, int32_t *shared, void *cuda_stream);
 
 /* Causal attention over all positions of each sequence, where neighbours share their first ones: query i of n of sequence s stands at p = lens[s] -
  * n + i and sees the positions j <= p;  out = softmax(softmax_scale q K^T) V over those, zero where there are none.  The sequences lead[s], .. of a
- * group follow one another, and positions j < shared[s] are read once for all of them, from the row of lead[s] in the table; the others from the
- * sequence's own row.  Every query of a group stands behind its shared positions.
- *   q, q_start, max_q, softmax_scale, out   as river_window_attention has them;  Hq / Hkv at most 128;  n_tokens * Hq at most 2^30;  n_seqs <= 8192
+ * group follow one another, and for positions j < shared[s] their rows of the table hold the same pages: those are read once for all of them, through the
+ * row of lead[s], where that is expected to take less time, else through each sequence's own row.  Every query of a group stands behind its shared positions.
+ *   q, q_start, max_q, softmax_scale, out   as river_window_attention has them;  Hq at most 8192, Hq / Hkv at most 128;  n_tokens * Hq at most 2^30;
+ *             n_seqs <= 8192;  n_pages * 2 * Hkv * page_size below 2^31
  *   lead      [dev] int32 [n_seqs]: the group's first sequence (s itself where s is that, or by itself)
  *   shared    [dev] int32 [n_seqs]: a multiple of page_size, the same for a group's sequences, at most lens[s] - n; 0: none
  *   max_own   about the most positions behind the shared ones that a sequence has, new ones included, by which the way of computing is chosen
- *             (0: as many as a row of the table holds); the result does not depend on it but for rounding
+ *             (0: as many as a row of the table holds); the result does not depend on it but for rounding.  The host takes what a row of the
+ *             table has room for as the sequences' length, and what max_own leaves of that as shared: calls are fastest with tables not much wider than
+ *             the longest sequence and a max_own that is about right (64 tokens behind 8200 positions 44 us, with max_own 0 69)
  *   workspace [dev] 128-byte aligned; what it holds before does not matter, and calls that may run at the same time have one each.
  *             river_prefix_attention_bytes(n_seqs, n_tokens, Hq, Hkv, dh) bytes do for every call of at most that many sequences and tokens; this call,
  *             by the way it goes, takes river_prefix_attention_needs bytes (small calls none).  With less it answers RIVER_E_NOMEM before anything is queued

@@ -9,9 +9,9 @@ Argument marshalling and checks only, like binding.py: every operator is one cal
     lens   int32 [n_seqs]                                                  positions held
     refs   int32 [n_pages]                                                 table entries that hold a page; 0: free
 
-all contiguous CUDA tensors of one device.  status (int32 [1]) takes what only the device can see: rope_append and window_attention write it only
-where something is wrong (the lowest code stays), pages_advance and pages_reorder every time - so not one word for both.  A context's pool (River.kv_pool) is not for them: its page table
-stays with the context.
+all contiguous CUDA tensors of one device.  status (int32 [1]) takes what only the device can see: rope_append, window_attention, prefix_attention and
+pages_slots write it only where something is wrong (the lowest code stays), pages_advance, pages_reorder and pages_admit every time - so not one word for
+both.  A context's pool (River.kv_pool) is not for them: its page table stays with the context.
 """
 from __future__ import annotations
 
@@ -275,7 +275,8 @@ def prefix_groups(table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor
                   least: int = 1, stream=None) -> None:
     """river_prefix_groups: lead[s] = the first sequence of the group that s shares its first pages with, shared[s] = how many positions.
 
-    Groups are neighbours that share `least` positions or more before their new tokens, of which sequence s has q_start[s + 1] - q_start[s]."""
+    Groups are neighbours that share `least` positions or more before their new tokens, of which sequence s has q_start[s + 1] - q_start[s].  A group shares
+    what all of its neighbours do: `least` is above what all requests begin with, where some share more."""
     _ints(page_size | least, "page_size, least")
     dev = table.get_device()
     c = _table(table, lens, 1, page_size, dev)
@@ -286,11 +287,12 @@ def prefix_groups(table: torch.Tensor, lens: torch.Tensor, q_start: torch.Tensor
 def prefix_attention(q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, pool: torch.Tensor, layer: int, table: torch.Tensor, lens: torch.Tensor,
                      lead: torch.Tensor, shared: torch.Tensor, *, max_q: int, max_own: int = 0, softmax_scale: Optional[float] = None,
                      workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None) -> None:
-    """river_prefix_attention: out[t] = causal attention of q[t] over its sequence, the first shared[s] positions read once for the group of lead[s].
+    """river_prefix_attention: out[t] = causal attention of q[t] over its sequence, whose first shared[s] positions the group of lead[s] holds in the same
+    pages; they are read once for all of it where that is expected to take less time.
 
     q: [tokens, Hq, dh] of the pool's type (any strides over tokens and heads that are multiples of 8); sequence s has the rows q_start[s] ..
     q_start[s + 1] - 1 (int32 [n_seqs + 1]), its last positions, at most max_q of them; max_own: about the most positions behind the shared ones (0: not
-    known); softmax_scale: default 1 / sqrt(dh); workspace (uint8): for callers who keep one,
+    known; by that and the table's width the way of computing is chosen: both are best near what the sequences hold); softmax_scale: default 1 / sqrt(dh); workspace (uint8): for callers who keep one,
     prefix_attention_bytes of them; calls that may run at the same time have one each."""
     _ints(layer | max_q | max_own, "layer, max_q, max_own")
     dev, qs, n = pool.get_device(), q.shape, lens.shape
